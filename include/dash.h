@@ -63,8 +63,15 @@ enum {
     DASH_RELU = 4,     /* a * sgn_{0,1}(a): sign gadget + mixed-modulus half gates           */
     DASH_SCALE = 5,    /* CRT scaling by 2, `repeat` times                                  */
     DASH_SIGN = 6,     /* sgn_{-1,1}(a)                                                     */
-    DASH_PROJ = 7      /* n independent unary gates Z_p -> Z_q with per-gate function tables */
+    DASH_PROJ = 7,     /* n independent unary gates Z_p -> Z_q with per-gate function tables */
+    DASH_EXPERTS = 8,  /* out[r][j] = sum_i W_e(r)[j][i] * in[r / top_k][i] (+ bias_e(r)[j])  free gates  */
+    DASH_COMBINE = 9   /* out[t][v] = sum_j gate[t][j] * in[t * top_k + j][v]           free gates  */
 };
+
+/* Weights of an EXPERTS layer: signed bytes, or 4-bit floats with a shared power of two for every 32. */
+enum { DASH_W8 = 0, DASH_MX4 = 1 };
+/* Types of the weights that dash_mx4_quantise reads. */
+enum { DASH_F32 = 0, DASH_BF16 = 1, DASH_F16 = 2 };
 
 typedef struct dash_ctx dash_ctx;
 
@@ -75,6 +82,14 @@ typedef struct {
     int64_t n_elem;
 } dash_labels;
 
+/* The rows of an EXPERTS layer sorted by expert: written by dash_route, read by every layer call of the same rows. */
+typedef struct {
+    void *data;             /* device, dash_route_bytes bytes, 16-byte aligned */
+    const dash_ctx *ctx;    /* the context it was made with */
+    int64_t n;              /* rows */
+    int32_t n_experts;
+} dash_routing;
+
 /* One layer call.  Fields not used by `kind` are ignored. */
 typedef struct {
     int32_t kind;
@@ -82,17 +97,24 @@ typedef struct {
     int64_t elem_base;  /* index, inside the whole layer, of this call's element 0: a layer may be
                            processed in several calls over disjoint element ranges (batch chunks) */
     int64_t n_elem;     /* RELU / SCALE / SIGN / PROJ: values (gates) in this call;
-                           DENSE / CONV2D / SUMPOOL: batch elements in this call */
-    /* DENSE (in_c = K inputs, out_c = M outputs), CONV2D, SUMPOOL (in_h, in_w, in_c) */
+                           DENSE / CONV2D / SUMPOOL: batch elements in this call;
+                           EXPERTS: rows (batch elements * top_k); COMBINE: batch elements of the output */
+    /* DENSE, EXPERTS (in_c = K inputs, out_c = M outputs), CONV2D, SUMPOOL (in_h, in_w, in_c), COMBINE (in_c values) */
     int32_t in_h, in_w, in_c, out_c, kh, kw, stride, pad;
-    const void *weights;  /* device, written by dash_weights_prepare */
-    const int32_t *bias;  /* device int32 [out_c] or NULL: added as bias * (constant-one wire) */
+    const void *weights;  /* device, written by dash_weights_prepare; EXPERTS: dash_weights8_prepare, dash_mx4_quantise */
+    const int32_t *bias;  /* device int32 [out_c] (EXPERTS: [n_experts][out_c]) or NULL: added as bias * (constant-one wire) */
     /* SCALE */
     int32_t repeat;
     /* PROJ: input tensor in->data[p_index], output tensor out->data[q_index] */
     int32_t p_index, q_index;
     const uint8_t *phi;   /* device, function tables, phi[g * phi_stride + a] in [0, q) */
     int64_t phi_stride;   /* p (one table per gate) or 0 (one table for all gates) */
+    /* EXPERTS, COMBINE */
+    int32_t top_k;                 /* rows per batch element, >= 1 */
+    int32_t n_experts;             /* EXPERTS: matrices in `weights`, >= 1 */
+    int32_t weight_format;         /* EXPERTS: DASH_W8 or DASH_MX4 */
+    const dash_routing *routing;   /* EXPERTS: host pointer; NULL with n_experts = 1: every row takes the one matrix (a dense layer) */
+    const int32_t *gates;          /* COMBINE: device int32 [n_elem][top_k], public */
 } dash_layer;
 
 /* Create a context on GPU `hip_device`: the CRT base (distinct primes, primes[0] must be 2 for
@@ -138,6 +160,37 @@ int dash_layer_sizes(const dash_ctx *ctx, const dash_layer *layer, int64_t *out_
  * of the contraction kernels.  w: device int32 [out_c][K] (K = kh*kw*in_c, order [ky][kx][ci]). */
 size_t dash_weights_bytes(const dash_ctx *ctx, int out_c, int K);
 int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void *prepared, void *hip_stream);
+
+/* Layers whose matrix depends on the row (EXPERTS).  Which expert serves a row is public: a garbled circuit is fixed before its
+ * inputs are known, so rows are routed by what is known then (the client, the task, a position), never by a label.
+ *
+ * Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] one after the other, 16-byte aligned, independent of the
+ * primes.  A matrix is cut into tiles of 32 rows x 64 columns, row tiles outermost, zeros past out_c and K.
+ *   DASH_W8   2048 bytes a tile: weight (r, c) at 64 r + 16 ((c / 16) ^ f(r)) + c % 16, f(r) = (r / 2) % 4 ^ (r / 8) % 2
+ *   DASH_MX4  1088 bytes a tile: the codes of (r, c) in byte 32 r + 16 (c / 32) + c % 16, low four bits where (c / 16) % 2 = 0, else
+ *             high; then the shifts, of (r, c) in byte 1024 + 2 r + c / 32.  A code is an e2m1 float: bit 3 the sign, bits 0..2
+ *             the magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6; the weight that enters the layer is the integer 2 * e2m1 * 2^shift. */
+size_t dash_expert_weights_bytes(int format, int n_experts, int out_c, int K);
+/* DASH_W8.  w: device int8, element (e, j, i) at w[e * expert_stride + j * row_stride + i] (row_stride >= K, expert_stride
+ * >= 0). */
+int dash_weights8_prepare(dash_ctx *ctx, const int8_t *w, int64_t row_stride, int64_t expert_stride, int n_experts, int out_c,
+                          int K, void *prepared, void *hip_stream);
+/* DASH_MX4, quantised on the device.  w: device, `dtype` elements, strides in elements as above.  Of 32 consecutive weights of a
+ * row (fewer at its end) with largest magnitude a, the shared exponent is E = floor(log2 a) - 2, brought into
+ * [base, base + max_shift] (-126 <= base <= 125, 0 <= max_shift <= 255; never above 125); each weight becomes the e2m1 value nearest
+ * to w / 2^E, ties to the even code, magnitudes past 6 the 6.  The stored shift is E - base: the layer multiplies by integers in
+ * units of 2^(base - 1), at most 12 * 2^max_shift of them, which is what the product of the primes has to hold beside the
+ * activations.  A NaN counts as 0, an infinity as the largest float32.  values: device, contiguous [n_experts][out_c][K] of
+ * `dtype`, or NULL: the weights that the codes stand for, e2m1 * 2^E (float16 rounds those outside its range). */
+int dash_mx4_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_stride, int64_t expert_stride, int n_experts, int out_c,
+                      int K, int base, int max_shift, void *prepared, void *values, void *hip_stream);
+/* Sorts rows by expert: experts: device int32 [n], the expert of every row in [0, n_experts); any other number: no expert, the
+ * row's outputs are all-zero labels on both sides (the value 0, no bias).  Fills *routing, which the caller keeps (with `data`) as long as layers refer
+ * to it; one routing serves garbler and evaluator, and every layer over the same rows.  `experts` may be changed once the stream
+ * has passed the call. */
+size_t dash_route_bytes(const dash_ctx *ctx, int64_t n, int n_experts);
+int dash_route(dash_ctx *ctx, const int32_t *experts, int64_t n, int n_experts, void *data, dash_routing *routing,
+               void *hip_stream);
 
 /* Gb, one layer: from the zero labels of the layer's input wires produce the zero labels of its
  * output wires and (RELU, SCALE, SIGN, PROJ) its ciphertext tables.  Fresh zero labels come from

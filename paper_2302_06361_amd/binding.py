@@ -13,12 +13,15 @@ _SO = os.path.join(_HERE, "libdash.so")
 
 MAX_PRIMES = 16
 MAX_DIGITS = 16
-DENSE, CONV2D, SUMPOOL, RELU, SCALE, SIGN, PROJ = 1, 2, 3, 4, 5, 6, 7
+DENSE, CONV2D, SUMPOOL, RELU, SCALE, SIGN, PROJ, EXPERTS, COMBINE = 1, 2, 3, 4, 5, 6, 7, 8, 9
+W8, MX4 = 0, 1
+F32, BF16, F16 = 0, 1, 2
 LAMBDA_CEIL, LAMBDA_FLOOR = 0, 1
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 SYMBOLS = ["dash_ctx_create", "dash_ctx_destroy", "dash_lambda", "dash_ctx_offset", "dash_ctx_one", "dash_ctx_digits",
-           "dash_layer_sizes", "dash_weights_bytes", "dash_weights_prepare", "dash_garble_layer", "dash_eval_layer",
+           "dash_layer_sizes", "dash_weights_bytes", "dash_weights_prepare", "dash_expert_weights_bytes", "dash_weights8_prepare",
+           "dash_mx4_quantise", "dash_route_bytes", "dash_route", "dash_garble_layer", "dash_eval_layer",
            "dash_garble_layers", "dash_eval_layers", "dash_eval_layer_noalloc", "dash_input_labels", "dash_encode", "dash_decode", "dash_labels_pack", "dash_labels_unpack", "dash_tables_packed_bytes", "dash_tables_pack", "dash_tables_unpack", "dash_strerror", "dash_profile_enable", "dash_profile_read", "dash_profile_aes"]
 
 
@@ -35,7 +38,13 @@ class CLayer(C.Structure):
                 ("in_h", C.c_int32), ("in_w", C.c_int32), ("in_c", C.c_int32), ("out_c", C.c_int32),
                 ("kh", C.c_int32), ("kw", C.c_int32), ("stride", C.c_int32), ("pad", C.c_int32),
                 ("weights", C.c_void_p), ("bias", C.c_void_p), ("repeat", C.c_int32),
-                ("p_index", C.c_int32), ("q_index", C.c_int32), ("phi", C.c_void_p), ("phi_stride", C.c_int64)]
+                ("p_index", C.c_int32), ("q_index", C.c_int32), ("phi", C.c_void_p), ("phi_stride", C.c_int64),
+                ("top_k", C.c_int32), ("n_experts", C.c_int32), ("weight_format", C.c_int32), ("routing", C.c_void_p),
+                ("gates", C.c_void_p)]
+
+
+class CRouting(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ctx", C.c_void_p), ("n", C.c_int64), ("n_experts", C.c_int32)]
 
 
 _lib = None
@@ -56,6 +65,8 @@ def lib():
         L.dash_strerror.restype = C.c_char_p
         L.dash_weights_bytes.restype = C.c_size_t
         L.dash_tables_packed_bytes.restype = C.c_size_t
+        L.dash_expert_weights_bytes.restype = C.c_size_t
+        L.dash_route_bytes.restype = C.c_size_t
         L.dash_ctx_destroy.restype = None
         _lib = L
     return _lib
@@ -123,6 +134,31 @@ class Labels:
         self.tensors[i][:, :self.n_elem, :].copy_(t)
 
 
+class ExpertWeights:
+    """Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] in one device buffer, `format` W8 or MX4.  Filled by
+    Context.weights8_prepare or Context.mx4_quantise."""
+
+    def __init__(self, ctx, format, n_experts, out_c, K):
+        import torch
+        self.format, self.n_experts, self.out_c, self.K = int(format), int(n_experts), int(out_c), int(K)
+        nbytes = ctx.L.dash_expert_weights_bytes(self.format, self.n_experts, self.out_c, self.K)
+        if nbytes == 0:
+            raise DashError("ExpertWeights: bad format or size")
+        self.data = torch.empty(nbytes, dtype=torch.uint8, device=ctx.device)
+
+
+class Routing:
+    """A dash_routing and its device buffer (Context.route)."""
+
+    def __init__(self, ctx, n, n_experts):
+        import torch
+        self.ctx, self.c = ctx, CRouting()
+        self.data = torch.empty(max(ctx.L.dash_route_bytes(ctx.h, C.c_int64(n), int(n_experts)), 16), dtype=torch.uint8, device=ctx.device)
+
+    def address(self):
+        return C.addressof(self.c)
+
+
 class Layer:
     """A dash_layer descriptor plus the Python objects that keep its device buffers alive."""
 
@@ -131,7 +167,15 @@ class Layer:
         self.c.kind, self.c.layer_id, self.c.n_elem, self.c.elem_base = kind, layer_id, n_elem, elem_base
         self.keep = []
         for k, v in kw.items():
-            if k in ("weights", "bias", "phi"):
+            if isinstance(v, ExpertWeights):
+                self.keep.append(v)
+                self.c.weights, self.c.weight_format = v.data.data_ptr(), v.format
+                self.c.n_experts, self.c.out_c, self.c.in_c = v.n_experts, v.out_c, v.K
+            elif k == "routing":
+                if v is not None:
+                    self.keep.append(v)
+                    self.c.routing = v.address()
+            elif k in ("weights", "bias", "phi", "gates"):
                 if v is not None:
                     self.keep.append(v)
                     setattr(self.c, k, v.data_ptr())
@@ -228,6 +272,58 @@ class Context:
                "dash_weights_prepare")
         torch.cuda.current_stream().synchronize()     # wt may be freed after return
         return buf
+
+    def _expert_matrices(self, w, what, dtypes):
+        """w [n_experts][out_c][K] (or [out_c][K]: one expert) on the context's device, rows contiguous -> the same, three-dimensional"""
+        if w.dim() == 2:
+            w = w[None]
+        if w.dim() != 3 or w.dtype not in dtypes or w.device != self.device or (w.shape[2] > 1 and w.stride(2) != 1) or 0 in w.shape:
+            raise DashError("%s: weights [n_experts][out_c][K] with contiguous rows on %s expected, got %s %s on %s" %
+                            (what, self.device, w.dtype, tuple(w.shape), w.device))
+        return w
+
+    def _expert_out(self, out, format, shape, what):
+        if out is None:
+            return ExpertWeights(self, format, *shape)
+        if (out.format, out.n_experts, out.out_c, out.K) != (format,) + tuple(shape):
+            raise DashError("%s: `out` was made for another format or size" % what)
+        return out
+
+    def weights8_prepare(self, w, out=None):
+        """w: int8 tensor [n_experts][out_c][K] on the device -> ExpertWeights in the W8 format"""
+        import torch
+        w = self._expert_matrices(w, "weights8_prepare", (torch.int8,))
+        out = self._expert_out(out, W8, w.shape, "weights8_prepare")
+        _check(self.L.dash_weights8_prepare(self.h, C.c_void_p(w.data_ptr()), C.c_int64(w.stride(1)), C.c_int64(w.stride(0)), *w.shape,
+                                            C.c_void_p(out.data.data_ptr()), _stream()), "dash_weights8_prepare")
+        return out
+
+    def mx4_quantise(self, w, base, max_shift=255, out=None, values=None):
+        """w: float32, bfloat16 or float16 tensor [n_experts][out_c][K] on the device -> ExpertWeights in the MX4 format: integers
+        2 * e2m1 * 2^shift in units of 2^(base - 1), shift <= max_shift.  values: contiguous tensor like w that receives the
+        weights the codes stand for."""
+        import torch
+        types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+        w = self._expert_matrices(w, "mx4_quantise", types)
+        out = self._expert_out(out, MX4, w.shape, "mx4_quantise")
+        if values is not None and (values.dtype != w.dtype or values.numel() != w.numel() or not values.is_contiguous() or values.device != w.device):
+            raise DashError("mx4_quantise: `values` has to be contiguous and of the size and type of the weights")
+        _check(self.L.dash_mx4_quantise(self.h, C.c_void_p(w.data_ptr()), types[w.dtype], C.c_int64(w.stride(1)), C.c_int64(w.stride(0)), *w.shape,
+                                        int(base), int(max_shift), C.c_void_p(out.data.data_ptr()),
+                                        C.c_void_p(values.data_ptr() if values is not None else 0), _stream()), "dash_mx4_quantise")
+        return out
+
+    def route(self, experts, n_experts, out=None):
+        """experts: int32 tensor [n] on the device, the expert of every row (outside [0, n_experts): none) -> Routing"""
+        import torch
+        if experts.dtype != torch.int32 or experts.device != self.device or not experts.is_contiguous():
+            raise DashError("route: a contiguous int32 tensor on %s expected" % self.device)
+        r = Routing(self, experts.numel(), n_experts) if out is None else out
+        if out is not None and r.data.numel() < self.L.dash_route_bytes(self.h, C.c_int64(experts.numel()), int(n_experts)):
+            raise DashError("route: `out` was made for fewer rows or experts")
+        _check(self.L.dash_route(self.h, C.c_void_p(experts.data_ptr()), C.c_int64(experts.numel()), int(n_experts),
+                                 C.c_void_p(r.data.data_ptr()), C.byref(r.c), _stream()), "dash_route")
+        return r
 
     def input_labels(self, first_wire, zero, n=None):
         """zero labels of the input wires first_wire .. first_wire + n - 1 (n: all elements of `zero` by default)"""

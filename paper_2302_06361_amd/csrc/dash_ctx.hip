@@ -613,6 +613,8 @@ static int run_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_l
         case DASH_DENSE: case DASH_CONV2D: case DASH_SUMPOOL: return linear_layer(c, L, garble, in, out, s);
         case DASH_RELU: case DASH_SCALE: case DASH_SIGN: return activation_layer(c, L, garble, in, out, tables, scratch, s);
         case DASH_PROJ: return proj_layer(c, L, garble, in, out, tables, s);
+        case DASH_EXPERTS: return experts_layer ? experts_layer(c, L, garble, in, out, s) : DASH_EUNSUPPORTED;
+        case DASH_COMBINE: return combine_layer ? combine_layer(c, L, in, out, s) : DASH_EUNSUPPORTED;
     }
     return DASH_EINVAL;
 }

@@ -140,6 +140,10 @@ int linear_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_label
 bool dense_mfma_wanted(const dash_layer* L, int64_t batch);
 int dense_mfma(dash_ctx* c, const dash_layer* L, bool garble, const dash_labels* in, dash_labels* out, hipStream_t s);
 
+// layers of experts (dash_experts.hip; weak: host builds of the other sources do without them)
+__attribute__((weak)) int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labels* in, dash_labels* out, hipStream_t s);
+__attribute__((weak)) int combine_layer(dash_ctx* c, const dash_layer* L, const dash_labels* in, dash_labels* out, hipStream_t s);
+
 // true if every vector of lam digits below m is below 2^128 as a base-m number (m^lam <= 2^128)
 inline bool fits_128_bits(uint32_t m, uint32_t lam) {
     if ((m & (m - 1)) == 0) { uint32_t t = 0; while ((1u << t) < m) t++; return t * lam <= 128; }

@@ -828,6 +828,12 @@ int layer_sizes(const dash_ctx* c, const dash_layer* L, int64_t* out_elems, size
             if (L->p_index < 0 || L->p_index >= c->k || L->q_index < 0 || L->q_index >= c->k) return DASH_EINVAL;
             oe = E; tb = (size_t)E * c->prime[L->p_index] * pitch_of(c, c->prime[L->q_index]); break;
         }
+        case DASH_EXPERTS:
+            if (L->in_c < 1 || L->out_c < 1 || L->top_k < 1 || L->n_experts < 1 || E % L->top_k) return DASH_EINVAL;
+            oe = L->out_c; break;
+        case DASH_COMBINE:
+            if (L->in_c < 1 || L->top_k < 1) return DASH_EINVAL;
+            oe = L->in_c; break;
         default: return DASH_EINVAL;
     }
     if (out_elems) *out_elems = oe;
@@ -869,7 +875,7 @@ static int table_segments(const dash_ctx* c, const dash_layer* L, std::vector<Se
             if (L->p_index < 0 || L->p_index >= k || L->q_index < 0 || L->q_index >= k) return DASH_EINVAL;
             out.push_back(SegDesc{(uint32_t)c->prime[L->p_index], (uint32_t)c->prime[L->q_index]});
             return DASH_OK;
-        case DASH_DENSE: case DASH_CONV2D: case DASH_SUMPOOL: return DASH_OK;       // free gates: no tables
+        case DASH_DENSE: case DASH_CONV2D: case DASH_SUMPOOL: case DASH_EXPERTS: case DASH_COMBINE: return DASH_OK;       // free gates: no tables
     }
     return DASH_EINVAL;
 }

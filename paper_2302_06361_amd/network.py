@@ -31,16 +31,53 @@ def build_layers(ctx, net, b, batch_base):
         elif kind == "scale":
             lay = B.Layer(B.SCALE, L["id"], n * b, elem_base=batch_base * n, repeat=L["repeat"])
             lay.per_batch_element = n
+        elif kind == "experts":
+            # rows of a batch element, each through the matrix of its (public) expert
+            if L.get("base") is None:
+                w = ctx.weights8_prepare(torch.as_tensor(np.asarray(L["W"], dtype=np.int8)).to(ctx.device))
+            else:
+                w = ctx.mx4_quantise(torch.as_tensor(np.asarray(L["W"], dtype=np.float32)).to(ctx.device), L["base"], L["max_shift"])
+            bias = None
+            if L.get("bias") is not None:
+                bias = torch.as_tensor(np.asarray(L["bias"], dtype=np.int32)).to(ctx.device)
+            routing = None
+            if L.get("route") is not None:
+                routing = _PerBatch(L["route"], L["rows"], ctx)
+            lay = B.Layer(B.EXPERTS, L["id"], b * L["rows"], top_k=L["top_k"], weights=w, bias=bias)
+            if routing is not None:
+                lay.routing = ctx.route(routing.part(batch_base, b), w.n_experts)
+                lay.c.routing = lay.routing.address()
+                lay.rebase = lambda base, lay=lay, r=routing, e=w.n_experts: ctx.route(r.part(base, b), e, out=lay.routing)
+        elif kind == "combine":
+            gates = _PerBatch(L["gates"], L["rows"] * L["top_k"], ctx)
+            part = gates.part(batch_base, b).clone()
+            lay = B.Layer(B.COMBINE, L["id"], b * L["rows"], in_c=L["V"], top_k=L["top_k"], gates=part)
+            lay.rebase = lambda base, part=part, g=gates: part.copy_(g.part(base, b))
         else:
             raise ValueError(kind)
         oe, tb, sb = ctx.layer_sizes(lay)
         if kind in ("conv", "sumpool"):
             n = oe
+        elif kind in ("experts", "combine"):
+            n = oe * L["rows"]
         layers.append(lay)
         table_bytes.append(tb)
         scratch_max = max(scratch_max, sb)
         sizes.append(n * b)
     return layers, sizes, table_bytes, scratch_max
+
+
+class _PerBatch:
+    """int32 entries of the whole batch on the device, `per` for every batch element"""
+
+    def __init__(self, values, per, ctx):
+        import torch
+        self.per, self.all = per, torch.as_tensor(np.asarray(values, dtype=np.int32).reshape(-1)).to(ctx.device)
+
+    def part(self, base, b):
+        if (base + b) * self.per > self.all.numel():
+            raise ValueError("experts or gates of batch elements %d..%d are missing" % (base, base + b - 1))
+        return self.all[base * self.per:(base + b) * self.per]
 
 
 class GarbledNetwork:
@@ -111,6 +148,8 @@ class StreamedNetwork:
             n = getattr(lay, "per_batch_element", None)
             if n is not None:
                 lay.c.elem_base = self.batch_base * n
+            if hasattr(lay, "rebase"):
+                lay.rebase(self.batch_base)
 
     def run(self, x_dev, on_boundary=None):
         """Gb, En, Ev, De over the whole network.  on_boundary(b, zero, act) sees the label bundles of

@@ -16,6 +16,9 @@ Network format: a dict with
      relu    : n (values per batch element)
      scale   : n, repeat      (repeat halvings = division by 2**repeat)
      sign    : n
+     experts : rows (per batch element), top_k (rows per input), W [experts][out_c][K]: int8, or float32 with base and max_shift
+               (quantised to 4-bit floats by the library), route int32 [batch * rows] (-1: no expert) or none, bias [experts][out_c] (opt.)
+     combine : rows (outputs per batch element), top_k, V (values per row), gates int32 [batch * rows][top_k]
 Tensors of one batch element are ordered [y][x][channel].
 """
 import numpy as np
@@ -170,6 +173,33 @@ def tiny_cnn(seed=8, k=4, batch=2, repeat=1):
     if repeat:
         b.scale(repeat)
     b.dense(3)
+    return b.net
+
+
+def mixture(seed=9, batch=4, k=8, n_in=48, hidden=32, n_out=10, experts=4, top_k=2, repeat=3, mx4=True):
+    """A mixture of experts with public routing: dense, ReLU, scale, then per batch element top_k two-layer experts (4-bit or
+    8-bit weights, ReLU and scale between), joined with integer gates, dense.  One row has no expert."""
+    b = _Builder(seed, k, batch, n_in, -7, 7)
+    g = b.g
+    b.net["x"] = g.integers(0, 16, batch * n_in).astype(np.int64)
+    b.dense(hidden); b.relu(); b.scale(repeat)
+    route = np.array([g.permutation(experts)[:top_k] for _ in range(batch)], np.int32).reshape(-1)
+    if batch * top_k > 3:
+        route[3] = -1
+
+    def matrices(M, K):
+        if not mx4:
+            return dict(W=g.integers(-8, 8, (experts, M, K)).astype(np.int8))
+        return dict(W=g.standard_normal((experts, M, K)).astype(np.float32), base=-2, max_shift=2)
+    b._add(dict(kind="experts", id=b.lid(), rows=top_k, top_k=top_k, route=route, **matrices(2 * hidden, hidden)))
+    b.n = top_k * 2 * hidden
+    b.relu(); b.scale(repeat)
+    b._add(dict(kind="experts", id=b.lid(), rows=top_k, top_k=1, route=route, bias=g.integers(-20, 20, (experts, hidden)).astype(np.int32),
+                **matrices(hidden, 2 * hidden)))
+    b._add(dict(kind="combine", id=b.lid(), rows=1, top_k=top_k, V=hidden, gates=g.integers(0, 4, (batch, top_k)).astype(np.int32)))
+    b.n = hidden
+    b.relu(); b.scale(repeat)
+    b.dense(n_out)
     return b.net
 
 
