@@ -8,7 +8,7 @@
 //   k_route_count / _scan / _fill : rows sorted by expert, in order inside an expert
 //   k_weights8_prepare            : signed bytes into the tiles of the products
 //   k_mx4_quantise                : weights to 4-bit floats with a power of two for every 32, into the tiles of the products
-//   k_experts                     : the products
+//   (the products: dash_experts_gemm.hip)
 //   k_combine                     : the weighted sums
 #include <hip/hip_bf16.h>
 #include <string.h>
@@ -23,8 +23,9 @@ constexpr int kWaves = kThreads / 64;
 struct RouteArgs {
     const int32_t* experts;
     int64_t n;
-    int E;
-    int32_t *offsets, *rows;
+    int E, k;
+    uint8_t nchunk[DASH_MAX_PRIMES];
+    RoutingView to;
 };
 __device__ __forceinline__ bool route_match(int32_t id, int e, int E) { return e < E ? id == e : (uint32_t)id >= (uint32_t)E; }
 
@@ -37,35 +38,61 @@ __global__ __launch_bounds__(kThreads) void k_route_count(const RouteArgs A) {
         const bool hit = r0 + lane < A.n && route_match(A.experts[r0 + lane], e, A.E);
         count += __popcll(__ballot(hit));
     }
-    if (lane == 0) A.offsets[e + 1] = count;
+    if (lane == 0) A.to.offsets[e + 1] = count;
 }
-// One block: counts to offsets.
+__device__ __forceinline__ int32_t route_tiles(const RouteArgs& A, int32_t rows, int groups) {
+    int32_t t = 0;
+    for (int i = 0; i < A.k; i++) t += (int32_t)(((int64_t)rows * A.nchunk[i] + groups - 1) / groups);
+    return t;
+}
+// One block: counts to offsets and to first tiles.
 __global__ __launch_bounds__(kThreads) void k_route_scan(const RouteArgs A) {
-    __shared__ int32_t part[kThreads];
+    __shared__ int32_t part[1 + kTileSizes][kThreads];
     const int n = A.E + 1, per = (n + kThreads - 1) / kThreads, e0 = threadIdx.x * per, e1 = e0 + per < n ? e0 + per : n;
-    int32_t sum = 0;
-    for (int e = e0; e < e1; e++) sum += A.offsets[e + 1];
-    part[threadIdx.x] = sum;
+    int32_t sum[1 + kTileSizes] = {};
+    for (int e = e0; e < e1; e++) {
+        const int32_t rows = A.to.offsets[e + 1];
+        sum[0] += rows;
+        for (int s = 0; s < kTileSizes; s++) sum[1 + s] += route_tiles(A, rows, kTileGroups[s]);
+    }
+    for (int s = 0; s < 1 + kTileSizes; s++) part[s][threadIdx.x] = sum[s];
     __syncthreads();
-    if (threadIdx.x == 0) {
+    if (threadIdx.x < 1 + kTileSizes) {
         int32_t at = 0;
-        for (int i = 0; i < kThreads; i++) { const int32_t s = part[i]; part[i] = at; at += s; }
-        A.offsets[0] = 0;
+        for (int i = 0; i < kThreads; i++) { const int32_t v = part[threadIdx.x][i]; part[threadIdx.x][i] = at; at += v; }
     }
     __syncthreads();
-    int32_t at = part[threadIdx.x];
-    for (int e = e0; e < e1; e++) { at += A.offsets[e + 1]; A.offsets[e + 1] = at; }
+    if (threadIdx.x == 0) {
+        A.to.offsets[0] = 0;
+        for (int s = 0; s < kTileSizes; s++) A.to.first_tile[s][0] = 0;
+    }
+    for (int s = 0; s < 1 + kTileSizes; s++) sum[s] = part[s][threadIdx.x];
+    for (int e = e0; e < e1; e++) {
+        const int32_t rows = A.to.offsets[e + 1];
+        sum[0] += rows;
+        A.to.offsets[e + 1] = sum[0];
+        for (int s = 0; s < kTileSizes; s++) { sum[1 + s] += route_tiles(A, rows, kTileGroups[s]); A.to.first_tile[s][e + 1] = sum[1 + s]; }
+    }
 }
-// The wave of an expert writes its rows in ascending order.
+// The wave of an expert writes its rows in ascending order, and its tiles.
 __global__ __launch_bounds__(kThreads) void k_route_fill(const RouteArgs A) {
     const int e = (int)(blockIdx.x * kWaves + threadIdx.x / 64), lane = threadIdx.x & 63;
     if (e > A.E) return;
-    int32_t at = A.offsets[e];
+    const int32_t start = A.to.offsets[e], count = A.to.offsets[e + 1] - start;
+    int32_t at = start;
     for (int64_t r0 = 0; r0 < A.n; r0 += 64) {
         const bool hit = r0 + lane < A.n && route_match(A.experts[r0 + lane], e, A.E);
         const uint64_t m = __ballot(hit);
-        if (hit) A.rows[at + __popcll(m & ((1ull << lane) - 1))] = (int32_t)(r0 + lane);
+        if (hit) A.to.rows[at + __popcll(m & ((1ull << lane) - 1))] = (int32_t)(r0 + lane);
         at += __popcll(m);
+    }
+    for (int s = 0; s < kTileSizes; s++) {
+        int32_t t0 = A.to.first_tile[s][e];
+        for (int i = 0; i < A.k; i++) {
+            const int32_t tiles = (int32_t)(((int64_t)count * A.nchunk[i] + kTileGroups[s] - 1) / kTileGroups[s]);
+            for (int32_t t = lane; t < tiles; t += 64) A.to.tiles[s][t0 + t] = RouteTile{(uint32_t)e | (uint32_t)i << 24, start, count, t * kTileGroups[s]};
+            t0 += tiles;
+        }
     }
 }
 
@@ -127,7 +154,7 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
     E = E > A.base + A.max_shift ? A.base + A.max_shift : E;
     E = E < A.base ? A.base : E;
     const float inv = __uint_as_float((uint32_t)(127 - E) << 23);                                     // E in [-126, 125]
-    const float two = E > -127 ? __uint_as_float((uint32_t)(127 + E) << 23) : 0.0f;
+    const float two = __uint_as_float((uint32_t)(127 + E) << 23);
     uint32_t code[4] = {0, 0, 0, 0};
     for (int i = 0; i < 32; i++) {
         const float a = __builtin_fabsf(v[i]) * inv;
@@ -145,68 +172,9 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
     dst[kMx4Codes + 2 * r + b] = (uint8_t)(E - A.base);
 }
 
-// ---- products ----------------------------------------------------------------------------------
-struct ExpPrime {
-    uint32_t p;
-    const uint8_t* one;     // chunked label of the constant-one wire, or NULL
-    LView in, out;
-};
-struct ExpArgs {
-    const ModInfo* mods;
-    const uint8_t* w;
-    const int32_t *bias, *offsets, *rows;
-    int64_t n;
-    int M, K, E, top_k, format;
-    ExpPrime pr[DASH_MAX_PRIMES];
-};
 __device__ __forceinline__ uint32_t signed_mod(int32_t v, const ModInfo& M) {
     const int32_t r = v % (int32_t)M.m;
     return (uint32_t)(r < 0 ? r + (int32_t)M.m : r);
-}
-// a lane per (row in routing order, output feature, 16-digit chunk); blockIdx.y = prime
-__global__ __launch_bounds__(kThreads) void k_experts(const ExpArgs A) {
-    const ExpPrime& P = A.pr[blockIdx.y];
-    const ModInfo M = A.mods[P.p];
-    const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x, per = A.n * A.M;
-    if (idx >= per * M.nchunk) return;
-    const int64_t ch = idx / per, at = (idx - ch * per) / A.M;
-    const int j = (int)((idx - ch * per) % A.M);
-    int e = 0;
-    int64_t row = at;
-    if (A.offsets) {
-        int lo = 0, hi = A.E;            // the expert whose rows hold number `at`
-        while (lo < hi) { const int mid = (lo + hi + 1) / 2; if (A.offsets[mid] <= at) lo = mid; else hi = mid - 1; }
-        e = lo;
-        row = A.rows[at];
-    }
-    uint32_t acc[16] = {};
-    if (e < A.E) {
-        const int64_t kt = col_tiles(A.K), tb = tile_bytes(A.format);
-        const uint8_t* w = A.w + e * matrix_bytes(A.format, A.M, A.K) + (int64_t)(j / kTileRows) * kt * tb;
-        const uint8_t* x = P.in.p + ch * P.in.cs + row / A.top_k * A.K * 16;
-        const int r = j % kTileRows;
-        for (int k = 0; k < A.K; k++) {
-            const uint8_t* t = w + (int64_t)(k / kTileCols) * tb;
-            const int c = k % kTileCols;
-            uint32_t wk;
-            if (A.format == DASH_MX4) {
-                const uint32_t code = t[32 * r + 16 * (c / 32) + c % 16] >> ((c / 16) % 2 * 4) & 15u, m = code & 7u;
-                const int32_t mag = (int32_t)(m < 4 ? m : m == 7 ? 12u : 2 * m - 4);
-                uint32_t two = 1;
-                for (int s = t[kMx4Codes + 2 * r + c / 32]; s > 0; s--) two = 2 * two % M.m;
-                wk = signed_mod((code & 8u ? -mag : mag) * (int32_t)two, M);
-            } else wk = signed_mod((int8_t)t[w8_at(r, c)], M);
-            for (int d = 0; d < 16; d++) acc[d] += wk * x[(int64_t)k * 16 + d];
-        }
-        const uint32_t bm = A.bias ? signed_mod(A.bias[(int64_t)e * A.M + j], M) : 0;
-        for (int d = 0; d < 16; d++) {
-            acc[d] %= M.m;
-            if (A.bias) acc[d] = (acc[d] + bm * P.one[16 * ch + d]) % M.m;
-        }
-    }
-    uint32_t v[4] = {0, 0, 0, 0};
-    for (int d = 0; d < 16; d++) v[d / 4] |= acc[d] << (8 * (d % 4));
-    *(uint4*)(P.out.p + ch * P.out.cs + (row * A.M + j) * 16) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 // ---- weighted sums -----------------------------------------------------------------------------
@@ -264,28 +232,10 @@ int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labe
         if (w * p1 * (uint64_t)K + p1 >= (1ull << 31)) return DASH_ESIZE;
     }
     if (n == 0) return DASH_OK;
-    ExpArgs A;
-    memset(&A, 0, sizeof(A));
-    A.mods = c->d_mods; A.w = (const uint8_t*)L->weights; A.bias = L->bias;
-    A.n = n; A.M = M; A.K = K; A.E = E; A.top_k = L->top_k; A.format = L->weight_format;
-    if (L->routing) {
-        const RoutingView R = routing_view(L->routing->data, n, E);
-        A.offsets = R.offsets; A.rows = R.rows;
-    }
-    int64_t lanes = 0;
-    double macs = 0, bytes = (double)E * matrix_bytes(L->weight_format, M, K);
-    for (int i = 0; i < c->k; i++) {
-        const ModInfo& Mi = c->mods[c->prime[i]];
-        A.pr[i] = ExpPrime{(uint32_t)c->prime[i], L->bias ? (garble ? c->d_one0[i] : c->d_one[i]) : nullptr, view_of(in, i), view_of(out, i)};
-        lanes = n * M * Mi.nchunk > lanes ? n * M * Mi.nchunk : lanes;
-        macs += (double)n * M * K * Mi.lam;
-        bytes += ((double)T * K + (double)n * M) * Mi.lam;
-    }
-    if (lanes > kMaxLanes) return DASH_ESIZE;
-    ProfScope ps(c->prof, DASH_PROF_LINEAR, s, macs, bytes);
-    hipLaunchKernelGGL(k_experts, dim3(blocks_of(lanes), c->k), dim3(kThreads), 0, s, A);
-    DASH_HIP(hipGetLastError());
-    return DASH_OK;
+    ExpertsCall call{(const uint8_t*)L->weights, L->bias, nullptr, n, M, K, E, L->top_k, L->weight_format, garble};
+    RoutingView R;
+    if (L->routing) { R = routing_view(c, L->routing->data, n, E); call.routing = &R; }
+    return experts_mfma(c, call, in, out, s);
 }
 
 int combine_layer(dash_ctx* c, const dash_layer* L, const dash_labels* in, dash_labels* out, hipStream_t s) {
@@ -363,15 +313,20 @@ int dash_mx4_quantise(dash_ctx* c, const void* w, int dtype, int64_t row_stride,
 }
 
 size_t dash_route_bytes(const dash_ctx* c, int64_t n, int n_experts) {
-    if (!c || n < 0 || n > 0x7fffffff || n_experts < 1 || n_experts > (1 << 20)) return 0;
-    return routing_view(nullptr, n, n_experts).bytes;
+    if (!c || n < 0 || n > 0x7fffffff || n_experts < 1 || n_experts > kMaxExperts) return 0;
+    const RoutingView v = routing_view(c, nullptr, n, n_experts);
+    for (int s = 0; s < kTileSizes; s++) if (v.max_tiles[s] > 0x7fffffff) return 0;
+    return v.bytes;
 }
 
 int dash_route(dash_ctx* c, const int32_t* experts, int64_t n, int n_experts, void* data, dash_routing* routing, void* stream) {
     if (!c || !data || ((uintptr_t)data & 15) || !routing || n < 0 || n_experts < 1 || (n > 0 && !experts)) return DASH_EINVAL;
     if (!dash_route_bytes(c, n, n_experts)) return DASH_ESIZE;
-    const RoutingView R = routing_view(data, n, n_experts);
-    const RouteArgs A{experts, n, n_experts, R.offsets, R.rows};
+    RouteArgs A;
+    memset(&A, 0, sizeof(A));
+    A.experts = experts; A.n = n; A.E = n_experts; A.k = c->k;
+    for (int i = 0; i < c->k; i++) A.nchunk[i] = (uint8_t)c->mods[c->prime[i]].nchunk;
+    A.to = routing_view(c, data, n, n_experts);
     const dim3 grid((uint32_t)((n_experts + 1 + kWaves - 1) / kWaves));
     hipLaunchKernelGGL(k_route_count, grid, dim3(kThreads), 0, (hipStream_t)stream, A);
     hipLaunchKernelGGL(k_route_scan, dim3(1), dim3(kThreads), 0, (hipStream_t)stream, A);

@@ -79,16 +79,22 @@ def run_experts(ctx, fmt, E, top_k, route, K, M, seed, bias=False, garble=False,
 FORMATS = ["w8", "mx4"]
 
 
+@pytest.fixture(params=["rule", "big", "narrow"])
+def tile(request, monkeypatch):
+    """the tile that the layer's sizes ask for, and each tile forced"""
+    monkeypatch.setenv("DASH_EXPERTS_TILE", request.param)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("K", [1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 129, 200, 257, 400])
-def test_experts_reduction_lengths(fmt, K):
+def test_experts_reduction_lengths(fmt, K, tile):
     ctx = context(workloads.PRIMES[:8])
     run_experts(ctx, fmt, 3, 1, [2, 0, 2, 1, 2], K, 37, K, bias=K % 2 == 0, garble=K % 3 == 0)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("M", [1, 2, 31, 32, 33, 64, 127, 128, 129, 255, 257])
-def test_experts_output_counts(fmt, M):
+def test_experts_output_counts(fmt, M, tile):
     ctx = context(workloads.PRIMES[:12])
     run_experts(ctx, fmt, 2, 1, [1, 0, 1], 70, M, M, bias=M % 2 == 1, garble=M % 3 == 0)
 
@@ -96,7 +102,7 @@ def test_experts_output_counts(fmt, M):
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("route,E", [([0], 1), ([-1], 1), ([4], 7), ([-1, -1, -1], 2), ([0] * 9, 3), ([2] * 65, 3), (list(range(40)), 40),
                                      ([5, -1, 0, 7, 2 ** 31 - 1, -2 ** 31, 5, 3], 8), ([i * i % 11 for i in range(130)], 11)])
-def test_experts_routes(fmt, route, E):
+def test_experts_routes(fmt, route, E, tile):
     """one row, rows of no expert, experts of no rows, one expert for all, an expert a row, numbers out of range"""
     ctx = context(workloads.PRIMES[:8])
     run_experts(ctx, fmt, E, 1, route, 65, 40, len(route) + E, bias=True)
@@ -104,7 +110,7 @@ def test_experts_routes(fmt, route, E):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("top_k", [2, 3, 8])
-def test_experts_several_rows_per_input(fmt, top_k):
+def test_experts_several_rows_per_input(fmt, top_k, tile):
     ctx = context(workloads.PRIMES[:9])
     g = np.random.default_rng(top_k)
     run_experts(ctx, fmt, 5, top_k, g.integers(-1, 5, 7 * top_k).tolist(), 100, 33, top_k, bias=True)
@@ -112,7 +118,7 @@ def test_experts_several_rows_per_input(fmt, top_k):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("n", [1, 2, 3, 7, 16, 17, 100])
-def test_dense_without_routing(fmt, n):
+def test_dense_without_routing(fmt, n, tile):
     """one expert, no routing: a dense layer; single rows and more than a tile of them"""
     ctx = context(workloads.PRIMES[:12])
     run_experts(ctx, fmt, 1, 1, [0] * n, 130, 70, n, bias=n % 2 == 1, garble=n % 3 == 0, routed=False)
@@ -120,7 +126,7 @@ def test_dense_without_routing(fmt, n):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("rows,E,M,K", [(40, 2, 300, 200), (96, 1, 256, 320), (33, 3, 513, 129), (64, 1, 700, 64)])
-def test_experts_many_tiles(fmt, rows, E, M, K):
+def test_experts_many_tiles(fmt, rows, E, M, K, tile):
     """more rows and outputs than a tile of any kernel holds"""
     ctx = context(workloads.PRIMES[:12])
     g = np.random.default_rng(rows)
@@ -129,20 +135,20 @@ def test_experts_many_tiles(fmt, rows, E, M, K):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("k", [1, 2, 5, 7])
-def test_experts_small_bases(fmt, k):
+def test_experts_small_bases(fmt, k, tile):
     ctx = context(workloads.PRIMES[:k])
     run_experts(ctx, fmt, 2, 1, [0, 1, 1], 90, 50, 70 + k, bias=True)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_experts_floor_rule_and_given_lengths(fmt):
+def test_experts_floor_rule_and_given_lengths(fmt, tile):
     from paper_2302_06361_amd import LAMBDA_FLOOR
     run_experts(context(workloads.PRIMES[:12], rule=LAMBDA_FLOOR), fmt, 2, 1, [0, 1, 1], 90, 50, 80, bias=True)
     run_experts(context(workloads.PRIMES[:5], lam=[1, 128, 16, 17, 33]), fmt, 2, 1, [0, 1, 1] * 7, 90, 50, 81, bias=True)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_experts_large_primes_and_extreme_values(fmt):
+def test_experts_large_primes_and_extreme_values(fmt, tile):
     """primes up to 127; weights of -128 on labels of p - 1; reductions whose sums pass 2^24"""
     ctx = context(P127)
     run_experts(ctx, fmt, 2, 1, [0, 1, -1, 1], 700, 33, 90, bias=True)
@@ -150,14 +156,14 @@ def test_experts_large_primes_and_extreme_values(fmt):
     run_experts(context(workloads.PRIMES[:12]), fmt, 1, 1, [0] * 3, 13000, 5, 92, routed=False, top=True)
 
 
-def test_mx4_shifts_over_their_whole_range():
+def test_mx4_shifts_over_their_whole_range(tile):
     ctx = context(workloads.PRIMES[:12])
     run_experts(ctx, "mx4", 2, 1, [0, 1, 1, 0], 512, 64, 93, max_shift=236)
     run_experts(context(P127), "mx4", 2, 1, [0, 1, 1, 0], 300, 64, 94, max_shift=236)
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_experts_slices_of_longer_bundles(fmt):
+def test_experts_slices_of_longer_bundles(fmt, tile):
     """bundles whose chunks lie further apart than their elements: nothing around the output is touched"""
     ctx = context(workloads.PRIMES[:8])
     run_experts(ctx, fmt, 3, 1, [2, 0, 2, 1, 2], 100, 37, 95, pad=(5, 3))
@@ -165,14 +171,14 @@ def test_experts_slices_of_longer_bundles(fmt):
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_experts_offsets_past_32_bits(fmt):
+def test_experts_offsets_past_32_bits(fmt, tile):
     """chunks 640 MB apart: the last chunk of the two-digit residue starts past 4 GB"""
     ctx = context([2, 3])
     run_experts(ctx, fmt, 2, 1, [1, 0, -1], 70, 40, 97, pad=(40_000_000, 0))
 
 
 @pytest.mark.parametrize("fmt", FORMATS)
-def test_experts_on_another_stream(fmt):
+def test_experts_on_another_stream(fmt, tile):
     ctx = context(workloads.PRIMES[:8])
     s = torch.cuda.Stream()
     s.wait_stream(torch.cuda.current_stream())
