@@ -10,7 +10,6 @@
 //   k_mx4_quantise                : weights to 4-bit floats with a power of two for every 32, into the tiles of the products
 //   (the products: dash_experts_gemm.hip)
 //   k_combine                     : the weighted sums
-#include <hip/hip_bf16.h>
 #include <string.h>
 
 #include "dash_experts.h"
@@ -126,50 +125,138 @@ struct QuantArgs {
     uint8_t* out;
     void* values;
 };
-template <class T> __device__ __forceinline__ float to_float(T v) { return (float)v; }
-template <> __device__ __forceinline__ float to_float(__hip_bfloat16 v) { return __bfloat162float(v); }
-template <class T> __device__ __forceinline__ T from_float(float v) { return (T)v; }
-template <> __device__ __forceinline__ __hip_bfloat16 from_float(float v) { return __float2bfloat16(v); }
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef uint16_t v8s __attribute__((ext_vector_type(8)));
+// V elements of a lane (16 bytes, at any address) as floats, and back
+struct QuantF32 {
+    static constexpr int V = 4;
+    typedef float T;
+    typedef v4f Vec;
+    typedef v4f VecAny __attribute__((aligned(4)));
+    static __device__ __forceinline__ float to(float v) { return v; }
+    static __device__ __forceinline__ float from(float v) { return v; }
+};
+struct QuantBF16 {
+    static constexpr int V = 8;
+    typedef uint16_t T;
+    typedef v8s Vec;
+    typedef v8s VecAny __attribute__((aligned(2)));
+    static __device__ __forceinline__ float to(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
+    static __device__ __forceinline__ uint16_t from(float v) { return (uint16_t)(__float_as_uint(v) >> 16); }       // two significant bits: exact
+};
+struct QuantF16 {
+    static constexpr int V = 8;
+    typedef uint16_t T;
+    typedef v8s Vec;
+    typedef v8s VecAny __attribute__((aligned(2)));
+    static __device__ __forceinline__ float to(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
+    static __device__ __forceinline__ uint16_t from(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+};
+// nibbles 0..3 of n to the low halves of the four bytes
+__device__ __forceinline__ uint32_t spread4(uint32_t n) {
+    n = (n | n << 8) & 0x00ff00ffu;
+    return (n | n << 4) & 0x0f0f0f0fu;
+}
 
-// a lane per block of 32 weights
-template <class T>
+// A wave per tile of 32 rows x 64 columns: a lane reads 16 bytes of a row (V weights), the 32 / V lanes of a block find its largest
+// magnitude among themselves, v_cvt_scalef32_pk_fp4_f32 rounds two weights at a time (nearest, ties to even, saturating).  Codes and
+// shifts go through LDS, so that a tile is written 16 bytes a lane.  Bound by HBM.
+template <class Q>
 __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
-    const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x, tile = idx / 64;
+    constexpr int V = Q::V, kLanes = 32 / V, kRowLanes = 64 / V, kRows = 64 / kRowLanes, kSteps = 32 / kRows;      // lanes of a block, of a row; rows at a time
+    typedef typename Q::T T;
+    __shared__ __attribute__((aligned(16))) uint8_t s_tile[kWaves][kMx4Tile];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t tile = blockIdx.x * kWaves + wave;
     if (tile >= A.tiles) return;
-    const int r = (int)(idx % 64) / 2, b = (int)(idx % 2);
-    const int64_t kt = col_tiles(A.K), mt = row_tiles(A.M), e = tile / (mt * kt), at = tile - e * mt * kt;
-    const int64_t row = at / kt * kTileRows + r, col = at % kt * kTileCols + 32 * b;
-    float v[32];
-    uint32_t amax = 0;
-    for (int i = 0; i < 32; i++) {
-        float x = 0;
-        if (row < A.M && col + i < A.K) x = to_float<T>(((const T*)A.w)[e * A.expert_stride + row * A.row_stride + col + i]);
-        x = x != x ? 0.0f : __builtin_fminf(__builtin_fmaxf(x, -3.402823466e38f), 3.402823466e38f);
-        v[i] = x;
-        const uint32_t a = __float_as_uint(x) & 0x7fffffffu;
-        amax = a > amax ? a : amax;
-    }
-    // floor(log2) of a normal number is its exponent; smaller numbers are below every base
-    int E = (int)(amax >> 23) - 127 - 2;
-    E = E > A.base + A.max_shift ? A.base + A.max_shift : E;
-    E = E < A.base ? A.base : E;
-    const float inv = __uint_as_float((uint32_t)(127 - E) << 23);                                     // E in [-126, 125]
-    const float two = __uint_as_float((uint32_t)(127 + E) << 23);
-    uint32_t code[4] = {0, 0, 0, 0};
-    for (int i = 0; i < 32; i++) {
-        const float a = __builtin_fabsf(v[i]) * inv;
-        // number of the e2m1 magnitude nearest to a, ties to the even one
-        const uint32_t m = (a > 0.25f) + (a >= 0.75f) + (a > 1.25f) + (a >= 1.75f) + (a > 2.5f) + (a >= 3.5f) + (a > 5.0f);
-        const uint32_t c = m ? m | (v[i] < 0 ? 8u : 0u) : 0u;
-        code[(i & 15) / 4] |= c << (8 * (i & 3) + (i >= 16 ? 4 : 0));
-        if (A.values && row < A.M && col + i < A.K) {
-            const float mag = m < 4 ? 0.5f * (float)m : m == 7 ? 6.0f : (float)(m - 2);
-            ((T*)A.values)[(e * A.M + row) * A.K + col + i] = from_float<T>((v[i] < 0 ? -mag : mag) * two);
+    const uint32_t kt = (uint32_t)col_tiles(A.K), mt = (uint32_t)row_tiles(A.M);
+    const uint32_t rt = tile / kt, e = rt / mt;
+    const int row0 = (int)(rt - e * mt) * kTileRows + lane / kRowLanes, col = (int)(tile - rt * kt) * kTileCols + lane % kRowLanes * V;
+    const T* const src = (const T*)A.w + (int64_t)e * A.expert_stride;
+    const int have = A.K - col;                      // columns from the lane's first to the end
+    // all loads go out before the first is waited for: no branch but the one on the tile; rows and columns past the end read the last
+    typename Q::Vec in[kSteps];
+    if ((int)(tile - rt * kt) * kTileCols + kTileCols <= A.K) {
+#pragma unroll
+        for (int s = 0; s < kSteps; s++) {
+            const int row = row0 + kRows * s < A.M ? row0 + kRows * s : A.M - 1;
+            in[s] = *(const typename Q::VecAny*)(src + (int64_t)row * A.row_stride + col);
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < kSteps; s++) {
+            const int row = row0 + kRows * s < A.M ? row0 + kRows * s : A.M - 1;
+#pragma unroll
+            for (int i = 0; i < V; i++) in[s][i] = src[(int64_t)row * A.row_stride + (i < have ? col + i : A.K - 1)];
         }
     }
-    uint8_t* dst = A.out + tile * kMx4Tile;
-    *(uint4*)(dst + 32 * r + 16 * b) = make_uint4(code[0], code[1], code[2], code[3]);
-    dst[kMx4Codes + 2 * r + b] = (uint8_t)(E - A.base);
+    uint8_t* const to = s_tile[wave];
+    T* const values = A.values ? (T*)A.values + ((int64_t)e * A.M + row0) * A.K + col : nullptr;
+#pragma unroll
+    for (int s = 0; s < kSteps; s++) {
+        float x[V];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int i = 0; i < V; i++) {
+            x[i] = Q::to(in[s][i]);
+            x[i] = x[i] == x[i] && i < have && row0 + kRows * s < A.M ? x[i] : 0.0f;
+            const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
+            amax = a > amax ? a : amax;
+        }
+#pragma unroll
+        for (int d = kLanes / 2; d; d /= 2) {
+            const uint32_t o = d == 4 ? (uint32_t)__builtin_amdgcn_ds_swizzle((int)amax, (4 << 10) | 0x1f)                              // lane ^ 4
+                             : d == 2 ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0x4E, 0xf, 0xf, true)                       // quad_perm:[2,3,0,1]
+                                      : (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0xB1, 0xf, 0xf, true);                      // quad_perm:[1,0,3,2]
+            amax = o > amax ? o : amax;
+        }
+        // floor(log2) of a normal number is its exponent; smaller numbers are below every base, an infinity counts as the largest number
+        int E = (int)(amax >> 23) - 127 - 2;
+        E = E > 125 ? 125 : E;
+        E = E > A.base + A.max_shift ? A.base + A.max_shift : E;
+        E = E < A.base ? A.base : E;
+        const float two = __uint_as_float((uint32_t)(127 + E) << 23);                                                 // E in [-126, 125]
+        uint32_t n = 0;
+        n = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(n, x[0], x[1], two, 0);
+        n = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(n, x[2], x[3], two, 1);
+        if constexpr (V == 8) {
+            n = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(n, x[4], x[5], two, 2);
+            n = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(n, x[6], x[7], two, 3);
+        }
+        n &= 0x77777777u | ((n | n >> 1 | n >> 2) & 0x11111111u) << 3;                                                // no sign of a zero
+        const int r = lane / kRowLanes + kRows * s, b = lane % kRowLanes / kLanes, at = lane % kLanes;
+        // the first half of a block's lanes takes the codes of the second into its high halves
+        if constexpr (V == 4) {
+            const uint32_t c = spread4(n), o = (uint32_t)__builtin_amdgcn_ds_swizzle((int)c, (4 << 10) | 0x1f);
+            if (at < 4) *(uint32_t*)(to + 32 * r + 16 * b + 4 * at) = c | o << 4;
+        } else {
+            const uint32_t c0 = spread4(n & 0xffffu), c1 = spread4(n >> 16);
+            const uint32_t o0 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)c0, 0x4E, 0xf, 0xf, true), o1 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)c1, 0x4E, 0xf, 0xf, true);
+            if (at < 2) *(uint2*)(to + 32 * r + 16 * b + 8 * at) = make_uint2(c0 | o0 << 4, c1 | o1 << 4);
+        }
+        if (at == 0) to[kMx4Codes + 2 * r + b] = (uint8_t)(E - A.base);
+        if (values && row0 + kRows * s < A.M) {
+            typename Q::Vec out;
+            const v2f v0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, two, 0), v1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, two, 1);
+            out[0] = Q::from(v0[0]); out[1] = Q::from(v0[1]); out[2] = Q::from(v1[0]); out[3] = Q::from(v1[1]);
+            if constexpr (V == 8) {
+                const v2f v2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, two, 2), v3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(n, two, 3);
+                out[4] = Q::from(v2[0]); out[5] = Q::from(v2[1]); out[6] = Q::from(v3[0]); out[7] = Q::from(v3[1]);
+            }
+            T* const p = values + (int64_t)(kRows * s) * A.K;
+            if (have >= V) *(typename Q::VecAny*)p = out;
+            else
+#pragma unroll
+                for (int i = 0; i < V - 1; i++) if (i < have) p[i] = out[i];
+        }
+    }
+    // (the wave's own LDS: its writes are done before its reads)
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    uint8_t* const dst = A.out + (int64_t)tile * kMx4Tile;
+    *(uint4*)(dst + 16 * lane) = *(const uint4*)(to + 16 * lane);
+    if (lane < 4) *(uint4*)(dst + kMx4Codes + 16 * lane) = *(const uint4*)(to + kMx4Codes + 16 * lane);
 }
 
 __device__ __forceinline__ uint32_t signed_mod(int32_t v, const ModInfo& M) {
@@ -304,9 +391,9 @@ int dash_mx4_quantise(dash_ctx* c, const void* w, int dtype, int64_t row_stride,
     const int64_t tiles = weight_tiles(w, row_stride, expert_stride, n_experts, out_c, K, prepared);
     if (!tiles) return DASH_EINVAL;
     const int64_t lanes = tiles * 64;
-    if (lanes > kMaxLanes) return DASH_ESIZE;
+    if (lanes > kMaxLanes || tiles > 0x7fffffff) return DASH_ESIZE;
     const QuantArgs A{w, row_stride, expert_stride, tiles, out_c, K, base, max_shift, (uint8_t*)prepared, values};
-    auto kernel = dtype == DASH_F32 ? k_mx4_quantise<float> : dtype == DASH_BF16 ? k_mx4_quantise<__hip_bfloat16> : k_mx4_quantise<_Float16>;
+    auto kernel = dtype == DASH_F32 ? k_mx4_quantise<QuantF32> : dtype == DASH_BF16 ? k_mx4_quantise<QuantBF16> : k_mx4_quantise<QuantF16>;
     hipLaunchKernelGGL(kernel, dim3(blocks_of(lanes)), dim3(kThreads), 0, (hipStream_t)stream, A);
     DASH_HIP(hipGetLastError());
     return DASH_OK;
