@@ -19,31 +19,31 @@ __host__ __device__ inline int w8_piece(int row, int q) { return q ^ ((row >> 1)
 __host__ __device__ inline int w8_at(int row, int col) { return 64 * row + 16 * w8_piece(row, col >> 4) + (col & 15); }
 
 // ---- routing: rows sorted by expert, and the tiles of the products ----
-// A group is 16 digits (a chunk) of one row; the groups of an expert's rows for one prime are numbered chunk by chunk.  A tile is up to
-// kTileGroups[s] consecutive groups of one expert and prime; tiles are sorted by expert, prime, first group.
-constexpr int kTileSizes = 2;
-constexpr int kTileGroups[kTileSizes] = {16, 8};
+// A group is 16 digits (a chunk) of one row.  The groups of an expert are numbered prime by prime, chunk by chunk, row by row.  A tile is up to
+// `groups` consecutive ones of one expert (byte weights: the operand is the same for every prime) or of one expert and prime (4-bit weights);
+// tiles are sorted by expert and first group.
+struct TileKind { int groups; bool one_prime; };
+constexpr int kTileKinds = 4;
+constexpr TileKind kTileKind[kTileKinds] = {{16, false}, {8, false}, {16, true}, {8, true}};
 struct RouteTile {          // (read as a uint4)
-    uint32_t expert_prime;  // expert (n_experts: none) | index of the prime << 24
+    uint32_t expert_prime;  // expert (n_experts: none) | index of the prime << 24 (one_prime; else 0)
     int32_t start, count;   // the expert's rows: rows[start .. start + count - 1]
     int32_t first;          // first group
 };
 constexpr int kMaxExperts = (1 << 24) - 2;
-// offsets int32[E + 2] (expert E: rows of no expert), rows int32[n]; per tile size: first tile of every expert int32[E + 2], tiles
+// offsets int32[E + 2] (expert E: rows of no expert), rows int32[n]; per tile kind: first tile of every expert int32[E + 2], tiles
 struct RoutingView {
     int32_t* offsets;
     int32_t* rows;
-    int32_t* first_tile[kTileSizes];
-    RouteTile* tiles[kTileSizes];
-    int64_t max_tiles[kTileSizes];
+    int32_t* first_tile[kTileKinds];
+    RouteTile* tiles[kTileKinds];
+    int64_t max_tiles[kTileKinds];
     size_t bytes;
 };
-// tiles that n rows can make: every expert of a row leaves at most one of them partly filled for a prime
-inline int64_t max_tiles(const dash_ctx* c, int64_t n, int E, int groups) {
-    int64_t t = 0;
-    const int64_t busy = n < E + 1 ? n : E + 1;
-    for (int i = 0; i < c->k; i++) t += (int64_t)c->mods[c->prime[i]].nchunk * n / groups + busy;
-    return t;
+inline int64_t total_chunks(const dash_ctx* c) {
+    int64_t n = 0;
+    for (int i = 0; i < c->k; i++) n += c->mods[c->prime[i]].nchunk;
+    return n;
 }
 inline RoutingView routing_view(const dash_ctx* c, void* data, int64_t n, int E) {
     RoutingView v;
@@ -51,8 +51,10 @@ inline RoutingView routing_view(const dash_ctx* c, void* data, int64_t n, int E)
     auto take = [&](size_t bytes) { uint8_t* p = (uint8_t*)data + at; at += (bytes + 63) / 64 * 64; return p; };
     v.offsets = (int32_t*)take(sizeof(int32_t) * (size_t)(E + 2));
     v.rows = (int32_t*)take(sizeof(int32_t) * (size_t)n);
-    for (int s = 0; s < kTileSizes; s++) {
-        v.max_tiles[s] = max_tiles(c, n, E, kTileGroups[s]);
+    // an expert with rows leaves at most one tile (one_prime: one a prime) partly filled
+    const int64_t busy = n < (int64_t)E + 1 ? n : (int64_t)E + 1, chunks = total_chunks(c);
+    for (int s = 0; s < kTileKinds; s++) {
+        v.max_tiles[s] = chunks * n / kTileKind[s].groups + busy * (kTileKind[s].one_prime ? c->k : 1);
         v.first_tile[s] = (int32_t*)take(sizeof(int32_t) * (size_t)(E + 2));
         v.tiles[s] = (RouteTile*)take(sizeof(RouteTile) * (size_t)v.max_tiles[s]);
     }

@@ -23,7 +23,7 @@ struct RouteArgs {
     const int32_t* experts;
     int64_t n;
     int E, k;
-    uint8_t nchunk[DASH_MAX_PRIMES];
+    int chunk_first[DASH_MAX_PRIMES + 1];       // first chunk of every prime in the numbering of all
     RoutingView to;
 };
 __device__ __forceinline__ bool route_match(int32_t id, int e, int E) { return e < E ? id == e : (uint32_t)id >= (uint32_t)E; }
@@ -39,38 +39,43 @@ __global__ __launch_bounds__(kThreads) void k_route_count(const RouteArgs A) {
     }
     if (lane == 0) A.to.offsets[e + 1] = count;
 }
-__device__ __forceinline__ int32_t route_tiles(const RouteArgs& A, int32_t rows, int groups) {
+// tiles of kind s that `rows` rows make of the chunks first .. last - 1
+__device__ __forceinline__ int32_t route_tiles(int32_t rows, int first, int last, int s) {
+    return (int32_t)(((int64_t)rows * (last - first) + kTileKind[s].groups - 1) / kTileKind[s].groups);
+}
+__device__ __forceinline__ int32_t route_tiles(const RouteArgs& A, int32_t rows, int s) {
+    if (!kTileKind[s].one_prime) return route_tiles(rows, 0, A.chunk_first[A.k], s);
     int32_t t = 0;
-    for (int i = 0; i < A.k; i++) t += (int32_t)(((int64_t)rows * A.nchunk[i] + groups - 1) / groups);
+    for (int i = 0; i < A.k; i++) t += route_tiles(rows, A.chunk_first[i], A.chunk_first[i + 1], s);
     return t;
 }
 // One block: counts to offsets and to first tiles.
 __global__ __launch_bounds__(kThreads) void k_route_scan(const RouteArgs A) {
-    __shared__ int32_t part[1 + kTileSizes][kThreads];
+    __shared__ int32_t part[1 + kTileKinds][kThreads];
     const int n = A.E + 1, per = (n + kThreads - 1) / kThreads, e0 = threadIdx.x * per, e1 = e0 + per < n ? e0 + per : n;
-    int32_t sum[1 + kTileSizes] = {};
+    int32_t sum[1 + kTileKinds] = {};
     for (int e = e0; e < e1; e++) {
         const int32_t rows = A.to.offsets[e + 1];
         sum[0] += rows;
-        for (int s = 0; s < kTileSizes; s++) sum[1 + s] += route_tiles(A, rows, kTileGroups[s]);
+        for (int s = 0; s < kTileKinds; s++) sum[1 + s] += route_tiles(A, rows, s);
     }
-    for (int s = 0; s < 1 + kTileSizes; s++) part[s][threadIdx.x] = sum[s];
+    for (int s = 0; s < 1 + kTileKinds; s++) part[s][threadIdx.x] = sum[s];
     __syncthreads();
-    if (threadIdx.x < 1 + kTileSizes) {
+    if (threadIdx.x < 1 + kTileKinds) {
         int32_t at = 0;
         for (int i = 0; i < kThreads; i++) { const int32_t v = part[threadIdx.x][i]; part[threadIdx.x][i] = at; at += v; }
     }
     __syncthreads();
     if (threadIdx.x == 0) {
         A.to.offsets[0] = 0;
-        for (int s = 0; s < kTileSizes; s++) A.to.first_tile[s][0] = 0;
+        for (int s = 0; s < kTileKinds; s++) A.to.first_tile[s][0] = 0;
     }
-    for (int s = 0; s < 1 + kTileSizes; s++) sum[s] = part[s][threadIdx.x];
+    for (int s = 0; s < 1 + kTileKinds; s++) sum[s] = part[s][threadIdx.x];
     for (int e = e0; e < e1; e++) {
         const int32_t rows = A.to.offsets[e + 1];
         sum[0] += rows;
         A.to.offsets[e + 1] = sum[0];
-        for (int s = 0; s < kTileSizes; s++) { sum[1 + s] += route_tiles(A, rows, kTileGroups[s]); A.to.first_tile[s][e + 1] = sum[1 + s]; }
+        for (int s = 0; s < kTileKinds; s++) { sum[1 + s] += route_tiles(A, rows, s); A.to.first_tile[s][e + 1] = sum[1 + s]; }
     }
 }
 // The wave of an expert writes its rows in ascending order, and its tiles.
@@ -85,11 +90,14 @@ __global__ __launch_bounds__(kThreads) void k_route_fill(const RouteArgs A) {
         if (hit) A.to.rows[at + __popcll(m & ((1ull << lane) - 1))] = (int32_t)(r0 + lane);
         at += __popcll(m);
     }
-    for (int s = 0; s < kTileSizes; s++) {
+    for (int s = 0; s < kTileKinds; s++) {
         int32_t t0 = A.to.first_tile[s][e];
-        for (int i = 0; i < A.k; i++) {
-            const int32_t tiles = (int32_t)(((int64_t)count * A.nchunk[i] + kTileGroups[s] - 1) / kTileGroups[s]);
-            for (int32_t t = lane; t < tiles; t += 64) A.to.tiles[s][t0 + t] = RouteTile{(uint32_t)e | (uint32_t)i << 24, start, count, t * kTileGroups[s]};
+        const bool one = kTileKind[s].one_prime;
+        for (int i = 0; i < (one ? A.k : 1); i++) {
+            const int c0 = one ? A.chunk_first[i] : 0, c1 = one ? A.chunk_first[i + 1] : A.chunk_first[A.k];
+            const int32_t tiles = route_tiles(count, c0, c1, s);
+            for (int32_t t = lane; t < tiles; t += 64)
+                A.to.tiles[s][t0 + t] = RouteTile{(uint32_t)e | (uint32_t)i << 24, start, count, c0 * count + t * kTileKind[s].groups};
             t0 += tiles;
         }
     }
@@ -400,9 +408,10 @@ int dash_mx4_quantise(dash_ctx* c, const void* w, int dtype, int64_t row_stride,
 }
 
 size_t dash_route_bytes(const dash_ctx* c, int64_t n, int n_experts) {
-    if (!c || n < 0 || n > 0x7fffffff || n_experts < 1 || n_experts > kMaxExperts) return 0;
+    // (groups and tiles are numbered in 32 bits)
+    if (!c || n < 0 || n_experts < 1 || n_experts > kMaxExperts || n > 0x7fffffff / (total_chunks(c) + 64)) return 0;
     const RoutingView v = routing_view(c, nullptr, n, n_experts);
-    for (int s = 0; s < kTileSizes; s++) if (v.max_tiles[s] > 0x7fffffff) return 0;
+    for (int s = 0; s < kTileKinds; s++) if (v.max_tiles[s] > 0x7fffffff) return 0;
     return v.bytes;
 }
 
@@ -412,7 +421,7 @@ int dash_route(dash_ctx* c, const int32_t* experts, int64_t n, int n_experts, vo
     RouteArgs A;
     memset(&A, 0, sizeof(A));
     A.experts = experts; A.n = n; A.E = n_experts; A.k = c->k;
-    for (int i = 0; i < c->k; i++) A.nchunk[i] = (uint8_t)c->mods[c->prime[i]].nchunk;
+    for (int i = 0; i < c->k; i++) A.chunk_first[i + 1] = A.chunk_first[i] + (int)c->mods[c->prime[i]].nchunk;
     A.to = routing_view(c, data, n, n_experts);
     const dim3 grid((uint32_t)((n_experts + 1 + kWaves - 1) / kWaves));
     hipLaunchKernelGGL(k_route_count, grid, dim3(kThreads), 0, (hipStream_t)stream, A);
