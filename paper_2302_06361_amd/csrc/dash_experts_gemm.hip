@@ -282,11 +282,11 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     };
     // Stage t in two halves of 32 inputs; the operands of its first half are in registers when it starts:
     //   products of the first half  | reads of the second half's operands; the second part of the loads of stage t - 1 + S; 4-bit: the
-    //                                 expansion of stage t + 1
+    //                                 second half of the expansion of stage t + 1
     //   wait for the loads of stage t + 1 (4-bit: t + 2), barrier
     //   products of the second half | the first part of the loads of stage t + S into the slot that stage t has left; reads of the first half
     //                                 of stage t + 1;
-    //                                 4-bit: codes and table entries of stage t + 2
+    //                                 4-bit: codes and table entries of stage t + 2, the first half of its expansion
     // The barrier stands behind all reads of stage t (each wave waits for its own), behind the expansion of stage t + 1, and behind
     // the arrival of stage t + 1.
     // The order inside a half is fixed: behind each product two reads (done well before the half ends), the loads far apart (a load that
@@ -299,19 +299,22 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     auto loop = [&](auto dn) __attribute__((always_inline)) {
         constexpr int kProducts = dn * FB, kReads = FB + 2 * dn;
         Operands o0, o1;
-        auto half = [&](const Operands& now, Operands& next, bool there, int t_read, int half_read, int t_load, auto part, int t_expand, int t_fetch) __attribute__((always_inline)) {
+        auto half = [&](const Operands& now, Operands& next, bool there, int t_read, int half_read, int t_load, auto part, int t_expand) __attribute__((always_inline)) {
             constexpr int kSlots = kProducts > 4 ? kProducts : 4, kLoads = part ? kParts - kPart0 : kPart0;
 #pragma unroll
             for (int m = 0; m < kSlots; m++) {
                 if (m < kProducts && there) multiply(now, m);
 #pragma unroll
                 for (int i = 0; i < kReads; i++) if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) read(next, t_read, half_read, i);
+                // (4-bit: the first half of an expansion follows its table entry, the second half has a half of products to itself)
                 if constexpr (!part) {
-                    if (m == 0) fetch_codes(t_fetch);
-                    if (m == kSlots / 2) fetch_table();
+                    if (m == 0) fetch_codes(t_expand);
+                    if (m == kSlots / 4) fetch_table();
+#pragma unroll
+                    for (int i = 0; i < kSteps / 2; i++) if (kSlots / 2 + i * kSlots / kSteps == m) expand(t_expand, i);
                 } else {
 #pragma unroll
-                    for (int i = 0; i < kSteps; i++) if (i * kSlots / kSteps == m) expand(t_expand, i);
+                    for (int i = 0; i < kSteps / 2; i++) if (i * 2 * kSlots / kSteps == m) expand(t_expand, kSteps / 2 + i);
                 }
 #pragma unroll
                 for (int i = 0; i < kLoads; i++) if ((2 * i + 1) * kSlots / (2 * kLoads) == m) load_piece(t_load, (part ? kPart0 : 0) + i);
@@ -322,12 +325,14 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         for (int i = 0; i < kReads; i++) read(o0, 0, 0, i);
         fetch_codes(1);
         fetch_table();
+#pragma unroll
+        for (int i = 0; i < kSteps / 2; i++) expand(1, i);
         for (int t = 0; t < stages; t++) {
             const bool there = WK == 1 || WK * t + ws < nk;         // (the last round may be short of a stage for some sets)
-            half(o0, o1, there, t, 1, t - 1 + S, k1, t + 1, 0);
+            half(o0, o1, there, t, 1, t - 1 + S, k1, t + 1);
             arrived(k_ahead);
             lds_barrier();
-            half(o1, o0, there, t + 1, 0, t + S, k0, 0, t + 2);
+            half(o1, o0, there, t + 1, 0, t + S, k0, t + 2);
         }
     };
 #pragma unroll
