@@ -72,6 +72,18 @@ def lib():
     return _lib
 
 
+def _describe(tensors, address, n_elem):
+    """The dash_labels of a list of tensors, through the host module built beside the library."""
+    global _describe
+    import torch  # noqa: F401  (the module uses its libraries)
+    try:
+        from ._bundle import describe
+    except ImportError as e:
+        raise DashError("the binding's host module is missing: build it with `python -m paper_2302_06361_amd.build` (%s)" % e)
+    _describe = describe
+    describe(tensors, address, n_elem)
+
+
 def _check(st, what):
     if st != 0:
         raise DashError("%s: %s (%d)" % (what, lib().dash_strerror(st).decode(), st))
@@ -79,7 +91,7 @@ def _check(st, what):
 
 def _stream():
     import torch
-    return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
 
 
 class Labels:
@@ -98,11 +110,7 @@ class Labels:
 
     def c(self):
         s = CLabels()
-        s.n_elem = self.n_elem
-        for i, t in enumerate(self.tensors):
-            if t is not None:
-                s.data[i] = t.data_ptr()
-                s.chunk_stride[i] = t.stride(0)
+        _describe(self.tensors, C.addressof(s), self.n_elem)
         return s
 
     def slice(self, e0, e1):

@@ -2,6 +2,7 @@
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -20,6 +21,23 @@ HEADERS = ["dash_chain_rule.h", "dash_core.h", "dash_experts.h", "dash_launch.h"
 FLAGS = ["-O3", "--offload-arch=gfx950", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function", "-Wno-pass-failed",
          # packed FP32 instructions are kept out of every code object of this library
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
+
+
+BUNDLE_SRC = os.path.join(CSRC, "bundle_module.cpp")
+
+
+def bundle_so():
+    return os.path.join(HERE, "_bundle" + sysconfig.get_config_var("EXT_SUFFIX"))
+
+
+def build_bundle():
+    """Compile the binding's host module against the installed torch (its headers only say where a tensor's address is)."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    include = os.path.join(root, "include")
+    subprocess.check_call(["g++", "-O2", "-fPIC", "-shared", "-std=c++17", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+                           "-isystem", include, "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
+                           BUNDLE_SRC, "-o", bundle_so(), "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 def build(force=True, verbose=False):
@@ -52,6 +70,8 @@ def build(force=True, verbose=False):
     if failed:
         raise RuntimeError("hipcc failed")
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", SO] + objs)
+    if force or not os.path.exists(bundle_so()) or os.path.getmtime(bundle_so()) < max(os.path.getmtime(BUNDLE_SRC), hdr_time):
+        build_bundle()
     return SO
 
 
