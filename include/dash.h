@@ -167,8 +167,7 @@ int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void
  * Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] one after the other, 16-byte aligned, independent of the
  * primes.  A matrix is cut into tiles of 32 rows x 64 columns, row tiles outermost, zeros past out_c and K.
  *   DASH_W8   2048 bytes a tile: weight (r, c) at 64 r + 16 ((c / 16) ^ f(r)) + c % 16, f(r) = (r / 2) % 4 ^ (r / 8) % 2
- *   DASH_MX4  1088 bytes a tile: the codes of (r, c) in byte 32 r + 16 (c / 32) + c % 16, low four bits where (c / 16) % 2 = 0, else
- *             high; then the shifts, of (r, c) in byte 1024 + 2 r + c / 32.  A code is an e2m1 float: bit 3 the sign, bits 0..2
+ *   DASH_MX4  1088 bytes a tile: the codes of (r, c) in byte 32 r + c % 32, low four bits where c < 32, else high; then the shifts, of (r, c) in byte 1024 + 2 r + c / 32.  A code is an e2m1 float: bit 3 the sign, bits 0..2
  *             the magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6; the weight that enters the layer is the integer 2 * e2m1 * 2^shift. */
 size_t dash_expert_weights_bytes(int format, int n_experts, int out_c, int K);
 /* DASH_W8.  w: device int8, element (e, j, i) at w[e * expert_stride + j * row_stride + i] (row_stride >= K, expert_stride

@@ -234,14 +234,14 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
         }
         n &= 0x77777777u | ((n | n >> 1 | n >> 2) & 0x11111111u) << 3;                                                // no sign of a zero
         const int r = lane / kRowLanes + kRows * s, b = lane % kRowLanes / kLanes, at = lane % kLanes;
-        // the first half of a block's lanes takes the codes of the second into its high halves
+        // the lanes of a row's first block take the codes of its second into the high halves
         if constexpr (V == 4) {
-            const uint32_t c = spread4(n), o = (uint32_t)__builtin_amdgcn_ds_swizzle((int)c, (4 << 10) | 0x1f);
-            if (at < 4) *(uint32_t*)(to + 32 * r + 16 * b + 4 * at) = c | o << 4;
+            const uint32_t c = spread4(n), o = (uint32_t)__builtin_amdgcn_ds_swizzle((int)c, (8 << 10) | 0x1f);             // lane ^ 8
+            if (b == 0) *(uint32_t*)(to + 32 * r + 4 * at) = c | o << 4;
         } else {
             const uint32_t c0 = spread4(n & 0xffffu), c1 = spread4(n >> 16);
-            const uint32_t o0 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)c0, 0x4E, 0xf, 0xf, true), o1 = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)c1, 0x4E, 0xf, 0xf, true);
-            if (at < 2) *(uint2*)(to + 32 * r + 16 * b + 8 * at) = make_uint2(c0 | o0 << 4, c1 | o1 << 4);
+            const uint32_t o0 = (uint32_t)__builtin_amdgcn_ds_swizzle((int)c0, (4 << 10) | 0x1f), o1 = (uint32_t)__builtin_amdgcn_ds_swizzle((int)c1, (4 << 10) | 0x1f);
+            if (b == 0) *(uint2*)(to + 32 * r + 8 * at) = make_uint2(c0 | o0 << 4, c1 | o1 << 4);
         }
         if (at == 0) to[kMx4Codes + 2 * r + b] = (uint8_t)(E - A.base);
         if (values && row0 + kRows * s < A.M) {

@@ -47,6 +47,8 @@ struct ETile {
 typedef ETile<1, 2, 4, 4, 2, 4, 2, 0> EBig;          // 256 digits x 256 features
 typedef ETile<1, 2, 2, 2, 2, 4, 2, 1> ENarrow;       // 128 digits x 128 features
 typedef ETile<2, 2, 2, 2, 2, 4, 2, 1> EDeep;         // the same by two sets of waves
+typedef ETile<1, 1, 4, 4, 1, 4, 2, 1> ENarrow4;      // the narrow tile for 4-bit weights
+typedef ETile<2, 1, 4, 4, 1, 4, 2, 1> EDeep4;
 
 struct ExpPrime {
     uint32_t p;
@@ -54,6 +56,7 @@ struct ExpPrime {
     uint32_t pow12;             // 4096 mod p
     uint32_t start;             // multiple of p that the sums start at
     uint32_t two_step;          // sums are too large for one multiplication by mmagic
+    int32_t chunk_first;        // first chunk in the numbering of all
     const uint8_t* one;         // chunked label of the constant-one wire, or NULL
     LView in, out;
 };
@@ -71,27 +74,31 @@ struct ExpArgs {
     ExpPrime pr[DASH_MAX_PRIMES];
 };
 
-// 16 (4) bytes a lane from base + off to LDS at `to` + 16 (4) * lane.  In flight until a wait on vmcnt; nothing in registers.
-__device__ __forceinline__ void load_lds16(uint32_t to, const uint8_t* base, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+// 16 (4) bytes a lane from offset `off` + At of the buffer to LDS at `to` + Slot + At + 16 (4) * lane; a lane whose offset lies past the end of
+// the buffer reads nothing.  In flight until a wait on vmcnt; no registers.
+template <int Slot, int At> __device__ __forceinline__ void load_lds16(uint32_t to, const v4i& buffer, uint32_t off) {
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen offset:%4 lds" ::"s"(to), "v"(off), "s"(buffer), "n"(Slot), "n"(At) : "memory", "m0", "scc");
 }
-__device__ __forceinline__ void load_lds4(uint32_t to, const uint8_t* base, uint32_t off) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
+template <int Slot> __device__ __forceinline__ void load_lds4(uint32_t to, const v4i& buffer, uint32_t off) {
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer), "n"(Slot) : "memory", "m0", "scc");
 }
+// a buffer of `bytes` bytes without a format (raw, stride 0)
+__device__ __forceinline__ v4i buffer_of(const uint8_t* p, uint32_t bytes) {
+    const uint64_t a = (uint64_t)p;
+    return v4i{__builtin_amdgcn_readfirstlane((int)(uint32_t)a), __builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32) & 0xffff),
+               __builtin_amdgcn_readfirstlane((int)bytes), 0x00020000};
+}
+__device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ uint64_t lane_of(uint64_t v, int lane) { return lane_of((uint32_t)v, lane) | (uint64_t)lane_of((uint32_t)(v >> 32), lane) << 32; }
 // the wave's LDS accesses done, then the block's barrier (loads stay in flight)
 __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 // at most N loads of the wave outstanding
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
-__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
-    const uint64_t a = (uint64_t)p;
-    return (const uint8_t*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)a) |
-                            (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(a >> 32)) << 32);
-}
-
 template <int FMT, class TL>
 __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A) {
-    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW, WK = TL::WK, T = TL::T;
+    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW, WK = TL::WK;
     constexpr bool kMx4 = FMT == DASH_MX4;
+    constexpr bool kDirect = kMx4 && TL::WD == 1;       // a wave's weights are its own: expanded in registers
     // ---- block -> tile ----
     // Work-groups go to the 8 XCDs in turn, each with an L2 of its own: an XCD takes a run of consecutive tiles, numbered in bands of `sty`
     // row blocks, row block after row block, then column after column.  The blocks on an XCD at one time then share a band's weights, which
@@ -117,35 +124,79 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     const int wd = wave / TL::WF, wf = wave % TL::WF;
 
     constexpr int kDig = G * 1024, kRaw = kMx4 ? 1280 : 2048;       // bytes of a stage's labels; of a stage's weights per feature tile, as loaded
-    constexpr int kExp = FT * 2048;                                 // 4-bit: bytes of an expanded stage
+    constexpr int kExp = kMx4 && !kDirect ? FT * 2048 : 0;          // 4-bit: bytes of an expanded stage
     // one array: its address goes into the loads, so that the compiler takes all of it to change at their waits and barriers
-    constexpr int kSet = S * kDig + S * FT * kRaw + (kMx4 ? 2 * kExp : 0);      // of a set of waves
+    constexpr int kSet = S * kDig + S * FT * kRaw + 2 * kExp;       // of a set of waves
     __shared__ __attribute__((aligned(1024))) uint8_t smem[WK * kSet];
-    static_assert((WK - 1) * NW * TL::DA * TL::FB * 4096 <= WK * kSet, "the sums of the sets are added up in it");
+    static_assert((WK - 1) * NW * DA * FB * 4096 <= WK * kSet, "the sums of the sets are added up in it");
     uint8_t* const s_dig = smem + ws * kSet;
     uint8_t* const s_raw = s_dig + S * kDig;
     uint8_t* const s_exp = s_raw + S * FT * kRaw;
     __shared__ u32x4 s_lut[kMx4 ? 256 : 1];
-    __shared__ u32x4 s_one[G];
-    __shared__ const uint8_t* s_src[G];
-    __shared__ uint8_t* s_dst[G];
-    __shared__ int s_prime[G];
 
-    // ---- the groups of the tile ----
-    if (tid < G) {
-        const bool valid = first + tid < end;
-        const int g = valid ? first + tid : first;                  // (a group past the end loads the tile's first and stores nothing)
-        const int chunk = g / count, t = g - chunk * count, row = A.rows ? A.rows[start + t] : t;
+    // ---- the groups of the tile: group g of it in lane g of every wave ----
+    const int n_groups = end - first < G ? end - first : G;
+    uint64_t g_src, g_dst, g_one = 0;
+    uint32_t g_prime, g_magic, g_pow12, g_start, g_two_step;
+    {
+        const int g = first + (lane < n_groups ? lane : 0), chunk = g / count, t = g - chunk * count, row = A.rows ? A.rows[start + t] : t;
         int p = 0;
 #pragma unroll
         for (int i = 1; i < DASH_MAX_PRIMES; i++) p += chunk >= A.chunk_first[i] ? 1 : 0;
         const ExpPrime& P = A.pr[p];
-        const int ch = chunk - A.chunk_first[p];
-        s_src[tid] = P.in.p + (int64_t)ch * P.in.cs + (int64_t)(row / A.top_k) * K * 16;
-        s_dst[tid] = valid ? P.out.p + (int64_t)ch * P.out.cs + (int64_t)row * M * 16 : nullptr;
-        s_prime[tid] = p;
-        if (A.bias) s_one[tid] = *(const u32x4*)(P.one + 16 * ch);
+        const int ch = chunk - P.chunk_first;
+        g_src = (uint64_t)(P.in.p + (int64_t)ch * P.in.cs + (int64_t)(row / A.top_k) * K * 16);
+        g_dst = (uint64_t)(P.out.p + (int64_t)ch * P.out.cs + (int64_t)row * M * 16);
+        if (A.bias) g_one = (uint64_t)(P.one + 16 * ch);
+        g_prime = P.p; g_magic = P.mmagic; g_pow12 = P.pow12; g_start = P.start; g_two_step = P.two_step;
     }
+    if (e >= A.E) {         // rows of no expert: the value 0 on both sides
+        for (int g = wave_; g < n_groups; g += NW * WK) {
+            uint8_t* const dst = (uint8_t*)lane_of(g_dst, g);
+            for (int j = by * TL::F + lane; j < M && j < by * TL::F + TL::F; j += 64) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
+        }
+        return;
+    }
+
+    // ---- loads ----
+    const int nk = (K + 63) / 64;
+    constexpr int kTileBytes = kMx4 ? kMx4Tile : kW8Tile;
+    const int row_tiles_ = (M + 31) / 32;
+    const uint8_t* const wexp = A.w + (int64_t)e * A.expert_bytes;
+    v4i lab[GP], wgt[WT];
+#pragma unroll
+    for (int i = 0; i < WT; i++) {                                  // (tiles past the last: empty buffers)
+        const int rt = by * FT + wave * WT + i;
+        wgt[i] = buffer_of(wexp + (int64_t)rt * nk * kTileBytes, rt < row_tiles_ ? (uint32_t)(nk * kTileBytes) : 0u);
+    }
+#pragma unroll
+    for (int i = 0; i < GP; i++) {
+        const int g = wave * GP + i;
+        lab[i] = buffer_of((const uint8_t*)lane_of(g_src, g), g < n_groups ? (uint32_t)K * 16u : 0u);
+    }
+    const uint32_t dig0 = (uint32_t)(uintptr_t)(lds_ptr)s_dig + wave * GP * 1024, raw0 = (uint32_t)(uintptr_t)(lds_ptr)s_raw + wave * WT * kRaw;
+    // A set takes every WK-th stage of 64 inputs: its stage t are the inputs from 64 (WK t + ws), in slot t % S.  Stages past the end load
+    // nothing (their offsets lie past the buffers) but count.  A lane's offsets run along with the stages.
+    // Words 8 .. 15 of every 16 of a group with an odd number stand before words 0 .. 7: the reads of two groups meet different banks.
+    uint32_t off_w = 16u * lane + (uint32_t)(ws * kTileBytes), off_s = 4u * (lane & 15) + kMx4Codes + (uint32_t)(ws * kTileBytes);
+    uint32_t off_l = 16u * lane + 1024u * ws;                       // (group with an odd number: ^ 128)
+    constexpr int kParts = 2 * WT + GP;                             // loads of a stage: weights, then labels
+    auto load_weights = [&](auto slot, int i) __attribute__((always_inline)) {
+        constexpr int kSlot = decltype(slot)::value * FT * kRaw;
+        const uint32_t to = raw0 + i / 2 * kRaw;
+        if (i % 2 == 0) load_lds16<kSlot, 0>(to, wgt[i / 2], off_w);
+        else if constexpr (kMx4) load_lds4<kSlot + kMx4Codes>(to, wgt[i / 2], off_s);
+        else load_lds16<kSlot, 1024>(to, wgt[i / 2], off_w);
+        if (i == 2 * WT - 1) { off_w += WK * kTileBytes; off_s += WK * kTileBytes; }
+    };
+    auto load_labels = [&](auto slot, int i) __attribute__((always_inline)) {
+        constexpr int kSlot = decltype(slot)::value * kDig;
+        load_lds16<kSlot, 0>(dig0 + i * 1024, lab[i], i % 2 ? off_l ^ 128u : off_l);
+        if (i == GP - 1) off_l += WK * 1024;
+    };
+
+    // ---- 4-bit weights ----
+    const int h = lane >> 5, j32 = lane & 31, l16 = lane & 15;
     if (kMx4 && tid < 256) {
         // 2^tid mod p, times the eight magnitudes, and p minus that
         const uint32_t prime = A.pr[pi].p, mmagic = A.pr[pi].mmagic;
@@ -166,263 +217,264 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         }
         s_lut[tid] = u32x4{w[0], w[1], w[2], w[3]};
     }
-    __syncthreads();
-    if (e >= A.E) {         // rows of no expert: the value 0 on both sides
-        for (int i = tid; i < G * TL::F; i += T) {
-            uint8_t* const dst = s_dst[i / TL::F];
-            const int j = by * TL::F + i % TL::F;
-            if (dst && j < M) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
-        }
-        return;
-    }
-
-    // ---- loads ----
-    const int nk = (K + 63) / 64;
-    const uint8_t* src[GP];
-#pragma unroll
-    for (int i = 0; i < GP; i++) src[i] = uniform(s_src[wave * GP + i]);
-    // (a wave whose groups lie past the end loads weights alone; large tiles are rarely short)
-    const bool loads_labels = DA > 2 || __builtin_amdgcn_readfirstlane(first + wave * GP < end);
-    const int row_tiles_ = (M + 31) / 32;
-    constexpr int kTileBytes = kMx4 ? kMx4Tile : kW8Tile;
-    const uint8_t* wsrc[WT];
-#pragma unroll
-    for (int i = 0; i < WT; i++) {
-        const int rt = by * FT + wave * WT + i;                     // (tiles past the end: the last again)
-        wsrc[i] = uniform(A.w + (int64_t)e * A.expert_bytes + (int64_t)(rt < row_tiles_ ? rt : row_tiles_ - 1) * nk * kTileBytes);
-    }
-    const uint32_t dig0 = (uint32_t)(uintptr_t)(lds_ptr)s_dig, raw0 = (uint32_t)(uintptr_t)(lds_ptr)s_raw;
-    // A set takes every WK-th stage of 64 inputs: its stage t are the inputs from 64 (WK t + ws).  Stage t goes into slot t % S; past the end
-    // the last one again, so that every stage counts the same loads.  A stage's loads come in two parts, one for each half of the work on a stage.
-    constexpr int kParts = 2 * WT + GP, kPart0 = (kParts + 1) / 2;
-    // words 8 .. 15 of every 16 of a group with an odd number stand before words 0 .. 7: the reads of two groups meet different banks
-    auto load_piece = [&](int t, int i) __attribute__((always_inline)) {
-        const int slot = t % S, k = WK * t + ws < nk ? WK * t + ws : nk - 1;
-        if (i < 2 * WT) {
-            const uint8_t* const w = wsrc[i / 2] + (int64_t)k * kTileBytes;
-            const uint32_t to = raw0 + (slot * FT + wave * WT + i / 2) * kRaw;
-            if (i % 2 == 0) load_lds16(to, w, 16u * lane);
-            else if constexpr (kMx4) load_lds4(to + 1024, w + kMx4Codes, 4u * (lane & 15));
-            else load_lds16(to + 1024, w + 1024, 16u * lane);
-        } else if (loads_labels) {
-            const int g = i - 2 * WT, last = K - 1 - 64 * k, word = lane ^ (g & 1) * 8;     // words past K: the last again (their weights are zero)
-            load_lds16(dig0 + slot * kDig + (wave * GP + g) * 1024, src[g] + (int64_t)k * 1024, 16u * (uint32_t)(word < last ? word : last));
-        }
-    };
-    auto issue = [&](int t, int part) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = part ? kPart0 : 0; i < (part ? kParts : kPart0); i++) load_piece(t, i);
-    };
-    // at most N stages of the wave's loads outstanding
-    auto arrived = [&](auto n) __attribute__((always_inline)) {
-        constexpr int N = decltype(n)::value;
-        if (loads_labels) wait_loads<N * kParts>(); else wait_loads<N * 2 * WT>();
-    };
-    // 4-bit: the wave's tiles of a stage, a block of 32 weights a lane: codes and shift, table entry (fetch), then bytes, 4 at a time (expand)
-    u32x4 code[WT], lut[WT], bytes[WT];
+    // A lane's 16 bytes of codes are 16 weights of a row's first block of 32 and 16 of its second (low and high halves of the bytes); shifts of
+    // both blocks, table entries of both, then four weights at a time as bytes.
+    // In registers (a wave's weights are its own: kDirect): lane (j32, h) holds what it multiplies, two stages in the making.
+    // Else through LDS: lane (row, half) = (lane / 2, lane % 2).
+    constexpr int kMaking = kDirect ? 2 : 1;
+    u32x4 code[kMaking][WT], lut[2][WT], bytes[WT];
     uint32_t shift[WT];
-    auto fetch_codes = [&](int t) __attribute__((always_inline)) {
+    const uint8_t* const raw_codes = s_raw + wave * WT * kRaw + 16 * (kDirect ? 2 * j32 + h : lane);
+    const uint8_t* const raw_shifts = s_raw + wave * WT * kRaw + kMx4Codes + 2 * (kDirect ? j32 : lane >> 1);
+    auto fetch_codes = [&](auto slot, int b) __attribute__((always_inline)) {
         if constexpr (kMx4) {
 #pragma unroll
             for (int i = 0; i < WT; i++) {
-                const uint8_t* const raw = s_raw + ((t % S) * FT + wave * WT + i) * kRaw;
-                code[i] = *(const u32x4*)(raw + 16 * lane);
-                shift[i] = raw[1024 + lane];
+                code[b][i] = *(const u32x4*)(raw_codes + (decltype(slot)::value * FT + i) * kRaw);
+                shift[i] = *(const uint16_t*)(raw_shifts + (decltype(slot)::value * FT + i) * kRaw);
             }
         }
     };
-    auto fetch_table = [&]() __attribute__((always_inline)) {
+    auto fetch_table = [&](int block) __attribute__((always_inline)) {
         if constexpr (kMx4) {
 #pragma unroll
-            for (int i = 0; i < WT; i++) lut[i] = s_lut[shift[i]];
+            for (int i = 0; i < WT; i++) lut[block][i] = s_lut[block ? shift[i] >> 8 : shift[i] & 255u];
         }
     };
+    uint32_t k3210 = 0x03020100u;
+    asm volatile("" : "+v"(k3210));             // (in a register: one instruction takes one literal)
+    auto four = [&](uint32_t x, const u32x4& l, int block) __attribute__((always_inline)) -> uint32_t {
+        const uint32_t sel = (block ? x >> 4 : x) & 0x07070707u, sign = ((block ? x >> 5 : x >> 1) & 0x04040404u) | k3210;
+        return __builtin_amdgcn_perm(__builtin_amdgcn_perm(l[3], l[2], sel), __builtin_amdgcn_perm(l[1], l[0], sel), sign);
+    };
     constexpr int kSteps = 8 * WT;
-    auto expand = [&](int t, int step) __attribute__((always_inline)) {
-        if constexpr (kMx4) {
-            const int i = step / 8, half = step / 4 % 2, d = step % 4;
-            const uint32_t x = half ? code[i][d] >> 4 : code[i][d], sel = x & 0x07070707u;
-            const uint32_t neg = __builtin_amdgcn_perm(0, 0, ((x >> 3) & 0x01010101u) | 0x0c0c0c0cu);    // selector 12: 0x00, 13: 0xff
-            const uint32_t a = __builtin_amdgcn_perm(lut[i][1], lut[i][0], sel), b = __builtin_amdgcn_perm(lut[i][3], lut[i][2], sel);
-            bytes[i][d] = (a & ~neg) | (b & neg);
-            if (d == 3) *(u32x4*)(s_exp + (t & 1) * kExp + (wave * WT + i) * 2048 + 64 * (lane >> 1) + 16 * w8_piece(lane >> 1, 2 * (lane & 1) + half)) = bytes[i];
+    uint8_t* const exp_to0 = s_exp + wave * WT * 2048 + 64 * (lane >> 1) + 16 * w8_piece(lane >> 1, lane & 1);
+    uint8_t* const exp_to1 = s_exp + wave * WT * 2048 + 64 * (lane >> 1) + 16 * w8_piece(lane >> 1, 2 + (lane & 1));
+    // (steps of the first block of every tile, then of the second)
+    auto expand = [&](int parity, int step) __attribute__((always_inline)) {
+        if constexpr (kMx4 && !kDirect) {
+            const int block = step / (4 * WT), i = step / 4 % WT, d = step % 4;
+            bytes[i][d] = four(code[0][i][d], lut[block][i], block);
+            if (d == 3) *(u32x4*)((block ? exp_to1 : exp_to0) + parity * kExp + i * 2048) = bytes[i];
         }
     };
 
     // ---- products ----
-    v16i acc[DA][FB];
-#pragma unroll
-    for (int d = 0; d < DA; d++) {
-        const int g0 = (wd * DA + d) * 2;
-        const int s0 = kMx4 || ws ? 0 : (int)A.pr[__builtin_amdgcn_readfirstlane(s_prime[g0])].start, s1 = kMx4 || ws ? 0 : (int)A.pr[__builtin_amdgcn_readfirstlane(s_prime[g0 + 1])].start;
-#pragma unroll
-        for (int f = 0; f < FB; f++)
-#pragma unroll
-            for (int r = 0; r < 16; r++) acc[d][f][r] = r < 8 ? s0 : s1;
-    }
-    const int h = lane >> 5, j32 = lane & 31, l16 = lane & 15;
     const int odd = (lane >> 4) & 1;
-    const int da = wd * DA * 2048 + odd * 1024 + h * 256 + (l16 >> 1) * 16 + (l16 & 1) * 8, da0 = da + odd * 128, da1 = da + 128 - odd * 128;
-    const int fb0 = wf * FB * 2048 + 64 * j32 + 16 * w8_piece(j32, h), fb1 = wf * FB * 2048 + 64 * j32 + 16 * w8_piece(j32, 2 + h);
-    // operands of one half (32 inputs) of stage t, in FB + 2 DA reads
+    const uint8_t* const da = s_dig + wd * DA * 2048 + odd * 1024 + h * 256 + (l16 >> 1) * 16 + (l16 & 1) * 8;
+    const uint8_t* const da0 = da + odd * 128;
+    const uint8_t* const da1 = da + 128 - odd * 128;
+    const uint8_t* const fb = (kMx4 ? s_exp : s_raw) + wf * FB * 2048 + 64 * j32;
+    const uint8_t* const fb0 = fb + 16 * w8_piece(j32, h);
+    const uint8_t* const fb1 = fb + 16 * w8_piece(j32, 2 + h);
+    // operands of one half (32 inputs) of a stage, in FB + 2 DA reads
     struct Operands { v4i b[FB]; v2i a[DA][2]; };
-    auto read = [&](Operands& o, int t, int half, int i) __attribute__((always_inline)) {
-        const uint8_t* const wgt = (kMx4 ? s_exp + (t & 1) * kExp : s_raw + (t % S) * FT * kRaw) + (half ? fb1 : fb0);
-        const uint8_t* const dig = s_dig + (t % S) * kDig + half * 512;
-        if (i < FB) o.b[i] = *(const v4i*)(wgt + i * 2048);
-        else {
+    auto read = [&](Operands& o, auto slot, int half, int i) __attribute__((always_inline)) {
+        constexpr int kSlot = decltype(slot)::value;
+        if (i < FB) {
+            if constexpr (!kDirect) o.b[i] = *(const v4i*)((half ? fb1 : fb0) + (kMx4 ? (kSlot & 1) * kExp : kSlot * FT * kRaw) + i * 2048);
+        } else {
             const int d = (i - FB) / 2, second = (i - FB) % 2;
-            o.a[d][second] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)(dig + (second ? da1 : da0) + d * 2048));
+            o.a[d][second] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)((second ? da1 : da0) + kSlot * kDig + half * 512 + d * 2048));
         }
     };
-    auto multiply = [&](const Operands& o, int i) __attribute__((always_inline)) {
-        const int d = i / FB, f = i % FB;
-        const v4i a = {o.a[d][0][0], o.a[d][0][1], o.a[d][1][0], o.a[d][1][1]};
-        acc[d][f] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, o.b[f], acc[d][f], 0, 0, 0);
-    };
     // Stage t in two halves of 32 inputs; the operands of its first half are in registers when it starts:
-    //   products of the first half  | reads of the second half's operands; the second part of the loads of stage t - 1 + S; 4-bit: the
-    //                                 second half of the expansion of stage t + 1
+    //   products of the first half  | reads of the second half's operands; loads of the labels of stage t - 1 + S
     //   wait for the loads of stage t + 1 (4-bit: t + 2), barrier
-    //   products of the second half | the first part of the loads of stage t + S into the slot that stage t has left; reads of the first half
-    //                                 of stage t + 1;
-    //                                 4-bit: codes and table entries of stage t + 2, the first half of its expansion
-    // The barrier stands behind all reads of stage t (each wave waits for its own), behind the expansion of stage t + 1, and behind
-    // the arrival of stage t + 1.
+    //   products of the second half | loads of the weights of stage t + S; reads of the first half of stage t + 1
+    // The barrier stands behind all reads of stage t (each wave waits for its own) and behind the arrival of stage t + 1: slot t % S may be
+    // loaded again, slot (t + 1) % S be read.
+    // 4-bit weights through LDS: codes, table entries and the first blocks' expansion of stage t + 2 in the second half of stage t, the second
+    // blocks' in the first half of stage t + 1; half (t + 2) % 2 of the expanded weights is free behind the barrier of stage t.
+    // In registers: codes and first entry of stage t + 1 in the first half of stage t, its first expansion and second entry in the second half,
+    // its second expansion in its own first half.
     // The order inside a half is fixed: behind each product two reads (done well before the half ends), the loads far apart (a load that
     // cannot go out holds up the products behind it).
     using std::integral_constant;
     constexpr integral_constant<int, 0> k0{};
     constexpr integral_constant<int, 1> k1{};
-    constexpr integral_constant<int, kMx4 ? S - 3 : S - 2> k_ahead{};
+    static_assert(S % 2 == 0, "parities of stages follow from their slots");
+    constexpr int kAhead = kMx4 ? S - 3 : S - 2;
     const int stages = (nk + WK - 1) / WK;
-    auto loop = [&](auto dn) __attribute__((always_inline)) {
-        constexpr int kProducts = dn * FB, kReads = FB + 2 * dn;
+    // dn: the wave's tiles of 32 digits that hold groups
+    auto work = [&](auto dn) __attribute__((always_inline)) {
+        constexpr int kProducts = dn * FB, kReads = FB + 2 * dn, kSlots = kProducts > 4 ? kProducts : 4;
+        v16i acc[dn][FB];
+#pragma unroll
+        for (int d = 0; d < dn; d++) {
+            const int g0 = (wd * DA + d) * 2;
+            const int s0 = kMx4 || ws ? 0 : (int)lane_of(g_start, g0), s1 = kMx4 || ws ? 0 : (int)lane_of(g_start, g0 + 1);
+#pragma unroll
+            for (int f = 0; f < FB; f++)
+#pragma unroll
+                for (int r = 0; r < 16; r++) acc[d][f][r] = r < 8 ? s0 : s1;
+        }
+        auto multiply = [&](const auto& o, int i) __attribute__((always_inline)) {
+            const int d = i / FB, f = i % FB;
+            const v4i a = {o.a[d][0][0], o.a[d][0][1], o.a[d][1][0], o.a[d][1][1]};
+            acc[d][f] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, o.b[f], acc[d][f], 0, 0, 0);
+        };
         Operands o0, o1;
-        auto half = [&](const Operands& now, Operands& next, bool there, int t_read, int half_read, int t_load, auto part, int t_expand) __attribute__((always_inline)) {
-            constexpr int kSlots = kProducts > 4 ? kProducts : 4, kLoads = part ? kParts - kPart0 : kPart0;
+        auto half = [&](const Operands& now, Operands& next, bool there, auto u, auto second) __attribute__((always_inline)) {
+            constexpr int U = decltype(u)::value, kHalf = decltype(second)::value, kLoads = kHalf ? 2 * WT : GP;
+            constexpr integral_constant<int, (U + 1) % S> u1{};
+            constexpr integral_constant<int, (U + 2) % S> u2{};
+            constexpr integral_constant<int, (U + S - 1) % S> before{};
 #pragma unroll
             for (int m = 0; m < kSlots; m++) {
                 if (m < kProducts && there) multiply(now, m);
 #pragma unroll
-                for (int i = 0; i < kReads; i++) if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) read(next, t_read, half_read, i);
-                // (4-bit: the first half of an expansion follows its table entry, the second half has a half of products to itself)
-                if constexpr (!part) {
-                    if (m == 0) fetch_codes(t_expand);
-                    if (m == kSlots / 4) fetch_table();
+                for (int i = 0; i < kReads; i++)
+                    if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) { if constexpr (kHalf) read(next, u1, 0, i); else read(next, u, 1, i); }
+                if constexpr (kDirect) {
+                    static_assert(FB == WT, "a wave expands what it multiplies");
+                    if (m == 0 && !kHalf) fetch_codes(u1, (U + 1) & 1);
 #pragma unroll
-                    for (int i = 0; i < kSteps / 2; i++) if (kSlots / 2 + i * kSlots / kSteps == m) expand(t_expand, i);
-                } else {
+                    for (int i = 0; i < 4 * FB; i++)
+                        if (i * kSlots / (4 * FB) == m) next.b[i / 4][i % 4] = (int)four(code[(U + kHalf) & 1][i / 4][i % 4], lut[!kHalf][i / 4], !kHalf);
+                    if (m == kSlots / 2) fetch_table(kHalf);
+                } else if constexpr (kMx4) {
+                    if constexpr (kHalf) {
+                        if (m == 0) fetch_codes(u2, 0);
+                        if (m == kSlots / 4) { fetch_table(0); fetch_table(1); }
 #pragma unroll
-                    for (int i = 0; i < kSteps / 2; i++) if (i * 2 * kSlots / kSteps == m) expand(t_expand, kSteps / 2 + i);
+                        for (int i = 0; i < kSteps / 2; i++) if (kSlots / 2 + i * kSlots / kSteps == m) expand(U & 1, i);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kSteps / 2; i++) if (i * 2 * kSlots / kSteps == m) expand((U + 1) & 1, kSteps / 2 + i);
+                    }
                 }
 #pragma unroll
-                for (int i = 0; i < kLoads; i++) if ((2 * i + 1) * kSlots / (2 * kLoads) == m) load_piece(t_load, (part ? kPart0 : 0) + i);
+                for (int i = 0; i < kLoads; i++)
+                    if ((2 * i + 1) * kSlots / (2 * kLoads) == m) { if constexpr (kHalf) load_weights(u, i); else load_labels(before, i); }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
-#pragma unroll
-        for (int i = 0; i < kReads; i++) read(o0, 0, 0, i);
-        fetch_codes(1);
-        fetch_table();
-#pragma unroll
-        for (int i = 0; i < kSteps / 2; i++) expand(1, i);
-        for (int t = 0; t < stages; t++) {
+        int t = 0;
+        // one stage in slot u; false: it was the last
+        auto stage = [&](auto u) __attribute__((always_inline)) -> bool {
             const bool there = WK == 1 || WK * t + ws < nk;         // (the last round may be short of a stage for some sets)
-            half(o0, o1, there, t, 1, t - 1 + S, k1, t + 1);
-            arrived(k_ahead);
+            half(o0, o1, there, u, k0);
+            wait_loads<kAhead * kParts>();
             lds_barrier();
-            half(o1, o0, there, t + 1, 0, t + S, k0, t + 2);
+            half(o1, o0, there, u, k1);
+            return ++t < stages;
+        };
+#pragma unroll
+        for (int i = 0; i < kReads; i++) read(o0, k0, 0, i);
+        if constexpr (kDirect) {
+            fetch_codes(k0, 0);
+            fetch_table(0); fetch_table(1);
+#pragma unroll
+            for (int i = 0; i < 4 * FB; i++) o0.b[i / 4][i % 4] = (int)four(code[0][i / 4][i % 4], lut[0][i / 4], 0);
+        } else if constexpr (kMx4) {
+            fetch_codes(k1, 0);
+            fetch_table(0); fetch_table(1);
+#pragma unroll
+            for (int i = 0; i < kSteps / 2; i++) expand(1, i);
         }
-    };
+        if constexpr (S == 4) {
+            while (stage(k0) && stage(k1) && stage(integral_constant<int, 2>{}) && stage(integral_constant<int, 3>{})) {}
+        } else {
+            static_assert(S == 2, "slots");
+            while (stage(k0) && stage(k1)) {}
+        }
+        wait_loads<0>();
+        if constexpr (WK > 1) {
+            // the sums of the other sets come through LDS
+            lds_barrier();
+            u32x4* const part = (u32x4*)smem + wave * DA * FB * 256 + lane;
 #pragma unroll
-    for (int t = 0; t < S; t++) { issue(t, 0); if (t < S - 1) issue(t, 1); }
-    // (stages 0 and, 4-bit, 1; the last stage's second part is not out yet)
-    auto first_arrived = [&](auto n) __attribute__((always_inline)) {
-        constexpr int N = decltype(n)::value * kParts - (kParts - kPart0), NW8 = decltype(n)::value * 2 * WT - (2 * WT > kPart0 ? 2 * WT - kPart0 : 0);
-        if (loads_labels) wait_loads<N>(); else wait_loads<NW8>();
-    };
-    if constexpr (kMx4) {
-        first_arrived(integral_constant<int, S - 1>{});
-        fetch_codes(0);
-        fetch_table();
+            for (int s = 1; s < WK; s++) {
+                if (ws == s) {
 #pragma unroll
-        for (int i = 0; i < kSteps; i++) expand(0, i);              // (what a wave expands, it has loaded itself)
-        first_arrived(integral_constant<int, S - 2>{});
-    } else first_arrived(integral_constant<int, S - 1>{});
-    lds_barrier();
-    if constexpr (DA > 2) loop(integral_constant<int, DA>{});
-    else {
-        // waves whose digits lie past the tile's groups, in part or whole, leave out those products
-        const int mine = ((end - first + 1) >> 1) - wd * DA;
-        if (mine >= DA) loop(integral_constant<int, DA>{});
-        else if (mine > 0) loop(k1);
-        else loop(k0);
-    }
-    wait_loads<0>();
-    if constexpr (WK > 1) {
-        // the sums of the other sets come through LDS
-        lds_barrier();
-        u32x4* const part = (u32x4*)smem + wave * DA * FB * 256 + lane;
-#pragma unroll
-        for (int s = 1; s < WK; s++) {
-            if (ws == s) {
-#pragma unroll
-                for (int i = 0; i < DA * FB * 4; i++) {
-                    const v16i& v = acc[i / 4 / FB][i / 4 % FB];
-                    part[((s - 1) * NW * DA * FB * 4 + i) * 64] = u32x4{(uint32_t)v[i % 4 * 4], (uint32_t)v[i % 4 * 4 + 1], (uint32_t)v[i % 4 * 4 + 2], (uint32_t)v[i % 4 * 4 + 3]};
+                    for (int i = 0; i < dn * FB * 4; i++) {
+                        const v16i& v = acc[i / 4 / FB][i / 4 % FB];
+                        part[((s - 1) * NW * DA * FB * 4 + i) * 64] = u32x4{(uint32_t)v[i % 4 * 4], (uint32_t)v[i % 4 * 4 + 1], (uint32_t)v[i % 4 * 4 + 2], (uint32_t)v[i % 4 * 4 + 3]};
+                    }
                 }
             }
+            lds_barrier();
+            if (ws) return;
+#pragma unroll
+            for (int s = 1; s < WK; s++)
+#pragma unroll
+                for (int i = 0; i < dn * FB * 4; i++) {
+                    const u32x4 v = part[((s - 1) * NW * DA * FB * 4 + i) * 64];
+#pragma unroll
+                    for (int r = 0; r < 4; r++) acc[i / 4 / FB][i / 4 % FB][i % 4 * 4 + r] += (int)v[r];
+                }
         }
-        lds_barrier();
-        if (ws) return;
-#pragma unroll
-        for (int s = 1; s < WK; s++)
-#pragma unroll
-            for (int i = 0; i < DA * FB * 4; i++) {
-                const u32x4 v = part[((s - 1) * NW * DA * FB * 4 + i) * 64];
-#pragma unroll
-                for (int r = 0; r < 4; r++) acc[i / 4 / FB][i / 4 % FB][i % 4 * 4 + r] += (int)v[r];
-            }
-    }
 
-    // ---- reduction mod p, 16 bytes a lane ----
+        // ---- reduction mod p, 16 bytes a lane ----
 #pragma unroll
-    for (int d = 0; d < DA; d++) {
-        const int g0 = (wd * DA + d) * 2;
-        if (first + g0 >= end) break;
-        uint8_t* const dst = s_dst[g0 + h];
-        const ExpPrime* const P[2] = {&A.pr[__builtin_amdgcn_readfirstlane(s_prime[g0])], &A.pr[__builtin_amdgcn_readfirstlane(s_prime[g0 + 1])]};
+        for (int d = 0; d < dn; d++) {
+            const int g0 = (wd * DA + d) * 2;
+            if (g0 >= n_groups) break;
+            const uint64_t dst0 = lane_of(g_dst, g0), dst1 = lane_of(g_dst, g0 + 1);
+            uint8_t* const dst = (uint8_t*)(h ? dst1 : dst0);
+            const bool valid = g0 + h < n_groups;
 #pragma unroll
-        for (int f = 0; f < FB; f++) {
-            const int j = by * TL::F + (wf * FB + f) * 32 + j32;
-            uint32_t w[4];          // digits 4 h .. and 8 + 4 h .. of the first group, of the second
+            for (int f = 0; f < FB; f++) {
+                const int j = by * TL::F + (wf * FB + f) * 32 + j32;
+                uint32_t w[4];          // digits 4 h .. and 8 + 4 h .. of the first group, of the second
 #pragma unroll
-            for (int g = 0; g < 2; g++) {
-                const uint32_t prime = P[g]->p, mmagic = P[g]->mmagic, pow12 = P[g]->pow12;
-                auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - mul24(mulhi(v, mmagic), prime); };
-                uint32_t v[8];
+                for (int g = 0; g < 2; g++) {
+                    const uint32_t prime = lane_of(g_prime, g0 + g), mmagic = lane_of(g_magic, g0 + g);
+                    auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - mul24(mulhi(v, mmagic), prime); };
+                    uint32_t v[8];
 #pragma unroll
-                for (int r = 0; r < 8; r++) v[r] = (uint32_t)acc[d][f][8 * g + r];
-                if (P[g]->two_step) {
+                    for (int r = 0; r < 8; r++) v[r] = (uint32_t)acc[d][f][8 * g + r];
+                    if (lane_of(g_two_step, g0 + g)) {
+                        const uint32_t pow12 = lane_of(g_pow12, g0 + g);
 #pragma unroll
-                    for (int r = 0; r < 8; r++) v[r] = mul24(red1(v[r] >> 12), pow12) + (v[r] & 4095u);
+                        for (int r = 0; r < 8; r++) v[r] = mul24(red1(v[r] >> 12), pow12) + (v[r] & 4095u);
+                    }
+                    if (A.bias) {
+                        const int32_t b = j < M ? A.bias[(int64_t)e * M + j] % (int32_t)prime : 0;
+                        const uint32_t bm = (uint32_t)(b < 0 ? b + (int32_t)prime : b);
+                        const uint32_t* const one = (const uint32_t*)lane_of(g_one, g0 + g);
+#pragma unroll
+                        for (int r = 0; r < 8; r++) v[r] = red1(v[r]) + mul24(bm, (one[2 * (r / 4) + h] >> (8 * (r % 4))) & 0xffu);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 2; q++) w[2 * g + q] = red1(v[4 * q]) | red1(v[4 * q + 1]) << 8 | red1(v[4 * q + 2]) << 16 | red1(v[4 * q + 3]) << 24;
                 }
-                if (A.bias) {
-                    const int32_t b = j < M ? A.bias[(int64_t)e * M + j] % (int32_t)prime : 0;
-                    const uint32_t bm = (uint32_t)(b < 0 ? b + (int32_t)prime : b);
-#pragma unroll
-                    for (int r = 0; r < 8; r++) v[r] = red1(v[r]) + mul24(bm, (s_one[g0 + g][2 * (r / 4) + h] >> (8 * (r % 4))) & 0xffu);
-                }
-#pragma unroll
-                for (int q = 0; q < 2; q++) w[2 * g + q] = red1(v[4 * q]) | red1(v[4 * q + 1]) << 8 | red1(v[4 * q + 2]) << 16 | red1(v[4 * q + 3]) << 24;
+                // lanes 0-31 hold dwords 0, 2 of both groups, lanes 32-63 dwords 1, 3: after the swaps the first half holds the first group
+                const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                if (valid && j < M) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                __builtin_amdgcn_sched_barrier(0);      // (else all accumulators are read at once)
             }
-            // lanes 0-31 hold dwords 0, 2 of both groups, lanes 32-63 dwords 1, 3: after the swaps the first half holds the first group
-            const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-            if (dst && j < M) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
-            __builtin_amdgcn_sched_barrier(0);      // (else all accumulators are read at once)
         }
+    };
+    auto fill = [&](auto self, auto u) __attribute__((always_inline)) -> void {
+        constexpr int U = decltype(u)::value;
+        if constexpr (U < S) {
+#pragma unroll
+            for (int i = 0; i < 2 * WT; i++) load_weights(u, i);
+            if constexpr (U < S - 1) {
+#pragma unroll
+                for (int i = 0; i < GP; i++) load_labels(u, i);
+                self(self, integral_constant<int, U + 1>{});
+            }
+        }
+    };
+    fill(fill, k0);
+    wait_loads<(kMx4 ? S - 2 : S - 1) * kParts - GP>();             // stage 0, 4-bit: stage 1 too; the labels of stage S - 1 are not out yet
+    lds_barrier();
+    if constexpr (kMx4 && !kDirect) {
+        fetch_codes(k0, 0);
+        fetch_table(0); fetch_table(1);
+#pragma unroll
+        for (int i = 0; i < kSteps; i++) expand(0, i);
+        lds_barrier();
     }
+    // waves whose digits lie past the tile's groups, in part or whole, leave out those products (large tiles are rarely short)
+    const int mine = ((n_groups + 1) >> 1) - wd * DA;
+    if constexpr (DA * FB > 4) work(integral_constant<int, DA>{});
+    else if (mine > 2) work(integral_constant<int, DA>{});
+    else if (mine == 2) work(integral_constant<int, 2>{});
+    else work(k1);
 }
 
 int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, hipStream_t s) {
@@ -438,6 +490,7 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         ExpPrime& P = A.pr[i];
         const ModInfo& Mi = c->mods[c->prime[i]];
         A.chunk_first[i + 1] = A.chunk_first[i] + (int)Mi.nchunk;
+        P.chunk_first = A.chunk_first[i];
         P.p = c->prime[i]; P.mmagic = Mi.mmagic; P.pow12 = 4096u % P.p;
         P.one = L.bias ? (L.garble ? c->d_one0[i] : c->d_one[i]) : nullptr;
         P.in = view_of(in, i); P.out = view_of(out, i);
@@ -455,9 +508,9 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
     }
     const int64_t groups = (int64_t)A.chunk_first[c->k] * L.n;
     if (groups > 0x7fffffff - 64) return DASH_ESIZE;
-    auto launch = [&](auto tl) -> int {
+    auto launch = [&](auto tl, auto fmt) -> int {
         typedef decltype(tl) TL;
-        const bool mx4 = L.format == DASH_MX4;
+        constexpr bool mx4 = decltype(fmt)::value == DASH_MX4;
         int64_t cols = 0;
         if (L.routing) {
             const int s = TL::KIND + (mx4 ? 2 : 0);
@@ -476,13 +529,15 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         const int64_t total = cols * A.row_blocks;
         if (cols * A.sty > 0x7fffffff || total > 0x7fffff00) return DASH_ESIZE;
         ProfScope ps(c->prof, DASH_PROF_LINEAR, s, macs, bytes);
-        auto kernel = mx4 ? k_experts_mfma<DASH_MX4, TL> : k_experts_mfma<DASH_W8, TL>;
-        hipLaunchKernelGGL(kernel, dim3((uint32_t)((total + 7) / 8 * 8)), dim3(TL::T), 0, s, A);
+        hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3((uint32_t)((total + 7) / 8 * 8)), dim3(TL::T), 0, s, A);
         return DASH_OK;
     };
     const int64_t blocks_big = groups / EBig::G * ((L.M + EBig::F - 1) / EBig::F), blocks_narrow = (groups + 7) / 8 * ((L.M + 127) / 128);
     const int tile = c->experts_tile ? c->experts_tile : blocks_big >= 256 ? 1 : blocks_narrow <= 256 ? 3 : 2;
-    const int st = tile == 1 ? launch(EBig{}) : tile == 3 ? launch(EDeep{}) : launch(ENarrow{});
+    const std::integral_constant<int, DASH_W8> w8{};
+    const std::integral_constant<int, DASH_MX4> mx4{};
+    const int st = L.format == DASH_MX4 ? (tile == 1 ? launch(EBig{}, mx4) : tile == 3 ? launch(EDeep4{}, mx4) : launch(ENarrow4{}, mx4))
+                                        : (tile == 1 ? launch(EBig{}, w8) : tile == 3 ? launch(EDeep{}, w8) : launch(ENarrow{}, w8));
     if (st) return st;
     DASH_HIP(hipGetLastError());
     return DASH_OK;

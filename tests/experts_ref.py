@@ -38,8 +38,8 @@ def mx4_unpack(buf, E, M, K):
     """prepared buffer -> (codes [E][M][K], shifts [E][M][ceil(K / 32)], everything else zero)"""
     mt, kt = -(-M // 32), -(-K // 64)
     t = buf.reshape(E, mt, kt, 1088)
-    by = t[..., :1024].reshape(E, mt, kt, 32, 2, 16)
-    codes = np.stack([by & 15, by >> 4], axis=-2).reshape(E, mt, kt, 32, 64).transpose(0, 1, 3, 2, 4).reshape(E, mt * 32, kt * 64)
+    by = t[..., :1024].reshape(E, mt, kt, 32, 32)
+    codes = np.concatenate([by & 15, by >> 4], axis=-1).transpose(0, 1, 3, 2, 4).reshape(E, mt * 32, kt * 64)
     shifts = t[..., 1024:].reshape(E, mt, kt, 32, 2).transpose(0, 1, 3, 2, 4).reshape(E, mt * 32, kt * 2)
     rest = codes.copy()
     rest[:, :M, :K] = 0
