@@ -33,29 +33,26 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 typedef __attribute__((address_space(3))) v2i* lds_v2i;
 
-// WK sets of WD x WF waves (along the inputs; along digits, along features), a wave DA x FB tiles of 32 digits x 32 features; S stages of 64
-// inputs in LDS for each set; WPE: waves per SIMD that the registers are held to; KIND: tiles of the routing (byte weights; + 2: 4-bit)
-template <int WK_, int WD_, int WF_, int DA_, int FB_, int S_, int WPE_, int KIND_>
+// WD x WF waves (along digits, along features), a wave DA x FB tiles of 32 digits x 32 features; S stages of 64 inputs in LDS; WPE: waves
+// per SIMD that the registers are held to; KIND: tiles of the routing (byte weights; + 2: 4-bit)
+template <int WD_, int WF_, int DA_, int FB_, int S_, int WPE_, int KIND_>
 struct ETile {
-    static constexpr int WK = WK_, WD = WD_, WF = WF_, DA = DA_, FB = FB_, S = S_, WPE = WPE_, KIND = KIND_;
-    static constexpr int NW = WD * WF, T = 64 * NW * WK;
+    static constexpr int WD = WD_, WF = WF_, DA = DA_, FB = FB_, S = S_, WPE = WPE_, KIND = KIND_;
+    static constexpr int NW = WD * WF, T = 64 * NW;
     static constexpr int G = 2 * WD * DA;            // groups per block
     static constexpr int FT = WF * FB, F = 32 * FT;  // feature tiles, features per block
     static constexpr int GP = G / NW, WT = FT / NW;  // groups and tiles of weights that a wave loads
     static_assert(G == kTileKind[KIND].groups && GP * NW == G && WT * NW == FT, "loader roles");
 };
-typedef ETile<1, 2, 4, 4, 2, 4, 2, 0> EBig;          // 256 digits x 256 features
-typedef ETile<1, 2, 2, 2, 2, 4, 2, 1> ENarrow;       // 128 digits x 128 features
-typedef ETile<2, 2, 2, 2, 2, 4, 2, 1> EDeep;         // the same by two sets of waves
-typedef ETile<1, 1, 4, 4, 1, 4, 2, 1> ENarrow4;      // the narrow tile for 4-bit weights
-typedef ETile<2, 1, 4, 4, 1, 4, 2, 1> EDeep4;
+typedef ETile<2, 4, 4, 2, 4, 2, 0> EBig;             // 256 digits x 256 features
+typedef ETile<2, 2, 2, 2, 4, 2, 1> ENarrow;          // 128 digits x 128 features
+typedef ETile<1, 4, 4, 1, 4, 2, 1> ENarrow4;         // the same for 4-bit weights
 
 struct ExpPrime {
     uint32_t p;
     uint32_t mmagic;            // ceil(2^32 / p)
     uint32_t pow12;             // 4096 mod p
     uint32_t start;             // multiple of p that the sums start at
-    uint32_t two_step;          // sums are too large for one multiplication by mmagic
     int32_t chunk_first;        // first chunk in the numbering of all
     const uint8_t* one;         // chunked label of the constant-one wire, or NULL
     LView in, out;
@@ -68,6 +65,7 @@ struct ExpArgs {
     const RouteTile* tiles;
     const int32_t* n_tiles;
     int M, K, E, n, top_k, k;
+    int plain;                          // no bias, and every sum v below the bound up to which v / p is one multiplication by mmagic
     int cols, row_blocks, sty;          // blocks along the groups (without routing) and along the features; rows of a band
     int first[DASH_MAX_PRIMES + 1];     // without routing, 4-bit: first block along the groups of every prime
     int chunk_first[DASH_MAX_PRIMES + 1];   // first chunk of every prime in the numbering of all; past the last prime: a number no chunk has
@@ -96,7 +94,7 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 template <int FMT, class TL>
 __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A) {
-    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW, WK = TL::WK;
+    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW;
     constexpr bool kMx4 = FMT == DASH_MX4;
     constexpr bool kDirect = kMx4 && TL::WD == 1;       // a wave's weights are its own: expanded in registers
     // ---- block -> tile ----
@@ -120,16 +118,14 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     } else first = bx * G;
     const int end = A.chunk_first[kMx4 ? pi + 1 : A.k] * count;        // groups of the tile: first .. min(first + G, end) - 1
     const int M = A.M, K = A.K;
-    const int tid = threadIdx.x, lane = tid & 63, wave_ = __builtin_amdgcn_readfirstlane(tid >> 6), ws = wave_ / NW, wave = wave_ % NW;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wd = wave / TL::WF, wf = wave % TL::WF;
 
     constexpr int kDig = G * 1024, kRaw = kMx4 ? 1280 : 2048;       // bytes of a stage's labels; of a stage's weights per feature tile, as loaded
     constexpr int kExp = kMx4 && !kDirect ? FT * 2048 : 0;          // 4-bit: bytes of an expanded stage
     // one array: its address goes into the loads, so that the compiler takes all of it to change at their waits and barriers
-    constexpr int kSet = S * kDig + S * FT * kRaw + 2 * kExp;       // of a set of waves
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[WK * kSet];
-    static_assert((WK - 1) * NW * DA * FB * 4096 <= WK * kSet, "the sums of the sets are added up in it");
-    uint8_t* const s_dig = smem + ws * kSet;
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[S * kDig + S * FT * kRaw + 2 * kExp];
+    uint8_t* const s_dig = smem;
     uint8_t* const s_raw = s_dig + S * kDig;
     uint8_t* const s_exp = s_raw + S * FT * kRaw;
     __shared__ u32x4 s_lut[kMx4 ? 256 : 1];
@@ -137,7 +133,7 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     // ---- the groups of the tile: group g of it in lane g of every wave ----
     const int n_groups = end - first < G ? end - first : G;
     uint64_t g_src, g_dst, g_one = 0;
-    uint32_t g_prime, g_magic, g_pow12, g_start, g_two_step;
+    uint32_t g_prime, g_magic, g_pow12, g_start;
     {
         const int g = first + (lane < n_groups ? lane : 0), chunk = g / count, t = g - chunk * count, row = A.rows ? A.rows[start + t] : t;
         int p = 0;
@@ -148,10 +144,10 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         g_src = (uint64_t)(P.in.p + (int64_t)ch * P.in.cs + (int64_t)(row / A.top_k) * K * 16);
         g_dst = (uint64_t)(P.out.p + (int64_t)ch * P.out.cs + (int64_t)row * M * 16);
         if (A.bias) g_one = (uint64_t)(P.one + 16 * ch);
-        g_prime = P.p; g_magic = P.mmagic; g_pow12 = P.pow12; g_start = P.start; g_two_step = P.two_step;
+        g_prime = P.p; g_magic = P.mmagic; g_pow12 = P.pow12; g_start = P.start;
     }
     if (e >= A.E) {         // rows of no expert: the value 0 on both sides
-        for (int g = wave_; g < n_groups; g += NW * WK) {
+        for (int g = wave; g < n_groups; g += NW) {
             uint8_t* const dst = (uint8_t*)lane_of(g_dst, g);
             for (int j = by * TL::F + lane; j < M && j < by * TL::F + TL::F; j += 64) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
         }
@@ -175,11 +171,11 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         lab[i] = buffer_of((const uint8_t*)lane_of(g_src, g), g < n_groups ? (uint32_t)K * 16u : 0u);
     }
     const uint32_t dig0 = (uint32_t)(uintptr_t)(lds_ptr)s_dig + wave * GP * 1024, raw0 = (uint32_t)(uintptr_t)(lds_ptr)s_raw + wave * WT * kRaw;
-    // A set takes every WK-th stage of 64 inputs: its stage t are the inputs from 64 (WK t + ws), in slot t % S.  Stages past the end load
-    // nothing (their offsets lie past the buffers) but count.  A lane's offsets run along with the stages.
+    // Stage t, the inputs from 64 t, goes into slot t % S.  Stages past the end load nothing (their offsets lie past the buffers) but count.  A
+    // lane's offsets run along with the stages.
     // Words 8 .. 15 of every 16 of a group with an odd number stand before words 0 .. 7: the reads of two groups meet different banks.
-    uint32_t off_w = 16u * lane + (uint32_t)(ws * kTileBytes), off_s = 4u * (lane & 15) + kMx4Codes + (uint32_t)(ws * kTileBytes);
-    uint32_t off_l = 16u * lane + 1024u * ws;                       // (group with an odd number: ^ 128)
+    uint32_t off_w = 16u * lane, off_s = 4u * (lane & 15) + kMx4Codes;
+    uint32_t off_l = 16u * lane;                                    // (group with an odd number: ^ 128)
     constexpr int kParts = 2 * WT + GP;                             // loads of a stage: weights, then labels
     auto load_weights = [&](auto slot, int i) __attribute__((always_inline)) {
         constexpr int kSlot = decltype(slot)::value * FT * kRaw;
@@ -187,12 +183,12 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         if (i % 2 == 0) load_lds16<kSlot, 0>(to, wgt[i / 2], off_w);
         else if constexpr (kMx4) load_lds4<kSlot + kMx4Codes>(to, wgt[i / 2], off_s);
         else load_lds16<kSlot, 1024>(to, wgt[i / 2], off_w);
-        if (i == 2 * WT - 1) { off_w += WK * kTileBytes; off_s += WK * kTileBytes; }
+        if (i == 2 * WT - 1) { off_w += kTileBytes; off_s += kTileBytes; }
     };
     auto load_labels = [&](auto slot, int i) __attribute__((always_inline)) {
         constexpr int kSlot = decltype(slot)::value * kDig;
         load_lds16<kSlot, 0>(dig0 + i * 1024, lab[i], i % 2 ? off_l ^ 128u : off_l);
-        if (i == GP - 1) off_l += WK * 1024;
+        if (i == GP - 1) off_l += 1024;
     };
 
     // ---- 4-bit weights ----
@@ -295,7 +291,6 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     constexpr integral_constant<int, 1> k1{};
     static_assert(S % 2 == 0, "parities of stages follow from their slots");
     constexpr int kAhead = kMx4 ? S - 3 : S - 2;
-    const int stages = (nk + WK - 1) / WK;
     // dn: the wave's tiles of 32 digits that hold groups
     auto work = [&](auto dn) __attribute__((always_inline)) {
         constexpr int kProducts = dn * FB, kReads = FB + 2 * dn, kSlots = kProducts > 4 ? kProducts : 4;
@@ -303,7 +298,7 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
 #pragma unroll
         for (int d = 0; d < dn; d++) {
             const int g0 = (wd * DA + d) * 2;
-            const int s0 = kMx4 || ws ? 0 : (int)lane_of(g_start, g0), s1 = kMx4 || ws ? 0 : (int)lane_of(g_start, g0 + 1);
+            const int s0 = kMx4 ? 0 : (int)lane_of(g_start, g0), s1 = kMx4 ? 0 : (int)lane_of(g_start, g0 + 1);
 #pragma unroll
             for (int f = 0; f < FB; f++)
 #pragma unroll
@@ -315,14 +310,14 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
             acc[d][f] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, o.b[f], acc[d][f], 0, 0, 0);
         };
         Operands o0, o1;
-        auto half = [&](const Operands& now, Operands& next, bool there, auto u, auto second) __attribute__((always_inline)) {
+        auto half = [&](const Operands& now, Operands& next, auto u, auto second) __attribute__((always_inline)) {
             constexpr int U = decltype(u)::value, kHalf = decltype(second)::value, kLoads = kHalf ? 2 * WT : GP;
             constexpr integral_constant<int, (U + 1) % S> u1{};
             constexpr integral_constant<int, (U + 2) % S> u2{};
             constexpr integral_constant<int, (U + S - 1) % S> before{};
 #pragma unroll
             for (int m = 0; m < kSlots; m++) {
-                if (m < kProducts && there) multiply(now, m);
+                if (m < kProducts) multiply(now, m);
 #pragma unroll
                 for (int i = 0; i < kReads; i++)
                     if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) { if constexpr (kHalf) read(next, u1, 0, i); else read(next, u, 1, i); }
@@ -353,12 +348,11 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         int t = 0;
         // one stage in slot u; false: it was the last
         auto stage = [&](auto u) __attribute__((always_inline)) -> bool {
-            const bool there = WK == 1 || WK * t + ws < nk;         // (the last round may be short of a stage for some sets)
-            half(o0, o1, there, u, k0);
+            half(o0, o1, u, k0);
             wait_loads<kAhead * kParts>();
             lds_barrier();
-            half(o1, o0, there, u, k1);
-            return ++t < stages;
+            half(o1, o0, u, k1);
+            return ++t < nk;
         };
 #pragma unroll
         for (int i = 0; i < kReads; i++) read(o0, k0, 0, i);
@@ -380,72 +374,50 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
             while (stage(k0) && stage(k1)) {}
         }
         wait_loads<0>();
-        if constexpr (WK > 1) {
-            // the sums of the other sets come through LDS
-            lds_barrier();
-            u32x4* const part = (u32x4*)smem + wave * DA * FB * 256 + lane;
-#pragma unroll
-            for (int s = 1; s < WK; s++) {
-                if (ws == s) {
-#pragma unroll
-                    for (int i = 0; i < dn * FB * 4; i++) {
-                        const v16i& v = acc[i / 4 / FB][i / 4 % FB];
-                        part[((s - 1) * NW * DA * FB * 4 + i) * 64] = u32x4{(uint32_t)v[i % 4 * 4], (uint32_t)v[i % 4 * 4 + 1], (uint32_t)v[i % 4 * 4 + 2], (uint32_t)v[i % 4 * 4 + 3]};
-                    }
-                }
-            }
-            lds_barrier();
-            if (ws) return;
-#pragma unroll
-            for (int s = 1; s < WK; s++)
-#pragma unroll
-                for (int i = 0; i < dn * FB * 4; i++) {
-                    const u32x4 v = part[((s - 1) * NW * DA * FB * 4 + i) * 64];
-#pragma unroll
-                    for (int r = 0; r < 4; r++) acc[i / 4 / FB][i / 4 % FB][i % 4 * 4 + r] += (int)v[r];
-                }
-        }
-
         // ---- reduction mod p, 16 bytes a lane ----
+        // (plain: no bias, every sum takes one multiplication; the common case, without branches)
+        auto finish = [&](auto plain) __attribute__((always_inline)) {
 #pragma unroll
-        for (int d = 0; d < dn; d++) {
-            const int g0 = (wd * DA + d) * 2;
-            if (g0 >= n_groups) break;
-            const uint64_t dst0 = lane_of(g_dst, g0), dst1 = lane_of(g_dst, g0 + 1);
-            uint8_t* const dst = (uint8_t*)(h ? dst1 : dst0);
-            const bool valid = g0 + h < n_groups;
+            for (int d = 0; d < dn; d++) {
+                const int g0 = (wd * DA + d) * 2;
+                if (g0 >= n_groups) break;
+                const uint64_t dst0 = lane_of(g_dst, g0), dst1 = lane_of(g_dst, g0 + 1);
+                uint8_t* const dst = (uint8_t*)(h ? dst1 : dst0);
+                const bool valid = g0 + h < n_groups;
 #pragma unroll
-            for (int f = 0; f < FB; f++) {
-                const int j = by * TL::F + (wf * FB + f) * 32 + j32;
-                uint32_t w[4];          // digits 4 h .. and 8 + 4 h .. of the first group, of the second
+                for (int f = 0; f < FB; f++) {
+                    const int j = by * TL::F + (wf * FB + f) * 32 + j32;
+                    uint32_t w[4];          // digits 4 h .. and 8 + 4 h .. of the first group, of the second
 #pragma unroll
-                for (int g = 0; g < 2; g++) {
-                    const uint32_t prime = lane_of(g_prime, g0 + g), mmagic = lane_of(g_magic, g0 + g);
-                    auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - mul24(mulhi(v, mmagic), prime); };
-                    uint32_t v[8];
+                    for (int g = 0; g < 2; g++) {
+                        const uint32_t prime = lane_of(g_prime, g0 + g), mmagic = lane_of(g_magic, g0 + g);
+                        auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - __umul24(mulhi(v, mmagic), prime); };
+                        uint32_t v[8];
 #pragma unroll
-                    for (int r = 0; r < 8; r++) v[r] = (uint32_t)acc[d][f][8 * g + r];
-                    if (lane_of(g_two_step, g0 + g)) {
-                        const uint32_t pow12 = lane_of(g_pow12, g0 + g);
+                        for (int r = 0; r < 8; r++) v[r] = (uint32_t)acc[d][f][8 * g + r];
+                        if constexpr (!plain) {
+                            const uint32_t pow12 = lane_of(g_pow12, g0 + g);
 #pragma unroll
-                        for (int r = 0; r < 8; r++) v[r] = mul24(red1(v[r] >> 12), pow12) + (v[r] & 4095u);
+                            for (int r = 0; r < 8; r++) v[r] = __umul24(red1(v[r] >> 12), pow12) + (v[r] & 4095u);
+                            if (A.bias) {
+                                const int32_t b = j < M ? A.bias[(int64_t)e * M + j] % (int32_t)prime : 0;
+                                const uint32_t bm = (uint32_t)(b < 0 ? b + (int32_t)prime : b);
+                                const uint32_t* const one = (const uint32_t*)lane_of(g_one, g0 + g);
+#pragma unroll
+                                for (int r = 0; r < 8; r++) v[r] = red1(v[r]) + __umul24(bm, (one[2 * (r / 4) + h] >> (8 * (r % 4))) & 0xffu);
+                            }
+                        }
+#pragma unroll
+                        for (int q = 0; q < 2; q++) w[2 * g + q] = red1(v[4 * q]) | red1(v[4 * q + 1]) << 8 | red1(v[4 * q + 2]) << 16 | red1(v[4 * q + 3]) << 24;
                     }
-                    if (A.bias) {
-                        const int32_t b = j < M ? A.bias[(int64_t)e * M + j] % (int32_t)prime : 0;
-                        const uint32_t bm = (uint32_t)(b < 0 ? b + (int32_t)prime : b);
-                        const uint32_t* const one = (const uint32_t*)lane_of(g_one, g0 + g);
-#pragma unroll
-                        for (int r = 0; r < 8; r++) v[r] = red1(v[r]) + mul24(bm, (one[2 * (r / 4) + h] >> (8 * (r % 4))) & 0xffu);
-                    }
-#pragma unroll
-                    for (int q = 0; q < 2; q++) w[2 * g + q] = red1(v[4 * q]) | red1(v[4 * q + 1]) << 8 | red1(v[4 * q + 2]) << 16 | red1(v[4 * q + 3]) << 24;
+                    // lanes 0-31 hold dwords 0, 2 of both groups, lanes 32-63 dwords 1, 3: after the swaps the first half holds the first group
+                    const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+                    if (valid && j < M) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                    __builtin_amdgcn_sched_barrier(0);      // (else all accumulators are read at once)
                 }
-                // lanes 0-31 hold dwords 0, 2 of both groups, lanes 32-63 dwords 1, 3: after the swaps the first half holds the first group
-                const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-                if (valid && j < M) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
-                __builtin_amdgcn_sched_barrier(0);      // (else all accumulators are read at once)
             }
-        }
+        };
+        if (A.plain) finish(k1); else finish(k0);
     };
     auto fill = [&](auto self, auto u) __attribute__((always_inline)) -> void {
         constexpr int U = decltype(u)::value;
@@ -484,6 +456,7 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
     A.M = L.M; A.K = L.K; A.E = L.E; A.n = (int)L.n; A.top_k = L.top_k;
     double macs = 0, bytes = (double)L.E * A.expert_bytes;
     A.k = c->k;
+    A.plain = L.bias == nullptr;
     for (int i = 0; i <= DASH_MAX_PRIMES; i++) A.chunk_first[i] = 0x7fffffff;
     A.chunk_first[0] = 0;
     for (int i = 0; i < c->k; i++) {
@@ -502,7 +475,7 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         }
         // v / p = mulhi(v, mmagic) as long as v times the rounding of mmagic stays below 2^32; the quotient goes into a 24-bit product
         const uint64_t over = (uint64_t)P.mmagic * P.p - (1ull << 32);
-        P.two_step = vmax * over >= (1ull << 32) || vmax / P.p >= (1u << 24);
+        if (vmax * over >= (1ull << 32) || vmax / P.p >= (1u << 24)) A.plain = 0;
         macs += (double)L.n * L.M * L.K * Mi.lam;
         bytes += ((double)(L.n / L.top_k) * L.K + (double)L.n * L.M) * Mi.lam;
     }
@@ -532,12 +505,11 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3((uint32_t)((total + 7) / 8 * 8)), dim3(TL::T), 0, s, A);
         return DASH_OK;
     };
-    const int64_t blocks_big = groups / EBig::G * ((L.M + EBig::F - 1) / EBig::F), blocks_narrow = (groups + 7) / 8 * ((L.M + 127) / 128);
-    const int tile = c->experts_tile ? c->experts_tile : blocks_big >= 256 ? 1 : blocks_narrow <= 256 ? 3 : 2;
+    const int64_t blocks_big = groups / EBig::G * ((L.M + EBig::F - 1) / EBig::F);
+    const bool big = c->experts_tile ? c->experts_tile == 1 : blocks_big >= 256;
     const std::integral_constant<int, DASH_W8> w8{};
     const std::integral_constant<int, DASH_MX4> mx4{};
-    const int st = L.format == DASH_MX4 ? (tile == 1 ? launch(EBig{}, mx4) : tile == 3 ? launch(EDeep4{}, mx4) : launch(ENarrow4{}, mx4))
-                                        : (tile == 1 ? launch(EBig{}, w8) : tile == 3 ? launch(EDeep{}, w8) : launch(ENarrow{}, w8));
+    const int st = L.format == DASH_MX4 ? (big ? launch(EBig{}, mx4) : launch(ENarrow4{}, mx4)) : (big ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
     if (st) return st;
     DASH_HIP(hipGetLastError());
     return DASH_OK;
