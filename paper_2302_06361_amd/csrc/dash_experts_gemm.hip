@@ -35,18 +35,22 @@ typedef __attribute__((address_space(3))) v2i* lds_v2i;
 
 // WD x WF waves (along digits, along features), a wave DA x FB tiles of 32 digits x 32 features; S stages of 64 inputs in LDS; WPE: waves
 // per SIMD that the registers are held to; KIND: tiles of the routing (byte weights; + 2: 4-bit)
-template <int WD_, int WF_, int DA_, int FB_, int S_, int WPE_, int KIND_>
+template <int WD_, int WF_, int DA_, int FB_, int S_, int WPE_, int KIND_, bool PERSIST_>
 struct ETile {
     static constexpr int WD = WD_, WF = WF_, DA = DA_, FB = FB_, S = S_, WPE = WPE_, KIND = KIND_;
+    static constexpr bool PERSIST = PERSIST_;        // a block takes tile after tile (one block per CU)
     static constexpr int NW = WD * WF, T = 64 * NW;
     static constexpr int G = 2 * WD * DA;            // groups per block
     static constexpr int FT = WF * FB, F = 32 * FT;  // feature tiles, features per block
     static constexpr int GP = G / NW, WT = FT / NW;  // groups and tiles of weights that a wave loads
     static_assert(G == kTileKind[KIND].groups && GP * NW == G && WT * NW == FT, "loader roles");
 };
-typedef ETile<2, 4, 4, 2, 4, 2, 0> EBig;             // 256 digits x 256 features
-typedef ETile<2, 2, 2, 2, 4, 2, 1> ENarrow;          // 128 digits x 128 features
-typedef ETile<1, 4, 4, 1, 4, 2, 1> ENarrow4;         // the same for 4-bit weights
+typedef ETile<2, 4, 4, 2, 4, 2, 0, true> EBig;       // 256 digits x 256 features
+typedef ETile<2, 4, 4, 2, 4, 2, 0, false> EBig4;     // the same for 4-bit weights (the registers do not hold a next tile beside them)
+typedef ETile<2, 2, 2, 2, 4, 2, 1, false> ENarrow;   // 128 digits x 128 features
+typedef ETile<1, 4, 4, 1, 4, 2, 1, false> ENarrow4;  // the same for 4-bit weights
+
+constexpr int kCus = 256;       // (a multiple of the 8 XCDs)
 
 struct ExpPrime {
     uint32_t p;
@@ -97,29 +101,38 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW;
     constexpr bool kMx4 = FMT == DASH_MX4;
     constexpr bool kDirect = kMx4 && TL::WD == 1;       // a wave's weights are its own: expanded in registers
-    // ---- block -> tile ----
+    const int M = A.M, K = A.K, nk = (K + 63) / 64;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wd = wave / TL::WF, wf = wave % TL::WF;
+
+    // ---- block -> tiles ----
     // Work-groups go to the 8 XCDs in turn, each with an L2 of its own: an XCD takes a run of consecutive tiles, numbered in bands of `sty`
     // row blocks, row block after row block, then column after column.  The blocks on an XCD at one time then share a band's weights, which
     // stay in its L2 while the labels pass once.
-    const int cols = A.tiles ? *A.n_tiles : A.cols, total = cols * A.row_blocks, run = (total + 7) >> 3;
-    const int seq = blockIdx.x >> 3, at = (int)(blockIdx.x & 7) * run + seq;
-    if (seq >= run || at >= total) return;
-    const int band = at / (A.sty * cols), in_band = at - band * (A.sty * cols);
-    const int height = A.row_blocks - band * A.sty < A.sty ? A.row_blocks - band * A.sty : A.sty;
-    const int bx = in_band / height, by = band * A.sty + in_band - bx * height;
-    int e = 0, pi = 0, start = 0, count = A.n, first;
-    if (A.tiles) {
-        const RouteTile t = A.tiles[bx];
-        e = (int)(t.expert_prime & 0xffffffu); pi = (int)(t.expert_prime >> 24);
-        start = t.start; count = t.count; first = t.first;
-    } else if (kMx4) {
-        while (bx >= A.first[pi + 1]) pi++;
-        first = A.chunk_first[pi] * count + (bx - A.first[pi]) * G;
-    } else first = bx * G;
-    const int end = A.chunk_first[kMx4 ? pi + 1 : A.k] * count;        // groups of the tile: first .. min(first + G, end) - 1
-    const int M = A.M, K = A.K;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wd = wave / TL::WF, wf = wave % TL::WF;
+    const int cols = A.tiles ? __builtin_amdgcn_readfirstlane(*A.n_tiles) : A.cols, total = cols * A.row_blocks, run = (total + 7) >> 3, run0 = (int)(blockIdx.x & 7) * run;
+    struct Tile { int by, e, pi, start, count, first, n_groups; };      // n_groups: groups first .. first + n_groups - 1, at most G
+    auto decode = [&](int seq, Tile& t) __attribute__((always_inline)) -> bool {
+        const int at = run0 + seq;
+        if (seq >= run || at >= total) return false;
+        const int band = at / (A.sty * cols), in_band = at - band * (A.sty * cols);
+        const int height = A.row_blocks - band * A.sty < A.sty ? A.row_blocks - band * A.sty : A.sty;
+        const int bx = in_band / height;
+        t.by = band * A.sty + in_band - bx * height;
+        t.e = 0; t.pi = 0; t.start = 0; t.count = A.n;
+        if (A.tiles) {
+            const RouteTile r = A.tiles[bx];
+            const uint32_t ep = (uint32_t)__builtin_amdgcn_readfirstlane((int)r.expert_prime);
+            t.e = (int)(ep & 0xffffffu); t.pi = (int)(ep >> 24);
+            t.start = __builtin_amdgcn_readfirstlane(r.start); t.count = __builtin_amdgcn_readfirstlane(r.count);
+            t.first = __builtin_amdgcn_readfirstlane(r.first);
+        } else if (kMx4) {
+            while (bx >= A.first[t.pi + 1]) t.pi++;
+            t.first = A.chunk_first[t.pi] * t.count + (bx - A.first[t.pi]) * G;
+        } else t.first = bx * G;
+        const int end = A.chunk_first[kMx4 ? t.pi + 1 : A.k] * t.count;
+        t.n_groups = end - t.first < G ? end - t.first : G;
+        return true;
+    };
 
     constexpr int kDig = G * 1024, kRaw = kMx4 ? 1280 : 2048;       // bytes of a stage's labels; of a stage's weights per feature tile, as loaded
     constexpr int kExp = kMx4 && !kDirect ? FT * 2048 : 0;          // 4-bit: bytes of an expanded stage
@@ -130,52 +143,72 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     uint8_t* const s_exp = s_raw + S * FT * kRaw;
     __shared__ u32x4 s_lut[kMx4 ? 256 : 1];
 
-    // ---- the groups of the tile: group g of it in lane g of every wave ----
-    const int n_groups = end - first < G ? end - first : G;
-    uint64_t g_src, g_dst, g_one = 0;
-    uint32_t g_prime, g_magic, g_pow12, g_start;
-    {
-        const int g = first + (lane < n_groups ? lane : 0), chunk = g / count, t = g - chunk * count, row = A.rows ? A.rows[start + t] : t;
-        int p = 0;
-#pragma unroll
-        for (int i = 1; i < DASH_MAX_PRIMES; i++) p += chunk >= A.chunk_first[i] ? 1 : 0;
-        const ExpPrime& P = A.pr[p];
-        const int ch = chunk - P.chunk_first;
-        g_src = (uint64_t)(P.in.p + (int64_t)ch * P.in.cs + (int64_t)(row / A.top_k) * K * 16);
-        g_dst = (uint64_t)(P.out.p + (int64_t)ch * P.out.cs + (int64_t)row * M * 16);
-        if (A.bias) g_one = (uint64_t)(P.one + 16 * ch);
-        g_prime = P.p; g_magic = P.mmagic; g_pow12 = P.pow12; g_start = P.start;
-    }
-    if (e >= A.E) {         // rows of no expert: the value 0 on both sides
-        for (int g = wave; g < n_groups; g += NW) {
-            uint8_t* const dst = (uint8_t*)lane_of(g_dst, g);
-            for (int j = by * TL::F + lane; j < M && j < by * TL::F + TL::F; j += 64) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
-        }
-        return;
+    // the primes, for lanes that each want another
+    struct PrimeLds { uint64_t in, in_cs, out, out_cs, one; uint32_t p, mmagic, pow12, start, chunk_first, pad; };
+    __shared__ PrimeLds s_pr[DASH_MAX_PRIMES];
+    if (tid < A.k) {
+        const ExpPrime& P = A.pr[tid];
+        s_pr[tid] = PrimeLds{(uint64_t)P.in.p, (uint64_t)P.in.cs, (uint64_t)P.out.p, (uint64_t)P.out.cs, (uint64_t)P.one, P.p, P.mmagic, P.pow12, P.start, (uint32_t)P.chunk_first, 0};
     }
 
+    // ---- the groups of a tile: group g of it in lane g of every wave ----
+    struct Begun { int chunk, row; };           // chunk in the numbering of all, row (a load in flight)
+    auto begin = [&](const Tile& t) __attribute__((always_inline)) -> Begun {
+        const int g = t.first + (lane < t.n_groups ? lane : 0), chunk = g / t.count, at = g - chunk * t.count;
+        return Begun{chunk, A.rows ? A.rows[t.start + at] : at};
+    };
+    struct Groups { uint64_t src, dst, one; uint32_t prime, magic, pow12, start; };
+    auto groups_of = [&](const Begun& b) __attribute__((always_inline)) -> Groups {
+        int p = 0;
+#pragma unroll
+        for (int i = 1; i < DASH_MAX_PRIMES; i++) p += b.chunk >= A.chunk_first[i] ? 1 : 0;
+        const PrimeLds& P = s_pr[p];
+        const int64_t ch = b.chunk - (int)P.chunk_first;
+        Groups g;
+        g.src = P.in + ch * P.in_cs + (int64_t)(b.row / A.top_k) * K * 16;
+        g.dst = P.out + ch * P.out_cs + (int64_t)b.row * M * 16;
+        g.one = P.one + 16 * ch;
+        g.prime = P.p; g.magic = P.mmagic; g.pow12 = P.pow12; g.start = P.start;
+        return g;
+    };
+    // rows of no expert: the value 0 on both sides
+    auto zeros = [&](const Tile& t) __attribute__((always_inline)) {
+        const Groups z = groups_of(begin(t));
+        for (int g = wave; g < t.n_groups; g += NW) {
+            uint8_t* const dst = (uint8_t*)lane_of(z.dst, g);
+            for (int j = t.by * TL::F + lane; j < M && j < t.by * TL::F + TL::F; j += 64) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
+        }
+    };
+    // the block's next tile with an expert
+    int seq = (int)(blockIdx.x >> 3) - (int)(gridDim.x >> 3);
+    auto next_tile = [&](Tile& t) __attribute__((always_inline)) -> bool {
+        for (;;) {
+            seq += (int)(gridDim.x >> 3);
+            if (!decode(seq, t)) return false;
+            if (t.e < A.E) return true;
+            zeros(t);
+        }
+    };
+
     // ---- loads ----
-    const int nk = (K + 63) / 64;
     constexpr int kTileBytes = kMx4 ? kMx4Tile : kW8Tile;
-    const int row_tiles_ = (M + 31) / 32;
-    const uint8_t* const wexp = A.w + (int64_t)e * A.expert_bytes;
     v4i lab[GP], wgt[WT];
+    uint32_t off_w, off_s, off_l;
+    auto open = [&](const Tile& t, const Groups& g) __attribute__((always_inline)) {
+        const uint8_t* const wexp = A.w + (int64_t)t.e * A.expert_bytes;
 #pragma unroll
-    for (int i = 0; i < WT; i++) {                                  // (tiles past the last: empty buffers)
-        const int rt = by * FT + wave * WT + i;
-        wgt[i] = buffer_of(wexp + (int64_t)rt * nk * kTileBytes, rt < row_tiles_ ? (uint32_t)(nk * kTileBytes) : 0u);
-    }
+        for (int i = 0; i < WT; i++) {                              // (tiles past the last: empty buffers)
+            const int rt = t.by * FT + wave * WT + i;
+            wgt[i] = buffer_of(wexp + (int64_t)rt * nk * kTileBytes, rt < (M + 31) / 32 ? (uint32_t)(nk * kTileBytes) : 0u);
+        }
 #pragma unroll
-    for (int i = 0; i < GP; i++) {
-        const int g = wave * GP + i;
-        lab[i] = buffer_of((const uint8_t*)lane_of(g_src, g), g < n_groups ? (uint32_t)K * 16u : 0u);
-    }
+        for (int i = 0; i < GP; i++) lab[i] = buffer_of((const uint8_t*)lane_of(g.src, wave * GP + i), wave * GP + i < t.n_groups ? (uint32_t)K * 16u : 0u);
+        off_w = 16u * lane; off_s = 4u * (lane & 15) + kMx4Codes; off_l = 16u * lane;
+    };
     const uint32_t dig0 = (uint32_t)(uintptr_t)(lds_ptr)s_dig + wave * GP * 1024, raw0 = (uint32_t)(uintptr_t)(lds_ptr)s_raw + wave * WT * kRaw;
     // Stage t, the inputs from 64 t, goes into slot t % S.  Stages past the end load nothing (their offsets lie past the buffers) but count.  A
     // lane's offsets run along with the stages.
     // Words 8 .. 15 of every 16 of a group with an odd number stand before words 0 .. 7: the reads of two groups meet different banks.
-    uint32_t off_w = 16u * lane, off_s = 4u * (lane & 15) + kMx4Codes;
-    uint32_t off_l = 16u * lane;                                    // (group with an odd number: ^ 128)
     constexpr int kParts = 2 * WT + GP;                             // loads of a stage: weights, then labels
     auto load_weights = [&](auto slot, int i) __attribute__((always_inline)) {
         constexpr int kSlot = decltype(slot)::value * FT * kRaw;
@@ -187,32 +220,34 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     };
     auto load_labels = [&](auto slot, int i) __attribute__((always_inline)) {
         constexpr int kSlot = decltype(slot)::value * kDig;
-        load_lds16<kSlot, 0>(dig0 + i * 1024, lab[i], i % 2 ? off_l ^ 128u : off_l);
+        load_lds16<kSlot, 0>(dig0 + i * 1024, lab[i], i % 2 ? off_l ^ 128u : off_l);          // (groups with an odd number)
         if (i == GP - 1) off_l += 1024;
     };
 
     // ---- 4-bit weights ----
     const int h = lane >> 5, j32 = lane & 31, l16 = lane & 15;
-    if (kMx4 && tid < 256) {
-        // 2^tid mod p, times the eight magnitudes, and p minus that
-        const uint32_t prime = A.pr[pi].p, mmagic = A.pr[pi].mmagic;
-        uint32_t two = 1, sq = prime == 2 ? 0 : 2;
+    auto make_table = [&](int pi) __attribute__((always_inline)) {
+        if (kMx4 && tid < 256) {
+            // 2^tid mod p, times the eight magnitudes, and p minus that
+            const uint32_t prime = A.pr[pi].p, mmagic = A.pr[pi].mmagic;
+            uint32_t two = 1, sq = prime == 2 ? 0 : 2;
 #pragma unroll
-        for (int b = 0; b < 8; b++) {
-            const uint32_t t = two * sq;
-            if (tid >> b & 1) two = t - mul24(mulhi(t, mmagic), prime);
-            sq *= sq; sq -= mul24(mulhi(sq, mmagic), prime);
-        }
-        uint32_t w[4] = {0, 0, 0, 0};
+            for (int b = 0; b < 8; b++) {
+                const uint32_t t = two * sq;
+                if (tid >> b & 1) two = t - mul24(mulhi(t, mmagic), prime);
+                sq *= sq; sq -= mul24(mulhi(sq, mmagic), prime);
+            }
+            uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int m = 0; m < 8; m++) {
-            uint32_t r = two * (uint32_t)(m < 4 ? m : m == 7 ? 12 : 2 * m - 4);
-            r -= mul24(mulhi(r, mmagic), prime);
-            w[m / 4] |= r << (8 * (m % 4));
-            w[2 + m / 4] |= (r ? prime - r : 0) << (8 * (m % 4));
+            for (int m = 0; m < 8; m++) {
+                uint32_t r = two * (uint32_t)(m < 4 ? m : m == 7 ? 12 : 2 * m - 4);
+                r -= mul24(mulhi(r, mmagic), prime);
+                w[m / 4] |= r << (8 * (m % 4));
+                w[2 + m / 4] |= (r ? prime - r : 0) << (8 * (m % 4));
+            }
+            s_lut[tid] = u32x4{w[0], w[1], w[2], w[3]};
         }
-        s_lut[tid] = u32x4{w[0], w[1], w[2], w[3]};
-    }
+    };
     // A lane's 16 bytes of codes are 16 weights of a row's first block of 32 and 16 of its second (low and high halves of the bytes); shifts of
     // both blocks, table entries of both, then four weights at a time as bytes.
     // In registers (a wave's weights are its own: kDirect): lane (j32, h) holds what it multiplies, two stages in the making.
@@ -291,14 +326,46 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     constexpr integral_constant<int, 1> k1{};
     static_assert(S % 2 == 0, "parities of stages follow from their slots");
     constexpr int kAhead = kMx4 ? S - 3 : S - 2;
-    // dn: the wave's tiles of 32 digits that hold groups
+    auto fill = [&](auto self, auto u) __attribute__((always_inline)) -> void {
+        constexpr int U = decltype(u)::value;
+        if constexpr (U < S) {
+#pragma unroll
+            for (int i = 0; i < 2 * WT; i++) load_weights(u, i);
+            if constexpr (U < S - 1) {
+#pragma unroll
+                for (int i = 0; i < GP; i++) load_labels(u, i);
+                self(self, integral_constant<int, U + 1>{});
+            }
+        }
+    };
+    Tile tile;
+    Groups g;
+    bool more = true;
+    // Products and results of the tile whose first loads are out; before the results, the first loads of the block's next tile.  dn: the wave's
+    // tiles of 32 digits that hold groups
     auto work = [&](auto dn) __attribute__((always_inline)) {
         constexpr int kProducts = dn * FB, kReads = FB + 2 * dn, kSlots = kProducts > 4 ? kProducts : 4;
+        Tile next = tile;
+        Begun begun = {0, 0};
+        make_table(tile.pi);        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
+        more = TL::PERSIST && next_tile(next);
+        if (more) begun = begin(next);
+        wait_loads<(kMx4 ? S - 2 : S - 1) * kParts - GP>();         // stage 0, 4-bit: stage 1 too; the labels of stage S - 1 are not out yet
+        lds_barrier();
+        if constexpr (kMx4 && !kDirect) {
+            fetch_codes(k0, 0);
+            fetch_table(0); fetch_table(1);
+#pragma unroll
+            for (int i = 0; i < kSteps; i++) expand(0, i);
+            lds_barrier();
+        }
+        int zero = 0;
+        asm volatile("" : "+s"(zero));          // (known zeros make the compiler keep a second set of sums)
         v16i acc[dn][FB];
 #pragma unroll
         for (int d = 0; d < dn; d++) {
             const int g0 = (wd * DA + d) * 2;
-            const int s0 = kMx4 ? 0 : (int)lane_of(g_start, g0), s1 = kMx4 ? 0 : (int)lane_of(g_start, g0 + 1);
+            const int s0 = kMx4 ? zero : (int)lane_of(g.start, g0), s1 = kMx4 ? zero : (int)lane_of(g.start, g0 + 1);
 #pragma unroll
             for (int f = 0; f < FB; f++)
 #pragma unroll
@@ -374,35 +441,45 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
             while (stage(k0) && stage(k1)) {}
         }
         wait_loads<0>();
+        const Tile done = tile;
+        const Groups gd = g;
+        if (more) {
+            lds_barrier();          // (the slots and the table are free)
+            g = groups_of(begun);
+            tile = next;
+            open(tile, g);
+            fill(fill, k0);
+        }
+
         // ---- reduction mod p, 16 bytes a lane ----
         // (plain: no bias, every sum takes one multiplication; the common case, without branches)
         auto finish = [&](auto plain) __attribute__((always_inline)) {
 #pragma unroll
             for (int d = 0; d < dn; d++) {
                 const int g0 = (wd * DA + d) * 2;
-                if (g0 >= n_groups) break;
-                const uint64_t dst0 = lane_of(g_dst, g0), dst1 = lane_of(g_dst, g0 + 1);
+                if (g0 >= done.n_groups) break;
+                const uint64_t dst0 = lane_of(gd.dst, g0), dst1 = lane_of(gd.dst, g0 + 1);
                 uint8_t* const dst = (uint8_t*)(h ? dst1 : dst0);
-                const bool valid = g0 + h < n_groups;
+                const bool valid = g0 + h < done.n_groups;
 #pragma unroll
                 for (int f = 0; f < FB; f++) {
-                    const int j = by * TL::F + (wf * FB + f) * 32 + j32;
+                    const int j = done.by * TL::F + (wf * FB + f) * 32 + j32;
                     uint32_t w[4];          // digits 4 h .. and 8 + 4 h .. of the first group, of the second
 #pragma unroll
                     for (int g = 0; g < 2; g++) {
-                        const uint32_t prime = lane_of(g_prime, g0 + g), mmagic = lane_of(g_magic, g0 + g);
+                        const uint32_t prime = lane_of(gd.prime, g0 + g), mmagic = lane_of(gd.magic, g0 + g);
                         auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - __umul24(mulhi(v, mmagic), prime); };
                         uint32_t v[8];
 #pragma unroll
                         for (int r = 0; r < 8; r++) v[r] = (uint32_t)acc[d][f][8 * g + r];
                         if constexpr (!plain) {
-                            const uint32_t pow12 = lane_of(g_pow12, g0 + g);
+                            const uint32_t pow12 = lane_of(gd.pow12, g0 + g);
 #pragma unroll
                             for (int r = 0; r < 8; r++) v[r] = __umul24(red1(v[r] >> 12), pow12) + (v[r] & 4095u);
                             if (A.bias) {
-                                const int32_t b = j < M ? A.bias[(int64_t)e * M + j] % (int32_t)prime : 0;
+                                const int32_t b = j < M ? A.bias[(int64_t)done.e * M + j] % (int32_t)prime : 0;
                                 const uint32_t bm = (uint32_t)(b < 0 ? b + (int32_t)prime : b);
-                                const uint32_t* const one = (const uint32_t*)lane_of(g_one, g0 + g);
+                                const uint32_t* const one = (const uint32_t*)lane_of(gd.one, g0 + g);
 #pragma unroll
                                 for (int r = 0; r < 8; r++) v[r] = red1(v[r]) + __umul24(bm, (one[2 * (r / 4) + h] >> (8 * (r % 4))) & 0xffu);
                             }
@@ -419,34 +496,18 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         };
         if (A.plain) finish(k1); else finish(k0);
     };
-    auto fill = [&](auto self, auto u) __attribute__((always_inline)) -> void {
-        constexpr int U = decltype(u)::value;
-        if constexpr (U < S) {
-#pragma unroll
-            for (int i = 0; i < 2 * WT; i++) load_weights(u, i);
-            if constexpr (U < S - 1) {
-#pragma unroll
-                for (int i = 0; i < GP; i++) load_labels(u, i);
-                self(self, integral_constant<int, U + 1>{});
-            }
-        }
-    };
+    __syncthreads();
+    if (!next_tile(tile)) return;
+    g = groups_of(begin(tile));
+    open(tile, g);
     fill(fill, k0);
-    wait_loads<(kMx4 ? S - 2 : S - 1) * kParts - GP>();             // stage 0, 4-bit: stage 1 too; the labels of stage S - 1 are not out yet
-    lds_barrier();
-    if constexpr (kMx4 && !kDirect) {
-        fetch_codes(k0, 0);
-        fetch_table(0); fetch_table(1);
-#pragma unroll
-        for (int i = 0; i < kSteps; i++) expand(0, i);
-        lds_barrier();
-    }
-    // waves whose digits lie past the tile's groups, in part or whole, leave out those products (large tiles are rarely short)
-    const int mine = ((n_groups + 1) >> 1) - wd * DA;
-    if constexpr (DA * FB > 4) work(integral_constant<int, DA>{});
-    else if (mine > 2) work(integral_constant<int, DA>{});
-    else if (mine == 2) work(integral_constant<int, 2>{});
-    else work(k1);
+    do {
+        // waves whose digits lie past the tile's groups, in part or whole, leave out those products (large tiles are rarely short)
+        const int mine = ((tile.n_groups + 1) >> 1) - wd * DA;
+        if (TL::PERSIST || mine > 2) work(integral_constant<int, DA>{});
+        else if (mine == 2) work(integral_constant<int, 2>{});
+        else work(k1);
+    } while (more);
 }
 
 int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, hipStream_t s) {
@@ -502,14 +563,14 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         const int64_t total = cols * A.row_blocks;
         if (cols * A.sty > 0x7fffffff || total > 0x7fffff00) return DASH_ESIZE;
         ProfScope ps(c->prof, DASH_PROF_LINEAR, s, macs, bytes);
-        hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3((uint32_t)((total + 7) / 8 * 8)), dim3(TL::T), 0, s, A);
+        hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3((uint32_t)(TL::PERSIST && total > kCus ? kCus : (total + 7) / 8 * 8)), dim3(TL::T), 0, s, A);
         return DASH_OK;
     };
     const int64_t blocks_big = groups / EBig::G * ((L.M + EBig::F - 1) / EBig::F);
     const bool big = c->experts_tile ? c->experts_tile == 1 : blocks_big >= 256;
     const std::integral_constant<int, DASH_W8> w8{};
     const std::integral_constant<int, DASH_MX4> mx4{};
-    const int st = L.format == DASH_MX4 ? (big ? launch(EBig{}, mx4) : launch(ENarrow4{}, mx4)) : (big ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
+    const int st = L.format == DASH_MX4 ? (big ? launch(EBig4{}, mx4) : launch(ENarrow4{}, mx4)) : (big ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
     if (st) return st;
     DASH_HIP(hipGetLastError());
     return DASH_OK;
