@@ -23,8 +23,8 @@ __host__ __device__ inline int w8_at(int row, int col) { return 64 * row + 16 * 
 // `groups` consecutive ones of one expert (byte weights: the operand is the same for every prime) or of one expert and prime (4-bit weights);
 // tiles are sorted by expert and first group.
 struct TileKind { int groups; bool one_prime; };
-constexpr int kTileKinds = 4;
-constexpr TileKind kTileKind[kTileKinds] = {{16, false}, {8, false}, {16, true}, {8, true}};
+constexpr int kTileKinds = 5;
+constexpr TileKind kTileKind[kTileKinds] = {{16, false}, {8, false}, {16, true}, {8, true}, {4, true}};
 struct RouteTile {          // (read as a uint4)
     uint32_t expert_prime;  // expert (n_experts: none) | index of the prime << 24 (one_prime; else 0)
     int32_t start, count;   // the expert's rows: rows[start .. start + count - 1]

@@ -33,22 +33,24 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 typedef __attribute__((address_space(3))) v2i* lds_v2i;
 
-// WD x WF waves (along digits, along features), a wave DA x FB tiles of 32 digits x 32 features; S stages of 64 inputs in LDS; WPE: waves
-// per SIMD that the registers are held to; KIND: tiles of the routing (byte weights; + 2: 4-bit)
-template <int WD_, int WF_, int DA_, int FB_, int S_, int WPE_, int KIND_, bool PERSIST_>
+// WK sets of WD x WF waves (along the inputs; along digits, along features), a wave DA x FB tiles of 32 digits x 32 features; S stages of 64
+// inputs in LDS for each set; KIND: tiles of the routing; PERSIST: a block takes tile after tile (one block per CU)
+template <int WK_, int WD_, int WF_, int DA_, int FB_, int S_, int KIND_, bool PERSIST_>
 struct ETile {
-    static constexpr int WD = WD_, WF = WF_, DA = DA_, FB = FB_, S = S_, WPE = WPE_, KIND = KIND_;
-    static constexpr bool PERSIST = PERSIST_;        // a block takes tile after tile (one block per CU)
-    static constexpr int NW = WD * WF, T = 64 * NW;
+    static constexpr int WK = WK_, WD = WD_, WF = WF_, DA = DA_, FB = FB_, S = S_, KIND = KIND_;
+    static constexpr bool PERSIST = PERSIST_;
+    static constexpr int NW = WD * WF, T = 64 * NW * WK;
     static constexpr int G = 2 * WD * DA;            // groups per block
     static constexpr int FT = WF * FB, F = 32 * FT;  // feature tiles, features per block
     static constexpr int GP = G / NW, WT = FT / NW;  // groups and tiles of weights that a wave loads
     static_assert(G == kTileKind[KIND].groups && GP * NW == G && WT * NW == FT, "loader roles");
+    static_assert(!PERSIST || WK == 1, "the sets' sums go through the slots");
 };
-typedef ETile<2, 4, 4, 2, 4, 2, 0, true> EBig;       // 256 digits x 256 features
-typedef ETile<2, 4, 4, 2, 4, 2, 0, false> EBig4;     // the same for 4-bit weights (the registers do not hold a next tile beside them)
-typedef ETile<2, 2, 2, 2, 4, 2, 1, false> ENarrow;   // 128 digits x 128 features
-typedef ETile<1, 4, 4, 1, 4, 2, 1, false> ENarrow4;  // the same for 4-bit weights
+typedef ETile<1, 2, 4, 4, 2, 4, 0, true> EBig;       // 256 digits x 256 features
+typedef ETile<1, 2, 4, 4, 2, 4, 2, false> EBig4;     // the same for 4-bit weights (the registers do not hold a next tile beside them)
+typedef ETile<1, 2, 2, 2, 2, 4, 1, false> ENarrow;   // 128 digits x 128 features
+typedef ETile<1, 1, 4, 4, 1, 4, 3, false> ENarrow4;  // the same for 4-bit weights
+typedef ETile<2, 1, 4, 2, 1, 4, 4, false> EFew4;     // 64 digits x 128 features by two sets of waves, 4-bit weights
 
 constexpr int kCus = 256;       // (a multiple of the 8 XCDs)
 
@@ -97,12 +99,12 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 // at most N loads of the wave outstanding
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 template <int FMT, class TL>
-__global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A) {
-    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW;
+__global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
+    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW, WK = TL::WK;
     constexpr bool kMx4 = FMT == DASH_MX4;
     constexpr bool kDirect = kMx4 && TL::WD == 1;       // a wave's weights are its own: expanded in registers
     const int M = A.M, K = A.K, nk = (K + 63) / 64;
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int tid = threadIdx.x, lane = tid & 63, wave_ = __builtin_amdgcn_readfirstlane(tid >> 6), ws = wave_ / NW, wave = wave_ % NW;
     const int wd = wave / TL::WF, wf = wave % TL::WF;
 
     // ---- block -> tiles ----
@@ -137,8 +139,10 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     constexpr int kDig = G * 1024, kRaw = kMx4 ? 1280 : 2048;       // bytes of a stage's labels; of a stage's weights per feature tile, as loaded
     constexpr int kExp = kMx4 && !kDirect ? FT * 2048 : 0;          // 4-bit: bytes of an expanded stage
     // one array: its address goes into the loads, so that the compiler takes all of it to change at their waits and barriers
-    __shared__ __attribute__((aligned(1024))) uint8_t smem[S * kDig + S * FT * kRaw + 2 * kExp];
-    uint8_t* const s_dig = smem;
+    constexpr int kSet = S * kDig + S * FT * kRaw + 2 * kExp;       // of a set of waves
+    __shared__ __attribute__((aligned(1024))) uint8_t smem[WK * kSet];
+    static_assert((WK - 1) * NW * DA * FB * 4096 <= WK * kSet, "the sums of the sets are added up in it");
+    uint8_t* const s_dig = smem + ws * kSet;
     uint8_t* const s_raw = s_dig + S * kDig;
     uint8_t* const s_exp = s_raw + S * FT * kRaw;
     __shared__ u32x4 s_lut[kMx4 ? 256 : 1];
@@ -174,7 +178,7 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     // rows of no expert: the value 0 on both sides
     auto zeros = [&](const Tile& t) __attribute__((always_inline)) {
         const Groups z = groups_of(begin(t));
-        for (int g = wave; g < t.n_groups; g += NW) {
+        for (int g = wave_; g < t.n_groups; g += NW * WK) {
             uint8_t* const dst = (uint8_t*)lane_of(z.dst, g);
             for (int j = t.by * TL::F + lane; j < M && j < t.by * TL::F + TL::F; j += 64) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
         }
@@ -203,10 +207,10 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         }
 #pragma unroll
         for (int i = 0; i < GP; i++) lab[i] = buffer_of((const uint8_t*)lane_of(g.src, wave * GP + i), wave * GP + i < t.n_groups ? (uint32_t)K * 16u : 0u);
-        off_w = 16u * lane; off_s = 4u * (lane & 15) + kMx4Codes; off_l = 16u * lane;
+        off_w = 16u * lane + ws * kTileBytes; off_s = 4u * (lane & 15) + kMx4Codes + ws * kTileBytes; off_l = (16u * lane ^ (GP % 2 ? (wave & 1) * 128u : 0u)) + ws * 1024;
     };
     const uint32_t dig0 = (uint32_t)(uintptr_t)(lds_ptr)s_dig + wave * GP * 1024, raw0 = (uint32_t)(uintptr_t)(lds_ptr)s_raw + wave * WT * kRaw;
-    // Stage t, the inputs from 64 t, goes into slot t % S.  Stages past the end load nothing (their offsets lie past the buffers) but count.  A
+    // A set takes every WK-th stage of 64 inputs: its stage t, the inputs from 64 (WK t + ws), goes into slot t % S.  Stages past the end load nothing (their offsets lie past the buffers) but count.  A
     // lane's offsets run along with the stages.
     // Words 8 .. 15 of every 16 of a group with an odd number stand before words 0 .. 7: the reads of two groups meet different banks.
     constexpr int kParts = 2 * WT + GP;                             // loads of a stage: weights, then labels
@@ -216,12 +220,12 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         if (i % 2 == 0) load_lds16<kSlot, 0>(to, wgt[i / 2], off_w);
         else if constexpr (kMx4) load_lds4<kSlot + kMx4Codes>(to, wgt[i / 2], off_s);
         else load_lds16<kSlot, 1024>(to, wgt[i / 2], off_w);
-        if (i == 2 * WT - 1) { off_w += kTileBytes; off_s += kTileBytes; }
+        if (i == 2 * WT - 1) { off_w += WK * kTileBytes; off_s += WK * kTileBytes; }
     };
     auto load_labels = [&](auto slot, int i) __attribute__((always_inline)) {
         constexpr int kSlot = decltype(slot)::value * kDig;
-        load_lds16<kSlot, 0>(dig0 + i * 1024, lab[i], i % 2 ? off_l ^ 128u : off_l);          // (groups with an odd number)
-        if (i == GP - 1) off_l += 1024;
+        load_lds16<kSlot, 0>(dig0 + i * 1024, lab[i], i % 2 ? off_l ^ 128u : off_l);          // (the wave's second group has an odd number; with one group a wave, see open)
+        if (i == GP - 1) off_l += WK * 1024;
     };
 
     // ---- 4-bit weights ----
@@ -365,7 +369,7 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
 #pragma unroll
         for (int d = 0; d < dn; d++) {
             const int g0 = (wd * DA + d) * 2;
-            const int s0 = kMx4 ? zero : (int)lane_of(g.start, g0), s1 = kMx4 ? zero : (int)lane_of(g.start, g0 + 1);
+            const int s0 = kMx4 || ws ? zero : (int)lane_of(g.start, g0), s1 = kMx4 || ws ? zero : (int)lane_of(g.start, g0 + 1);
 #pragma unroll
             for (int f = 0; f < FB; f++)
 #pragma unroll
@@ -377,14 +381,14 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
             acc[d][f] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a, o.b[f], acc[d][f], 0, 0, 0);
         };
         Operands o0, o1;
-        auto half = [&](const Operands& now, Operands& next, auto u, auto second) __attribute__((always_inline)) {
+        auto half = [&](const Operands& now, Operands& next, bool there, auto u, auto second) __attribute__((always_inline)) {
             constexpr int U = decltype(u)::value, kHalf = decltype(second)::value, kLoads = kHalf ? 2 * WT : GP;
             constexpr integral_constant<int, (U + 1) % S> u1{};
             constexpr integral_constant<int, (U + 2) % S> u2{};
             constexpr integral_constant<int, (U + S - 1) % S> before{};
 #pragma unroll
             for (int m = 0; m < kSlots; m++) {
-                if (m < kProducts) multiply(now, m);
+                if (m < kProducts && there) multiply(now, m);
 #pragma unroll
                 for (int i = 0; i < kReads; i++)
                     if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) { if constexpr (kHalf) read(next, u1, 0, i); else read(next, u, 1, i); }
@@ -415,11 +419,12 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
         int t = 0;
         // one stage in slot u; false: it was the last
         auto stage = [&](auto u) __attribute__((always_inline)) -> bool {
-            half(o0, o1, u, k0);
+            const bool there = WK == 1 || WK * t + ws < nk;         // (the last round may be short of a stage for some sets)
+            half(o0, o1, there, u, k0);
             wait_loads<kAhead * kParts>();
             lds_barrier();
-            half(o1, o0, u, k1);
-            return ++t < nk;
+            half(o1, o0, there, u, k1);
+            return ++t < (nk + WK - 1) / WK;
         };
 #pragma unroll
         for (int i = 0; i < kReads; i++) read(o0, k0, 0, i);
@@ -441,6 +446,31 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
             while (stage(k0) && stage(k1)) {}
         }
         wait_loads<0>();
+        if constexpr (WK > 1) {
+            // the sums of the other sets come through LDS
+            lds_barrier();
+            u32x4* const part = (u32x4*)smem + wave * DA * FB * 256 + lane;
+#pragma unroll
+            for (int s = 1; s < WK; s++) {
+                if (ws == s) {
+#pragma unroll
+                    for (int i = 0; i < dn * FB * 4; i++) {
+                        const v16i& v = acc[i / 4 / FB][i / 4 % FB];
+                        part[((s - 1) * NW * DA * FB * 4 + i) * 64] = u32x4{(uint32_t)v[i % 4 * 4], (uint32_t)v[i % 4 * 4 + 1], (uint32_t)v[i % 4 * 4 + 2], (uint32_t)v[i % 4 * 4 + 3]};
+                    }
+                }
+            }
+            lds_barrier();
+            if (ws) return;
+#pragma unroll
+            for (int s = 1; s < WK; s++)
+#pragma unroll
+                for (int i = 0; i < dn * FB * 4; i++) {
+                    const u32x4 v = part[((s - 1) * NW * DA * FB * 4 + i) * 64];
+#pragma unroll
+                    for (int r = 0; r < 4; r++) acc[i / 4 / FB][i / 4 % FB][i % 4 * 4 + r] += (int)v[r];
+                }
+        }
         const Tile done = tile;
         const Groups gd = g;
         if (more) {
@@ -504,8 +534,8 @@ __global__ __launch_bounds__(TL::T, TL::WPE) void k_experts_mfma(const ExpArgs A
     do {
         // waves whose digits lie past the tile's groups, in part or whole, leave out those products (large tiles are rarely short)
         const int mine = ((tile.n_groups + 1) >> 1) - wd * DA;
-        if (TL::PERSIST || mine > 2) work(integral_constant<int, DA>{});
-        else if (mine == 2) work(integral_constant<int, 2>{});
+        if (TL::PERSIST || mine > 2 || (DA == 2 && mine == 2)) work(integral_constant<int, DA>{});
+        else if (DA > 2 && mine == 2) work(integral_constant<int, 2>{});
         else work(k1);
     } while (more);
 }
@@ -547,7 +577,8 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         constexpr bool mx4 = decltype(fmt)::value == DASH_MX4;
         int64_t cols = 0;
         if (L.routing) {
-            const int s = TL::KIND + (mx4 ? 2 : 0);
+            constexpr int s = TL::KIND;
+            static_assert(kTileKind[s].one_prime == mx4, "tiles of the format");
             cols = L.routing->max_tiles[s];
             A.rows = L.routing->rows; A.tiles = L.routing->tiles[s]; A.n_tiles = L.routing->first_tile[s] + L.E + 1;
         } else if (mx4)
@@ -567,10 +598,11 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         return DASH_OK;
     };
     const int64_t blocks_big = groups / EBig::G * ((L.M + EBig::F - 1) / EBig::F);
-    const bool big = c->experts_tile ? c->experts_tile == 1 : blocks_big >= 256;
+    const int tile = c->experts_tile ? c->experts_tile : blocks_big >= 256 ? 1 : 2;
     const std::integral_constant<int, DASH_W8> w8{};
     const std::integral_constant<int, DASH_MX4> mx4{};
-    const int st = L.format == DASH_MX4 ? (big ? launch(EBig4{}, mx4) : launch(ENarrow4{}, mx4)) : (big ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
+    const int st = L.format == DASH_MX4 ? (tile == 1 ? launch(EBig4{}, mx4) : tile == 3 ? launch(EFew4{}, mx4) : launch(ENarrow4{}, mx4))
+                                        : (tile == 1 ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
     if (st) return st;
     DASH_HIP(hipGetLastError());
     return DASH_OK;
