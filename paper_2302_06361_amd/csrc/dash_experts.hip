@@ -120,8 +120,10 @@ __global__ __launch_bounds__(kThreads) void k_weights8_prepare(const PrepArgs8 A
     uint32_t v[4] = {0, 0, 0, 0};
     if (row < A.M) {
         const int8_t* src = A.w + e * A.expert_stride + row * A.row_stride + col;
-        for (int i = 0; i < 16; i++)
-            if (col + i < A.K) v[i / 4] |= (uint32_t)(uint8_t)src[i] << (8 * (i % 4));
+        if (col + 16 <= A.K) __builtin_memcpy(v, src, 16);          // (at any address)
+        else
+            for (int i = 0; i < 16; i++)
+                if (col + i < A.K) v[i / 4] |= (uint32_t)(uint8_t)src[i] << (8 * (i % 4));
     }
     *(uint4*)(A.out + tile * kW8Tile + w8_at(r, 16 * q)) = make_uint4(v[0], v[1], v[2], v[3]);
 }
@@ -313,7 +315,7 @@ int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labe
     if (!L->weights || ((uintptr_t)L->weights & 15) || (L->weight_format != DASH_W8 && L->weight_format != DASH_MX4)) return DASH_EINVAL;
     const int64_t n = L->n_elem, T = n / L->top_k;
     const int M = L->out_c, K = L->in_c, E = L->n_experts;
-    if (T > 0x7fffffff / K || n > 0x7fffffff / M) return DASH_ESIZE;
+    if (T > 0x7fffffff / K || n > 0x7fffffff / M || K > 1 << 26) return DASH_ESIZE;        // (offsets inside a row of weights or a row's labels: 32 bits)
     if (L->routing) {
         if (!L->routing->data || L->routing->ctx != c || L->routing->n != n || L->routing->n_experts != E) return DASH_EINVAL;
     } else if (E != 1) return DASH_EINVAL;

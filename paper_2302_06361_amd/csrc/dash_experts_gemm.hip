@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "dash_experts.h"
+#include "dash_experts_rule.h"
 
 #pragma clang diagnostic ignored "-Winline-asm"       // (m0 as a clobber)
 
@@ -597,12 +598,13 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3((uint32_t)(TL::PERSIST && total > kCus ? kCus : (total + 7) / 8 * 8)), dim3(TL::T), 0, s, A);
         return DASH_OK;
     };
-    const int64_t blocks_big = groups / EBig::G * ((L.M + EBig::F - 1) / EBig::F);
-    const int tile = c->experts_tile ? c->experts_tile : blocks_big >= 256 ? 1 : 2;
+    ExpertsShape shape{L.n, L.E, L.M, L.K, L.format == DASH_MX4, c->k, {}};
+    for (int i = 0; i < c->k; i++) shape.chunks[i] = A.chunk_first[i + 1] - A.chunk_first[i];
+    const ExpertsTile tile = experts_tile(c->experts_tile, shape);
     const std::integral_constant<int, DASH_W8> w8{};
     const std::integral_constant<int, DASH_MX4> mx4{};
-    const int st = L.format == DASH_MX4 ? (tile == 1 ? launch(EBig4{}, mx4) : tile == 3 ? launch(EFew4{}, mx4) : launch(ENarrow4{}, mx4))
-                                        : (tile == 1 ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
+    const int st = L.format == DASH_MX4 ? (tile == EXPERTS_BIG ? launch(EBig4{}, mx4) : tile == EXPERTS_FEW ? launch(EFew4{}, mx4) : launch(ENarrow4{}, mx4))
+                                        : (tile == EXPERTS_BIG ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
     if (st) return st;
     DASH_HIP(hipGetLastError());
     return DASH_OK;

@@ -1,0 +1,63 @@
+// dash_experts_rule.h -- which tile the products of an expert layer take, as a function of its sizes alone (host code)
+#pragma once
+#include <stdint.h>
+
+namespace dash {
+
+// 256 digits x 256 features a block; 128 x 128; 64 x 128 with the inputs dealt out to two sets of waves (4-bit weights)
+enum ExpertsTile { EXPERTS_BY_SIZE = 0, EXPERTS_BIG = 1, EXPERTS_NARROW = 2, EXPERTS_FEW = 3 };
+
+struct ExpertsShape {
+    int64_t rows;           // of all experts
+    int experts, M, K;
+    bool mx4;
+    int k;                  // primes, and the 16-digit chunks of their labels
+    int chunks[16];
+};
+// Rows are taken to be spread evenly over the experts (the host does not see the routing).  A group is a chunk of a row.
+inline double experts_groups(const ExpertsShape& S, double* busy) {
+    *busy = S.rows < S.experts ? (double)S.rows : (double)S.experts;
+    double c = 0;
+    for (int i = 0; i < S.k; i++) c += S.chunks[i];
+    return c * (double)S.rows / *busy;
+}
+// tiles of `groups` groups an expert makes: across primes for byte weights, for every prime for 4-bit weights
+inline double experts_tiles(const ExpertsShape& S, int groups) {
+    double busy, t = 0;
+    const double all = experts_groups(S, &busy);
+    auto up = [&](double g) { const double q = g / groups; const int64_t f = (int64_t)q; return (double)(f + (q - (double)f > 1e-9 ? 1 : 0)); };
+    if (!S.mx4) t = up(all);
+    else for (int i = 0; i < S.k; i++) t += up(S.chunks[i] * (double)S.rows / busy);
+    return t * busy;
+}
+// Time in us: a launch, and on the fullest CU what a block takes beside its stages of 64 inputs, and the stages, at the rate of one block's
+// latency or of what shares the CU.  From runs over 15 layers (rows x K -> M; measured us: big, narrow, few):
+//   bytes  1 x 4096 -> 4096: 37, 16.  4: 41, 43.  16: 138, 141.  128: 966, 1249.  1 x 784 -> 128, 8 primes: 12, 5.9.  16 rows, 8 experts, 400 -> 120:
+//          10, 5.3.  256 rows, 32 experts, 1024 -> 2048: 336, 378.  64 rows, 64 experts, 1024 -> 1024: 51, 50.  256 x 2048 -> 64: 74, 59.
+//          200 rows, 8 experts, 100 -> 1500: 60, 86.
+//   4-bit  43, 27, 26.  47, 50, 60.  149, 159, 222.  1030, 1290, 2000.  13, 7.9, 7.1.  11, 6.6, 6.3.  420, 448, 687.  110, 81, 103.  87, 65, 79.
+//          81, 94, 178.
+inline double experts_us(const ExpertsShape& S, ExpertsTile tile) {
+    const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_NARROW ? 8 : 4, features = tile == EXPERTS_BIG ? 256 : 128, resident = tile == EXPERTS_BIG ? 1 : 2;
+    double block, latency, rate, busy;
+    const double tiles = experts_tiles(S, groups), fill = experts_groups(S, &busy) * busy / (tiles * groups);
+    if (!S.mx4) {
+        block = tile == EXPERTS_BIG ? 4.4 : 3.4; latency = tile == EXPERTS_BIG ? 0.46 : 0.18; rate = tile == EXPERTS_BIG ? 0.75 : 0.23;
+    } else if (tile == EXPERTS_BIG) { block = 5.0; latency = 0.60; rate = 0.75; }
+    else if (tile == EXPERTS_NARROW) { block = 1.8 + 1.8 * fill; latency = 0.28; rate = 0.14 + 0.10 * fill; }      // (products of missing groups are left out)
+    else { block = 2.6; latency = 0.18; rate = 0.165; }
+    double per_cu = tiles * (double)((S.M + features - 1) / features) / 256;
+    if (per_cu <= 4) per_cu = (double)(int64_t)(per_cu + 1 - 1e-9);
+    if (per_cu < 1) per_cu = 1;
+    const double stages = (double)(((int64_t)S.K + 63) / 64), rounds = per_cu / resident < 1 ? 1 : per_cu / resident;
+    return 2 + block * rounds + stages * (latency > rate * per_cu ? latency : rate * per_cu);
+}
+inline ExpertsTile experts_tile(int forced, const ExpertsShape& S) {
+    if (forced == EXPERTS_BIG || forced == EXPERTS_NARROW || (forced == EXPERTS_FEW && S.mx4)) return (ExpertsTile)forced;
+    const double big = experts_us(S, EXPERTS_BIG), narrow = experts_us(S, EXPERTS_NARROW);
+    ExpertsTile best = big < narrow ? EXPERTS_BIG : EXPERTS_NARROW;
+    if (S.mx4 && experts_us(S, EXPERTS_FEW) < (big < narrow ? big : narrow)) best = EXPERTS_FEW;
+    return best;
+}
+
+}  // namespace dash

@@ -80,7 +80,7 @@ struct dash_ctx {
     int linear_form;                 // form of the linear layers: 0 by layer shape, else a LinearForm (dash_linear_rule.h; tuning and test hook)
     int pack_run_log2;               // repacking of tables: a wave takes 2^this tiles at a time; -1 by their number (dash_pack_rule.h; tuning and test hook)
     int gemm_tile;                   // tile shape of the MFMA contraction: 0 by layer shape, 1 big, 2 wide (tuning and test hook)
-    int experts_tile;                // tile of the expert layers' products: 0 by rule, 1 big, 2 narrow, 3 few (tuning and test hook)
+    int experts_tile;                // tile of the expert layers' products: 0 by rule (dash_experts_rule.h), else an ExpertsTile (tuning and test hook)
 };
 
 namespace dash {
