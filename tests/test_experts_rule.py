@@ -44,6 +44,7 @@ MEASURED = [
     ((4, 1, 4096, 4096, 12), (41, 43), (47.2, 50.1, 60.2)), ((16, 1, 4096, 4096, 12), (138, 141), (148.5, 158.5, 221)),
     ((128, 1, 4096, 4096, 12), (966, 1249), (1030, 1290, 2000)), ((16, 8, 400, 120, 8), (10, 5.3), (11, 6.6, 6.3)),
     ((256, 32, 1024, 2048, 12), (336, 378), (420, 448, 687)), ((128, 16, 512, 768, 9), (43.5, 43.5), (46.7, 51.2, 82)),
+    ((64, 12, 4096, 256, 12), (57, 64), (62, 72, 83)),
     ((64, 64, 1024, 1024, 12), (51, 50), (110, 81, 103)), ((64, 16, 1024, 1024, 12), (49.5, 48.3), (62.7, 60.9, 92)),
     ((2, 1, 2048, 2048, 12), (21.3, 9.7), (26, 14.4, 16.2)), ((8, 1, 256, 4096, 8), (11.05, 11.8), (19, 14.1, 23)),
     ((256, 1, 2048, 64, 12), (74, 59), (87, 65, 79)), ((200, 8, 100, 1500, 9), (60, 86), (81, 94, 178)),
