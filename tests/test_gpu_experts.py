@@ -156,6 +156,33 @@ def test_experts_large_primes_and_extreme_values(fmt, tile):
     run_experts(context(workloads.PRIMES[:12]), fmt, 1, 1, [0] * 3, 13000, 5, 92, routed=False, top=True)
 
 
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_experts_long_reductions(fmt, tile):
+    """more than a thousand stages, an odd end"""
+    ctx = context(workloads.PRIMES[:8])
+    run_experts(ctx, fmt, 1, 1, [0, 0], 70001, 5, 99, routed=False)
+    run_experts(ctx, fmt, 2, 1, [1], 9000, 130, 100, bias=True)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_experts_many_rows_and_many_experts(fmt, tile):
+    """more experts than rows; more tiles of rows than blocks on the device; rows of no expert among them"""
+    ctx = context(workloads.PRIMES[:8])
+    g = np.random.default_rng(11)
+    run_experts(ctx, fmt, 700, 1, g.integers(0, 700, 60).tolist(), 20, 9, 101)
+    run_experts(ctx, fmt, 7, 1, g.integers(-1, 7, 4000).tolist(), 8, 3, 102, bias=True)
+    run_experts(ctx, fmt, 1, 1, [0] * 3000, 70, 2, 103, routed=False)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_experts_one_output_bundle_for_two_contexts_in_turn(fmt):
+    """calls of different sizes one after the other leave nothing behind for the next"""
+    a, b = context(workloads.PRIMES[:12]), context(workloads.PRIMES[:5])
+    for i, (K, M) in enumerate(((300, 260), (33, 5), (64, 129), (1, 1))):
+        run_experts(a, fmt, 3, 1, [i % 3, 2, 0], K, M, 104 + i)
+        run_experts(b, fmt, 2, 2, [1, 0], K, M, 110 + i, bias=True)
+
+
 def test_mx4_shifts_over_their_whole_range(tile):
     ctx = context(workloads.PRIMES[:12])
     run_experts(ctx, "mx4", 2, 1, [0, 1, 1, 0], 512, 64, 93, max_shift=236)
