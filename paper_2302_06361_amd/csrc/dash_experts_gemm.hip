@@ -316,7 +316,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     };
     // Stage t in two halves of 32 inputs; the operands of its first half are in registers when it starts:
     //   products of the first half  | reads of the second half's operands; loads of the labels of stage t - 1 + S
-    //   wait for the loads of stage t + 1 (4-bit: t + 2), barrier
+    //   wait for the loads of stage t + 1 (4-bit: and the weights of stage t + 2), barrier
     //   products of the second half | loads of the weights of stage t + S; reads of the first half of stage t + 1
     // The barrier stands behind all reads of stage t (each wave waits for its own) and behind the arrival of stage t + 1: slot t % S may be
     // loaded again, slot (t + 1) % S be read.
@@ -330,7 +330,8 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr integral_constant<int, 0> k0{};
     constexpr integral_constant<int, 1> k1{};
     static_assert(S % 2 == 0, "parities of stages follow from their slots");
-    constexpr int kAhead = kMx4 ? S - 3 : S - 2;
+    // loads that may be in flight at the barrier of stage t: those behind the labels of stage t + 1, 4-bit: behind the weights of stage t + 2
+    constexpr int kInFlight = kMx4 ? (S - 3) * kParts + GP : (S - 2) * kParts;
     auto fill = [&](auto self, auto u) __attribute__((always_inline)) -> void {
         constexpr int U = decltype(u)::value;
         if constexpr (U < S) {
@@ -355,7 +356,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         make_table(tile.pi);        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
         more = TL::PERSIST && next_tile(next);
         if (more) begun = begin(next);
-        wait_loads<(kMx4 ? S - 2 : S - 1) * kParts - GP>();         // stage 0, 4-bit: stage 1 too; the labels of stage S - 1 are not out yet
+        wait_loads<kMx4 ? (S - 2) * kParts : (S - 1) * kParts - GP>();      // stage 0, 4-bit: the weights of stage 1 too; the labels of stage S - 1 are not out yet
         lds_barrier();
         if constexpr (kMx4 && !kDirect) {
             fetch_codes(k0, 0);
@@ -422,7 +423,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         auto stage = [&](auto u) __attribute__((always_inline)) -> bool {
             const bool there = WK == 1 || WK * t + ws < nk;         // (the last round may be short of a stage for some sets)
             half(o0, o1, there, u, k0);
-            wait_loads<kAhead * kParts>();
+            wait_loads<kInFlight>();
             lds_barrier();
             half(o1, o0, there, u, k1);
             return ++t < (nk + WK - 1) / WK;
