@@ -66,6 +66,7 @@ def lib():
         L.dash_weights_bytes.restype = C.c_size_t
         L.dash_tables_packed_bytes.restype = C.c_size_t
         L.dash_expert_weights_bytes.restype = C.c_size_t
+        L.dash_mx4_quantise.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64] + [C.c_int] * 5 + [C.c_void_p] * 3
         L.dash_route_bytes.restype = C.c_size_t
         L.dash_ctx_destroy.restype = None
         _lib = L
@@ -89,9 +90,17 @@ def _check(st, what):
         raise DashError("%s: %s (%d)" % (what, lib().dash_strerror(st).decode(), st))
 
 
+_raw_stream = _current_device = None
+
+
 def _stream():
-    import torch
-    return C.c_void_p(torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()))
+    """the current stream of the current device"""
+    global _raw_stream, _current_device
+    if _raw_stream is None:
+        import torch
+        torch.cuda.current_device()                   # (initialises)
+        _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    return C.c_void_p(_raw_stream(_current_device()))
 
 
 class Labels:
@@ -212,6 +221,7 @@ class Context:
         n = self.L.dash_ctx_digits(self.h, buf)
         self.digits = [int(buf[j]) for j in range(n)]
         self._lam = {}
+        self._types = None
 
     def close(self):
         if getattr(self, "h", None):
@@ -285,24 +295,25 @@ class Context:
         """w [n_experts][out_c][K] (or [out_c][K]: one expert) on the context's device, rows contiguous -> the same, three-dimensional"""
         if w.dim() == 2:
             w = w[None]
-        if w.dim() != 3 or w.dtype not in dtypes or w.device != self.device or (w.shape[2] > 1 and w.stride(2) != 1) or 0 in w.shape:
+        shape, stride = w.shape, w.stride()
+        if len(shape) != 3 or w.dtype not in dtypes or w.device != self.device or (stride[2] != 1 and shape[2] > 1) or 0 in shape:
             raise DashError("%s: weights [n_experts][out_c][K] with contiguous rows on %s expected, got %s %s on %s" %
-                            (what, self.device, w.dtype, tuple(w.shape), w.device))
-        return w
+                            (what, self.device, w.dtype, tuple(shape), w.device))
+        return w, shape, stride
 
     def _expert_out(self, out, format, shape, what):
         if out is None:
             return ExpertWeights(self, format, *shape)
-        if (out.format, out.n_experts, out.out_c, out.K) != (format,) + tuple(shape):
+        if out.format != format or (out.n_experts, out.out_c, out.K) != shape:
             raise DashError("%s: `out` was made for another format or size" % what)
         return out
 
     def weights8_prepare(self, w, out=None):
         """w: int8 tensor [n_experts][out_c][K] on the device -> ExpertWeights in the W8 format"""
         import torch
-        w = self._expert_matrices(w, "weights8_prepare", (torch.int8,))
-        out = self._expert_out(out, W8, w.shape, "weights8_prepare")
-        _check(self.L.dash_weights8_prepare(self.h, C.c_void_p(w.data_ptr()), C.c_int64(w.stride(1)), C.c_int64(w.stride(0)), *w.shape,
+        w, shape, stride = self._expert_matrices(w, "weights8_prepare", (torch.int8,))
+        out = self._expert_out(out, W8, shape, "weights8_prepare")
+        _check(self.L.dash_weights8_prepare(self.h, C.c_void_p(w.data_ptr()), C.c_int64(stride[1]), C.c_int64(stride[0]), *shape,
                                             C.c_void_p(out.data.data_ptr()), _stream()), "dash_weights8_prepare")
         return out
 
@@ -311,14 +322,17 @@ class Context:
         2 * e2m1 * 2^shift in units of 2^(base - 1), shift <= max_shift.  values: contiguous tensor like w that receives the
         weights the codes stand for."""
         import torch
-        types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-        w = self._expert_matrices(w, "mx4_quantise", types)
-        out = self._expert_out(out, MX4, w.shape, "mx4_quantise")
-        if values is not None and (values.dtype != w.dtype or values.numel() != w.numel() or not values.is_contiguous() or values.device != w.device):
-            raise DashError("mx4_quantise: `values` has to be contiguous and of the size and type of the weights")
-        _check(self.L.dash_mx4_quantise(self.h, C.c_void_p(w.data_ptr()), types[w.dtype], C.c_int64(w.stride(1)), C.c_int64(w.stride(0)), *w.shape,
-                                        int(base), int(max_shift), C.c_void_p(out.data.data_ptr()),
-                                        C.c_void_p(values.data_ptr() if values is not None else 0), _stream()), "dash_mx4_quantise")
+        if self._types is None:
+            self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+        w, shape, stride = self._expert_matrices(w, "mx4_quantise", self._types)
+        out = self._expert_out(out, MX4, shape, "mx4_quantise")
+        dtype, to = w.dtype, None
+        if values is not None:
+            to = values.data_ptr()
+            if values.dtype != dtype or values.numel() != shape[0] * shape[1] * shape[2] or not values.is_contiguous() or values.device != self.device:
+                raise DashError("mx4_quantise: `values` has to be contiguous and of the size and type of the weights")
+        _check(self.L.dash_mx4_quantise(self.h, w.data_ptr(), self._types[dtype], stride[1], stride[0], *shape, base, max_shift, out.data.data_ptr(), to, _stream()),
+               "dash_mx4_quantise")
         return out
 
     def route(self, experts, n_experts, out=None):
