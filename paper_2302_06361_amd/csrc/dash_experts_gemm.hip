@@ -6,16 +6,25 @@
 // digits in 4 consecutive accumulators, so the result needs no turning around: pack 4 bytes, swap halves of the wave (2 groups a
 // tile), store 16 bytes a lane, neighbouring lanes neighbouring features.
 //
-// Loads.  Everything comes by loads that write LDS directly (global_load_lds: no registers, no LDS write instructions).  64 words of a
-// group are 1 KB in a row, one instruction; prepared weights are laid out in tiles for the same.  Labels are turned around (the MFMA
-// wants 16 consecutive inputs of one digit) by the LDS itself: ds_read_b64_tr_b8 gives lane l of 16 the byte l of 8 words.
-// A ring of S stages of 64 inputs; each wave waits for its own loads of the next stage (vmcnt counts down in order, all stages issue the
-// same number), then one barrier a stage.
+// Loads.  Everything comes by buffer loads that write LDS directly: no registers, no LDS write instructions, and what lies past the end of a
+// row of inputs or of a row of weight tiles is left out by the buffer's size.  64 words of a group are 1 KB in a row, one instruction;
+// prepared weights are laid out in tiles for the same.  Labels are turned around (the MFMA wants 16 consecutive inputs of one digit) by the
+// LDS itself: ds_read_b64_tr_b8 gives lane l of 16 the byte l of 8 words.  A ring of S stages of 64 inputs, the loop unrolled over its
+// slots; each wave waits for its own loads of the stages ahead (vmcnt counts down in order, all stages issue the same number), then
+// one barrier a stage.  (With loads through registers and byte permutes, as the dense layers have them, the same product takes
+// 1 096 us; with the slots as run-time numbers small tiles issued twice the instructions: one row, 4096 -> 4096: 40 us, now 27.)
 //
-// Weights.  Signed bytes are the operand as they are, for every prime: the sums start at a multiple of p that keeps them positive and
-// are reduced once.  4-bit floats: 2 e2m1 2^shift mod p by table: the 8 magnitudes of a shift and their negatives are 16 bytes of
-// LDS, a v_perm picks four of them by four 3-bit codes at a time; a stage's tile is expanded once a block, a stage ahead, into the
-// layout of the byte weights.
+// Weights.  Signed bytes are the operand as they are, for every prime: a tile goes across primes, the sums start at a multiple of p that
+// keeps them positive and are reduced once.  4-bit floats: 2 e2m1 2^shift mod p by table: the 8 magnitudes of a shift and their
+// negatives are 16 bytes of LDS; two v_perm pick four of each by four 3-bit codes, a third picks by the signs: 6.5 instructions for
+// four weights.  Large tiles expand a stage's weights once a block, through LDS, into the layout of the byte weights; in the others a
+// wave's weights are its own and stay in registers.
+//
+// What bounds it (us).  128 rows, 4096 -> 4096, 12 primes: 960 to 1 025 with bytes from box to box (2.3 to 2.5 POP/s counted over the label digits, 2.6 to
+// 2.8 with the zero digits of the last chunks; a library's int8 product of 16384 reaches 2.4): power, the matrix pipe is busy 76 % of the cycles and the clock falls
+// from 2.7 to 1.6 GHz.  4-bit: 1 010 to 1 030, the expansion beside it.  32 experts, 256 rows, 1024 -> 2048, 4-bit: 419; 17 us a tile, of which 6 are its
+// start and its results.  One row, 4096 -> 4096, 4-bit: 25; latency of the stages, about 110 instructions by one or two waves a SIMD.  One row, 784 -> 128, 4-bit: 7.1,
+// 4.8 of them for a single stage: launch, the chain of loads to the first labels, results.
 #include <string.h>
 
 #include <type_traits>
@@ -48,7 +57,7 @@ struct ETile {
     static_assert(!PERSIST || WK == 1, "the sets' sums go through the slots");
 };
 typedef ETile<1, 2, 4, 4, 2, 4, 0, true> EBig;       // 256 digits x 256 features
-typedef ETile<1, 2, 4, 4, 2, 4, 2, false> EBig4;     // the same for 4-bit weights (the registers do not hold a next tile beside them)
+typedef ETile<1, 2, 4, 4, 2, 4, 2, false> EBig4;     // the same for 4-bit weights (tile after tile: 2 % at 16 stages, but 8 % lost at two)
 typedef ETile<1, 2, 2, 2, 2, 4, 1, false> ENarrow;   // 128 digits x 128 features
 typedef ETile<1, 1, 4, 4, 1, 4, 3, false> ENarrow4;  // the same for 4-bit weights
 typedef ETile<2, 1, 4, 2, 1, 4, 4, false> EFew4;     // 64 digits x 128 features by two sets of waves, 4-bit weights
