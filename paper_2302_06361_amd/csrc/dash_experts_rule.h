@@ -31,21 +31,21 @@ inline double experts_tiles(const ExpertsShape& S, int groups) {
     return t * busy;
 }
 // Time in us: a launch, and on the fullest CU what a block takes beside its stages of 64 inputs, and the stages, at the rate of one block's
-// latency or of what shares the CU.  From runs over 15 layers (rows x K -> M; measured us: big, narrow, few):
+// latency or of what shares the CU.  From runs over 18 layers (rows x K -> M; measured us: big, narrow, few):
 //   bytes  1 x 4096 -> 4096: 37, 16.  4: 41, 43.  16: 138, 141.  128: 966, 1249.  1 x 784 -> 128, 8 primes: 12, 5.9.  16 rows, 8 experts, 400 -> 120:
 //          10, 5.3.  256 rows, 32 experts, 1024 -> 2048: 336, 378.  64 rows, 64 experts, 1024 -> 1024: 51, 50.  256 x 2048 -> 64: 74, 59.
 //          200 rows, 8 experts, 100 -> 1500: 60, 86.  64 rows, 12 experts, 4096 -> 256, inputs not in any cache: 57, 64.
 //   4-bit  43, 27, 26.  47, 50, 60.  149, 159, 222.  1030, 1290, 2000.  13, 7.9, 7.1.  11, 6.6, 6.3.  420, 448, 687.  110, 81, 103.  87, 65, 79.
 //          81, 94, 178.  62, 72.
 inline double experts_us(const ExpertsShape& S, ExpertsTile tile) {
-    const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_NARROW ? 8 : 4, features = tile == EXPERTS_BIG ? 256 : 128, resident = tile == EXPERTS_BIG ? 1 : 2;
-    double block, latency, rate, busy;
+    const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_NARROW ? 8 : 4, features = tile == EXPERTS_BIG ? 256 : 128;
+    double block, latency, rate, busy, resident = tile == EXPERTS_BIG ? 1 : tile == EXPERTS_NARROW ? 2 : 1.3;       // (blocks that start side by side)
     const double tiles = experts_tiles(S, groups), fill = experts_groups(S, &busy) * busy / (tiles * groups);
     if (!S.mx4) {
         block = tile == EXPERTS_BIG ? 4.4 : 3.4; latency = tile == EXPERTS_BIG ? 0.46 : 0.18; rate = tile == EXPERTS_BIG ? 0.75 : 0.25;
     } else if (tile == EXPERTS_BIG) { block = 5.0; latency = 0.60; rate = 0.70; }
     else if (tile == EXPERTS_NARROW) { block = 1.8 + 1.8 * fill; latency = 0.28; rate = 0.14 + 0.115 * fill; }      // (products of missing groups are left out)
-    else { block = 2.6; latency = 0.18; rate = 0.18; }
+    else { block = 2.0 + 1.2 * fill; latency = 0.18; rate = 0.165; }
     double per_cu = tiles * (double)((S.M + features - 1) / features) / 256;
     if (per_cu <= 4) per_cu = (double)(int64_t)(per_cu + 1 - 1e-9);
     if (per_cu < 1) per_cu = 1;

@@ -47,6 +47,7 @@ MEASURED = [
     ((64, 12, 4096, 256, 12), (57, 64), (62, 72, 83)),
     ((64, 64, 1024, 1024, 12), (51, 50), (110, 81, 103)), ((64, 16, 1024, 1024, 12), (49.5, 48.3), (62.7, 60.9, 92)),
     ((2, 1, 2048, 2048, 12), (21.3, 9.7), (26, 14.4, 16.2)), ((8, 1, 256, 4096, 8), (11.05, 11.8), (19, 14.1, 23)),
+    ((39, 4, 81, 29, 12), (9, 6), (9.7, 6.5, 8.0)), ((65, 4, 228, 12, 7), (10, 6), (11.0, 7.1, 8.7)), ((12, 6, 3833, 172, 9), (47, 14), (47.5, 24.3, 19.0)),
     ((256, 1, 2048, 64, 12), (74, 59), (87, 65, 79)), ((200, 8, 100, 1500, 9), (60, 86), (81, 94, 178)),
 ]
 
