@@ -60,6 +60,7 @@ typedef ETile<1, 2, 4, 4, 2, 4, 0, true> EBig;       // 256 digits x 256 feature
 typedef ETile<1, 2, 4, 4, 2, 4, 2, false> EBig4;     // the same for 4-bit weights (tile after tile: 2 % at 16 stages, but 8 % lost at two)
 typedef ETile<1, 2, 2, 2, 2, 4, 1, false> ENarrow;   // 128 digits x 128 features
 typedef ETile<1, 1, 4, 4, 1, 4, 3, false> ENarrow4;  // the same for 4-bit weights
+typedef ETile<1, 1, 4, 4, 2, 4, 3, false> EWide4;    // 128 digits x 256 features, 4-bit weights in registers, two blocks per CU
 typedef ETile<2, 1, 4, 2, 1, 4, 4, false> EFew4;     // 64 digits x 128 features by two sets of waves, 4-bit weights
 
 constexpr int kCus = 256;       // (a multiple of the 8 XCDs)
@@ -624,7 +625,7 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
     const ExpertsTile tile = experts_tile(c->experts_tile, shape);
     const std::integral_constant<int, DASH_W8> w8{};
     const std::integral_constant<int, DASH_MX4> mx4{};
-    const int st = L.format == DASH_MX4 ? (tile == EXPERTS_BIG ? launch(EBig4{}, mx4) : tile == EXPERTS_FEW ? launch(EFew4{}, mx4) : launch(ENarrow4{}, mx4))
+    const int st = L.format == DASH_MX4 ? (tile == EXPERTS_BIG ? launch(EBig4{}, mx4) : tile == EXPERTS_FEW ? launch(EFew4{}, mx4) : tile == EXPERTS_WIDE ? launch(EWide4{}, mx4) : launch(ENarrow4{}, mx4))
                                         : (tile == EXPERTS_BIG ? launch(EBig{}, w8) : launch(ENarrow{}, w8));
     if (st) return st;
     DASH_HIP(hipGetLastError());

@@ -4,8 +4,8 @@
 
 namespace dash {
 
-// 256 digits x 256 features a block; 128 x 128; 64 x 128 with the inputs dealt out to two sets of waves (4-bit weights)
-enum ExpertsTile { EXPERTS_BY_SIZE = 0, EXPERTS_BIG = 1, EXPERTS_NARROW = 2, EXPERTS_FEW = 3 };
+// 256 digits x 256 features a block; 128 x 128; for 4-bit weights also 64 x 128 with the inputs dealt out to two sets of waves, and 128 x 256
+enum ExpertsTile { EXPERTS_BY_SIZE = 0, EXPERTS_BIG = 1, EXPERTS_NARROW = 2, EXPERTS_FEW = 3, EXPERTS_WIDE = 4 };
 
 struct ExpertsShape {
     int64_t rows;           // of all experts
@@ -38,13 +38,14 @@ inline double experts_tiles(const ExpertsShape& S, int groups) {
 //   4-bit  43, 27, 26.  47, 50, 60.  149, 159, 222.  1030, 1290, 2000.  13, 7.9, 7.1.  11, 6.6, 6.3.  420, 448, 687.  110, 81, 103.  87, 65, 79.
 //          81, 94, 178.  62, 72.
 inline double experts_us(const ExpertsShape& S, ExpertsTile tile) {
-    const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_NARROW ? 8 : 4, features = tile == EXPERTS_BIG ? 256 : 128;
-    double block, latency, rate, busy, resident = tile == EXPERTS_BIG ? 1 : tile == EXPERTS_NARROW ? 2 : 1.3;       // (blocks that start side by side)
+    const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_FEW ? 4 : 8, features = tile == EXPERTS_BIG || tile == EXPERTS_WIDE ? 256 : 128;
+    double block, latency, rate, busy, resident = tile == EXPERTS_BIG ? 1 : tile == EXPERTS_FEW ? 1.3 : 2;       // (blocks that start side by side)
     const double tiles = experts_tiles(S, groups), fill = experts_groups(S, &busy) * busy / (tiles * groups);
     if (!S.mx4) {
         block = tile == EXPERTS_BIG ? 4.4 : 3.4; latency = tile == EXPERTS_BIG ? 0.46 : 0.18; rate = tile == EXPERTS_BIG ? 0.75 : 0.25;
     } else if (tile == EXPERTS_BIG) { block = 5.0; latency = 0.60; rate = 0.70; }
     else if (tile == EXPERTS_NARROW) { block = 1.8 + 1.8 * fill; latency = 0.28; rate = 0.14 + 0.115 * fill; }      // (products of missing groups are left out)
+    else if (tile == EXPERTS_WIDE) { block = 4.4; latency = 0.43; rate = 0.38; }
     else { block = 2.0 + 1.2 * fill; latency = 0.18; rate = 0.165; }
     double per_cu = tiles * (double)((S.M + features - 1) / features) / 256;
     if (per_cu <= 4) per_cu = (double)(int64_t)(per_cu + 1 - 1e-9);
@@ -53,11 +54,11 @@ inline double experts_us(const ExpertsShape& S, ExpertsTile tile) {
     return 2 + block * rounds + stages * (latency > rate * per_cu ? latency : rate * per_cu);
 }
 inline ExpertsTile experts_tile(int forced, const ExpertsShape& S) {
-    if (forced == EXPERTS_BIG || forced == EXPERTS_NARROW || (forced == EXPERTS_FEW && S.mx4)) return (ExpertsTile)forced;
-    const double big = experts_us(S, EXPERTS_BIG), narrow = experts_us(S, EXPERTS_NARROW);
-    ExpertsTile best = big < narrow ? EXPERTS_BIG : EXPERTS_NARROW;
-    if (S.mx4 && experts_us(S, EXPERTS_FEW) < (big < narrow ? big : narrow)) best = EXPERTS_FEW;
-    return best;
+    if (forced == EXPERTS_BIG || forced == EXPERTS_NARROW || ((forced == EXPERTS_FEW || forced == EXPERTS_WIDE) && S.mx4)) return (ExpertsTile)forced;
+    int best = EXPERTS_BIG;
+    for (int t = EXPERTS_NARROW; t <= (S.mx4 ? EXPERTS_WIDE : EXPERTS_NARROW); t++)
+        if (experts_us(S, (ExpertsTile)t) < experts_us(S, (ExpertsTile)best)) best = t;
+    return (ExpertsTile)best;
 }
 
 }  // namespace dash

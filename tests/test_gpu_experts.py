@@ -79,7 +79,7 @@ def run_experts(ctx, fmt, E, top_k, route, K, M, seed, bias=False, garble=False,
 FORMATS = ["w8", "mx4"]
 
 
-@pytest.fixture(params=["rule", "big", "narrow", "few"])
+@pytest.fixture(params=["rule", "big", "narrow", "few", "wide"])
 def tile(request, monkeypatch):
     """the tile that the layer's sizes ask for, and each tile forced"""
     monkeypatch.setenv("DASH_EXPERTS_TILE", request.param)
