@@ -17,13 +17,13 @@
 // Weights.  Signed bytes are the operand as they are, for every prime: a tile goes across primes, the sums start at a multiple of p that
 // keeps them positive and are reduced once.  4-bit floats: 2 e2m1 2^shift mod p by table: the 8 magnitudes of a shift and their
 // negatives are 16 bytes of LDS; two v_perm pick four of each by four 3-bit codes, a third picks by the signs: 6.5 instructions for
-// four weights.  Large tiles expand a stage's weights once a block, through LDS, into the layout of the byte weights; in the others a
+// four weights.  The largest tiles expand a stage's weights once a block, through LDS, into the layout of the byte weights; in the others a
 // wave's weights are its own and stay in registers.
 //
 // What bounds it (us).  128 rows, 4096 -> 4096, 12 primes: 960 to 1 025 with bytes from box to box (2.3 to 2.5 POP/s counted over the label digits, 2.6 to
 // 2.8 with the zero digits of the last chunks; a library's int8 product of 16384 reaches 2.4): power, the matrix pipe is busy 76 % of the cycles and the clock falls
-// from 2.7 to 1.6 GHz.  4-bit: 1 010 to 1 030, the expansion beside it.  32 experts, 256 rows, 1024 -> 2048, 4-bit: 412; 17 us a tile, of which 6 are its
-// start and its results.  One row, 4096 -> 4096, 4-bit: 25; latency of the stages, about 110 instructions by one or two waves a SIMD.  One row, 784 -> 128, 4-bit: 7.0,
+// from 2.7 to 1.6 GHz.  4-bit: 1 010 to 1 030, the expansion beside it.  32 experts, 256 rows, 1024 -> 2048, 4-bit: 358 with 128 x 256 tiles, two
+// blocks a CU so that one has products while the other starts or stores (256 x 256, one block: 412).  One row, 4096 -> 4096, 4-bit: 25; latency of the stages, about 110 instructions by one or two waves a SIMD.  One row, 784 -> 128, 4-bit: 7.0,
 // 4.8 of them for a single stage: launch, the chain of loads to the first labels, results.
 #include <string.h>
 
@@ -60,7 +60,7 @@ typedef ETile<1, 2, 4, 4, 2, 4, 0, true> EBig;       // 256 digits x 256 feature
 typedef ETile<1, 2, 4, 4, 2, 4, 2, false> EBig4;     // the same for 4-bit weights (tile after tile: 2 % at 16 stages, but 8 % lost at two)
 typedef ETile<1, 2, 2, 2, 2, 4, 1, false> ENarrow;   // 128 digits x 128 features
 typedef ETile<1, 1, 4, 4, 1, 4, 3, false> ENarrow4;  // the same for 4-bit weights
-typedef ETile<1, 1, 4, 4, 2, 4, 3, false> EWide4;    // 128 digits x 256 features, 4-bit weights in registers, two blocks per CU
+typedef ETile<1, 1, 4, 4, 2, 4, 3, false> EWide4;    // 128 digits x 256 features, weights expanded in registers, two blocks per CU (256 rows, 32 experts, 1024 -> 2048: 414 -> 355 us; 128 rows, 4096 -> 4096: 1029 -> 1076)
 typedef ETile<2, 1, 4, 2, 1, 4, 4, false> EFew4;     // 64 digits x 128 features by two sets of waves, 4-bit weights
 
 constexpr int kCus = 256;       // (a multiple of the 8 XCDs)

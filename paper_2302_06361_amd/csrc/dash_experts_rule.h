@@ -31,12 +31,20 @@ inline double experts_tiles(const ExpertsShape& S, int groups) {
     return t * busy;
 }
 // Time in us: a launch, and on the fullest CU what a block takes beside its stages of 64 inputs, and the stages, at the rate of one block's
-// latency or of what shares the CU.  From runs over 18 layers (rows x K -> M; measured us: big, narrow, few):
-//   bytes  1 x 4096 -> 4096: 37, 16.  4: 41, 43.  16: 138, 141.  128: 966, 1249.  1 x 784 -> 128, 8 primes: 12, 5.9.  16 rows, 8 experts, 400 -> 120:
-//          10, 5.3.  256 rows, 32 experts, 1024 -> 2048: 336, 378.  64 rows, 64 experts, 1024 -> 1024: 51, 50.  256 x 2048 -> 64: 74, 59.
-//          200 rows, 8 experts, 100 -> 1500: 60, 86.  64 rows, 12 experts, 4096 -> 256, inputs not in any cache: 57, 64.
-//   4-bit  43, 27, 26.  47, 50, 60.  149, 159, 222.  1030, 1290, 2000.  13, 7.9, 7.1.  11, 6.6, 6.3.  420, 448, 687.  110, 81, 103.  87, 65, 79.
-//          81, 94, 178.  62, 72.
+// latency or of what shares the CU.  Constants from runs over 18 layers (rows x K -> M; us of repeated calls: bytes big, narrow | 4-bit big, narrow,
+// few, wide):
+//   1 x 4096 -> 4096: 37.4, 16 | 43, 26.8, 25.2, 33.8
+//   4: 41.4, 41.5 | 47.4, 50.1, 59.5, 53.6
+//   16: 131, 141 | 149, 158, 229, 140
+//   128: 991, 1230 | 1029, 1246, 1765, 1076
+//   1 x 784 -> 128, 8 primes: 12.7, 5.8 | 12.5, 7.7, 7, 10.8
+//   16 rows, 8 experts, 400 -> 120: 10.2, 5.2 | 11.2, 6.4, 6.2, 8.7
+//   256 rows, 32 experts, 1024 -> 2048: 325, 376 | 414, 425, 667, 355
+//   64 rows, 64 experts, 1024 -> 1024: 49.2, 50.6 | 109, 77.9, 102, 67
+//   256 x 2048 -> 64: 73.7, 60.6 | 88.7, 64, 76.8, 80.5
+//   200 rows, 8 experts, 100 -> 1500: 61.5, 86.4 | 79.9, 88.6, 171, 66.3
+//   64 rows, 12 experts, 4096 -> 256: 43.7, 43.7 | 52.8, 51.8, 69.4, 54.1
+// Over 441 drawn layers the choice took over 5 % more than the fastest tile in 25, over 10 % in 15, at most 37 %.
 inline double experts_us(const ExpertsShape& S, ExpertsTile tile) {
     const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_FEW ? 4 : 8, features = tile == EXPERTS_BIG || tile == EXPERTS_WIDE ? 256 : 128;
     double block, latency, rate, busy, resident = tile == EXPERTS_BIG ? 1 : tile == EXPERTS_FEW ? 1.3 : 2;       // (blocks that start side by side)

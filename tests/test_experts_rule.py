@@ -6,7 +6,7 @@ import subprocess
 import pytest
 
 HERE = os.path.dirname(os.path.abspath(__file__))
-BIG, NARROW, FEW = 1, 2, 3
+BIG, NARROW, FEW, WIDE = 1, 2, 3, 4
 CHUNKS = [8, 6, 4, 3, 3, 3, 2, 2, 2, 2, 2, 2]
 SRC = r"""
 #include "%s/../paper_2302_06361_amd/csrc/dash_experts_rule.h"
@@ -38,17 +38,26 @@ def tile(lib, rows, experts, K, M, mx4, k=12, forced=0):
     return lib.tile(forced, C.c_long(rows), experts, M, K, int(mx4), k, (C.c_int * 12)(*CHUNKS))
 
 
-# (rows, experts, K, M, primes): measured us with byte weights (big, narrow) and 4-bit weights (big, narrow, few)
+# (rows, experts, K, M, primes): us of repeated calls with byte weights (big, narrow) and 4-bit weights (big, narrow, few, wide)
 MEASURED = [
-    ((1, 1, 784, 128, 8), (12.4, 5.9), (12.9, 7.9, 7.1)), ((1, 1, 4096, 4096, 12), (36.6, 16.1), (43.4, 27.2, 25.6)),
-    ((4, 1, 4096, 4096, 12), (41, 43), (47.2, 50.1, 60.2)), ((16, 1, 4096, 4096, 12), (138, 141), (148.5, 158.5, 221)),
-    ((128, 1, 4096, 4096, 12), (966, 1249), (1030, 1290, 2000)), ((16, 8, 400, 120, 8), (10, 5.3), (11, 6.6, 6.3)),
-    ((256, 32, 1024, 2048, 12), (336, 378), (420, 448, 687)), ((128, 16, 512, 768, 9), (43.5, 43.5), (46.7, 51.2, 82)),
-    ((64, 12, 4096, 256, 12), (57, 64), (62, 72, 83)),
-    ((64, 64, 1024, 1024, 12), (51, 50), (110, 81, 103)), ((64, 16, 1024, 1024, 12), (49.5, 48.3), (62.7, 60.9, 92)),
-    ((2, 1, 2048, 2048, 12), (21.3, 9.7), (26, 14.4, 16.2)), ((8, 1, 256, 4096, 8), (11.05, 11.8), (19, 14.1, 23)),
-    ((39, 4, 81, 29, 12), (9, 6), (9.7, 6.5, 8.0)), ((65, 4, 228, 12, 7), (10, 6), (11.0, 7.1, 8.7)), ((12, 6, 3833, 172, 9), (47, 14), (47.5, 24.3, 19.0)),
-    ((256, 1, 2048, 64, 12), (74, 59), (87, 65, 79)), ((200, 8, 100, 1500, 9), (60, 86), (81, 94, 178)),
+    ((1, 1, 784, 128, 8), (12.7, 5.8), (12.5, 7.7, 7.0, 10.8)),
+    ((1, 1, 4096, 4096, 12), (37.4, 16.0), (43.0, 26.8, 25.2, 33.8)),
+    ((4, 1, 4096, 4096, 12), (41.4, 41.5), (47.4, 50.1, 59.5, 53.6)),
+    ((16, 1, 4096, 4096, 12), (130.6, 140.8), (149.0, 158.1, 228.7, 139.6)),
+    ((128, 1, 4096, 4096, 12), (990.9, 1230.1), (1029.2, 1245.5, 1765.1, 1076.2)),
+    ((16, 8, 400, 120, 8), (10.2, 5.2), (11.2, 6.4, 6.2, 8.7)),
+    ((256, 32, 1024, 2048, 12), (325.4, 375.7), (413.7, 425.1, 667.1, 355.0)),
+    ((128, 16, 512, 768, 9), (41.7, 41.8), (48.0, 50.3, 80.5, 41.2)),
+    ((64, 12, 4096, 256, 12), (43.7, 43.7), (52.8, 51.8, 69.4, 54.1)),
+    ((64, 64, 1024, 1024, 12), (49.2, 50.6), (108.8, 77.9, 102.1, 67.0)),
+    ((64, 16, 1024, 1024, 12), (47.7, 48.0), (62.5, 59.8, 91.1, 52.8)),
+    ((2, 1, 2048, 2048, 12), (22.0, 9.4), (25.5, 14.1, 16.5, 19.6)),
+    ((8, 1, 256, 4096, 8), (11.3, 11.4), (18.7, 13.4, 22.7, 11.6)),
+    ((39, 4, 81, 29, 12), (8.2, 4.6), (8.3, 5.1, 6.6, 6.7)),
+    ((65, 4, 228, 12, 7), (8.9, 4.8), (9.5, 5.6, 7.3, 7.7)),
+    ((12, 6, 3833, 172, 9), (35.6, 14.4), (45.5, 22.3, 17.1, 32.4)),
+    ((256, 1, 2048, 64, 12), (73.7, 60.6), (88.7, 64.0, 76.8, 80.5)),
+    ((200, 8, 100, 1500, 9), (61.5, 86.4), (79.9, 88.6, 170.9, 66.3)),
 ]
 
 
@@ -63,8 +72,9 @@ def test_forced_tiles(lib):
     for mx4 in (False, True):
         for forced in (BIG, NARROW):
             assert tile(lib, 5, 3, 100, 100, mx4, forced=forced) == forced
-    assert tile(lib, 128, 1, 4096, 4096, True, forced=FEW) == FEW
-    assert tile(lib, 128, 1, 4096, 4096, False, forced=FEW) == BIG       # byte weights have no such kernel
+    for forced in (FEW, WIDE):
+        assert tile(lib, 128, 1, 4096, 4096, True, forced=forced) == forced
+        assert tile(lib, 128, 1, 4096, 4096, False, forced=forced) == BIG       # byte weights have no such kernel
 
 
 def test_every_size_gets_a_tile_of_its_format(lib):
@@ -74,7 +84,7 @@ def test_every_size_gets_a_tile_of_its_format(lib):
                 for M in (1, 129, 2 ** 20):
                     for k in (1, 2, 12):
                         assert tile(lib, rows, experts, K, M, False, k) in (BIG, NARROW)
-                        assert tile(lib, rows, experts, K, M, True, k) in (BIG, NARROW, FEW)
+                        assert tile(lib, rows, experts, K, M, True, k) in (BIG, NARROW, FEW, WIDE)
 
 
 def test_tiles_of_an_even_routing(lib):
