@@ -23,7 +23,8 @@
 // What bounds it (us).  128 rows, 4096 -> 4096, 12 primes: 960 to 1 025 with bytes from box to box (2.3 to 2.5 POP/s counted over the label digits, 2.6 to
 // 2.8 with the zero digits of the last chunks; a library's int8 product of 16384 reaches 2.4): power, the matrix pipe is busy 76 % of the cycles and the clock falls
 // from 2.7 to 1.6 GHz.  4-bit: 1 010 to 1 030, the expansion beside it.  32 experts, 256 rows, 1024 -> 2048, 4-bit: 358 with 128 x 256 tiles, two
-// blocks a CU (256 x 256, one block: 412): vector instructions of the expansion in 68 % of the cycles, the matrix pipe in 41 %.  One row, 4096 -> 4096, 4-bit: 25; latency of the stages, about 110 instructions by one or two waves a SIMD.  One row, 784 -> 128, 4-bit: 7.0,
+// blocks a CU (256 x 256, one block: 412): vector instructions of the expansion in 68 % of the cycles, the matrix pipe in 41 %.  One row,
+// 4096 -> 4096, 4-bit: 25; latency of the stages, about 110 instructions by one or two waves a SIMD.  One row, 784 -> 128, 4-bit: 7.0,
 // 4.8 of them for a single stage: launch, the chain of loads to the first labels, results.
 #include <string.h>
 
