@@ -91,12 +91,14 @@ struct ExpArgs {
 };
 
 // 16 (4) bytes a lane from offset `off` + At of the buffer to LDS at `to` + Slot + At + 16 (4) * lane; a lane whose offset lies past the end of
-// the buffer reads nothing.  In flight until a wait on vmcnt; no registers.
+// the buffer reads nothing.  In flight until a wait on vmcnt; no registers.  A buffer's words that a vector instruction has written (a readfirstlane,
+// a spilled word's way back) may be read five wait states later at the earliest, and the compiler does not look after that in front of an assembly
+// block: the block brings all five, whatever stands in front of it.
 template <int Slot, int At> __device__ __forceinline__ void load_lds16(uint32_t to, const v4i& buffer, uint32_t off) {
-    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen offset:%4 lds" ::"s"(to), "v"(off), "s"(buffer), "n"(Slot), "n"(At) : "memory", "m0", "scc");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen offset:%4 lds" ::"s"(to), "v"(off), "s"(buffer), "n"(Slot), "n"(At) : "memory", "m0", "scc");
 }
 template <int Slot> __device__ __forceinline__ void load_lds4(uint32_t to, const v4i& buffer, uint32_t off) {
-    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer), "n"(Slot) : "memory", "m0", "scc");
+    asm volatile("s_add_u32 m0, %0, %3\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(to), "v"(off), "s"(buffer), "n"(Slot) : "memory", "m0", "scc");
 }
 // a buffer of `bytes` bytes without a format (raw, stride 0)
 __device__ __forceinline__ v4i buffer_of(const uint8_t* p, uint32_t bytes) {
