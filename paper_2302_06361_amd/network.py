@@ -34,22 +34,22 @@ def build_layers(ctx, net, b, batch_base):
         elif kind == "experts":
             # rows of a batch element, each through the matrix of its (public) expert
             if L.get("base") is None:
-                w = ctx.weights8_prepare(torch.as_tensor(np.asarray(L["W"], dtype=np.int8)).to(ctx.device))
+                w = ctx.weights8_prepare(torch.as_tensor(_integers(L["W"], np.int8, "W")).to(ctx.device))
             else:
                 w = ctx.mx4_quantise(torch.as_tensor(np.asarray(L["W"], dtype=np.float32)).to(ctx.device), L["base"], L["max_shift"])
             bias = None
             if L.get("bias") is not None:
-                bias = torch.as_tensor(np.asarray(L["bias"], dtype=np.int32)).to(ctx.device)
+                bias = torch.as_tensor(_integers(L["bias"], np.int32, "bias")).to(ctx.device)
             routing = None
             if L.get("route") is not None:
-                routing = _PerBatch(L["route"], L["rows"], ctx)
+                routing = _PerBatch(L["route"], L["rows"], ctx, "route")
             lay = B.Layer(B.EXPERTS, L["id"], b * L["rows"], top_k=L["top_k"], weights=w, bias=bias)
             if routing is not None:
                 lay.routing = ctx.route(routing.part(batch_base, b), w.n_experts)
                 lay.c.routing = lay.routing.address()
                 lay.rebase = lambda base, lay=lay, r=routing, e=w.n_experts: ctx.route(r.part(base, b), e, out=lay.routing)
         elif kind == "combine":
-            gates = _PerBatch(L["gates"], L["rows"] * L["top_k"], ctx)
+            gates = _PerBatch(L["gates"], L["rows"] * L["top_k"], ctx, "gates")
             part = gates.part(batch_base, b).clone()
             lay = B.Layer(B.COMBINE, L["id"], b * L["rows"], in_c=L["V"], top_k=L["top_k"], gates=part)
             lay.rebase = lambda base, part=part, g=gates: part.copy_(g.part(base, b))
@@ -67,12 +67,25 @@ def build_layers(ctx, net, b, batch_base):
     return layers, sizes, table_bytes, scratch_max
 
 
+def _integers(values, dtype, what):
+    """the entry `what` of a layer as an array of integers of the type that the library takes; what the type does not hold is refused"""
+    given = np.asarray(values)
+    try:
+        with np.errstate(invalid="ignore"):
+            cast = given.astype(dtype)
+    except (OverflowError, TypeError, ValueError):
+        cast = None
+    if cast is None or not np.array_equal(given, cast):
+        raise ValueError("%s: integers of %s expected" % (what, np.dtype(dtype).name))
+    return cast
+
+
 class _PerBatch:
     """int32 entries of the whole batch on the device, `per` for every batch element"""
 
-    def __init__(self, values, per, ctx):
+    def __init__(self, values, per, ctx, what):
         import torch
-        self.per, self.all = per, torch.as_tensor(np.asarray(values, dtype=np.int32).reshape(-1)).to(ctx.device)
+        self.per, self.all = per, torch.as_tensor(_integers(values, np.int32, what).reshape(-1)).to(ctx.device)
 
     def part(self, base, b):
         if (base + b) * self.per > self.all.numel():
