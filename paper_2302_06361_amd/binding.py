@@ -194,6 +194,11 @@ class Layer:
                     self.c.routing = v.address()
             elif k in ("weights", "bias", "phi", "gates"):
                 if v is not None:
+                    if k in ("bias", "gates") and kind in (EXPERTS, COMBINE):
+                        # (several numbers a row, read by address)
+                        import torch
+                        if v.dtype != torch.int32 or not v.is_contiguous():
+                            raise DashError("Layer: %s has to be a contiguous int32 tensor" % k)
                     self.keep.append(v)
                     setattr(self.c, k, v.data_ptr())
             else:

@@ -36,7 +36,7 @@ def build_layers(ctx, net, b, batch_base):
             if L.get("base") is None:
                 w = ctx.weights8_prepare(torch.as_tensor(_integers(L["W"], np.int8, "W")).to(ctx.device))
             else:
-                w = ctx.mx4_quantise(torch.as_tensor(np.asarray(L["W"], dtype=np.float32)).to(ctx.device), L["base"], L["max_shift"])
+                w = ctx.mx4_quantise(torch.as_tensor(np.ascontiguousarray(L["W"], dtype=np.float32)).to(ctx.device), L["base"], L["max_shift"])
             bias = None
             if L.get("bias") is not None:
                 bias = torch.as_tensor(_integers(L["bias"], np.int32, "bias")).to(ctx.device)
@@ -68,11 +68,11 @@ def build_layers(ctx, net, b, batch_base):
 
 
 def _integers(values, dtype, what):
-    """the entry `what` of a layer as an array of integers of the type that the library takes; what the type does not hold is refused"""
+    """the entry `what` of a layer as a contiguous array of integers of the type that the library takes; what the type does not hold is refused"""
     given = np.asarray(values)
     try:
         with np.errstate(invalid="ignore"):
-            cast = given.astype(dtype)
+            cast = np.ascontiguousarray(given.astype(dtype))
     except (OverflowError, TypeError, ValueError):
         cast = None
     if cast is None or not np.array_equal(given, cast):
