@@ -203,6 +203,9 @@ class Layer:
                     setattr(self.c, k, v.data_ptr())
             else:
                 setattr(self.c, k, v)
+        weights, bias = kw.get("weights"), kw.get("bias")
+        if isinstance(weights, ExpertWeights) and bias is not None and bias.numel() < weights.n_experts * weights.out_c:
+            raise DashError("Layer: bias [n_experts][out_c] expected, got %d numbers" % bias.numel())
 
 
 class Context:

@@ -57,3 +57,25 @@ def test_tensors_that_a_layer_cannot_read():
             assert (getattr(Layer(kind, 1, 4, **{name: good}).c, name) or 0) == (0 if good is None else good.data_ptr())
     # dense layers as before
     assert Layer(DENSE, 1, 4, bias=t[0, ::2]).c.bias == t.data_ptr()
+
+
+def expert_weights(format, E, M, K):
+    from paper_2302_06361_amd import ExpertWeights
+    w = ExpertWeights.__new__(ExpertWeights)
+    w.format, w.n_experts, w.out_c, w.K, w.data = format, E, M, K, torch.zeros(16, dtype=torch.uint8)
+    return w
+
+
+def test_bias_has_an_entry_for_every_expert_and_output():
+    """the products read n_experts * out_c of them"""
+    W = expert_weights(0, 3, 5, 7)
+    for n in (15, 16):
+        b = torch.zeros(n, dtype=torch.int32)
+        for kw in (dict(weights=W, bias=b), dict(bias=b, weights=W)):
+            assert Layer(EXPERTS, 1, 2, top_k=1, **kw).c.bias == b.data_ptr()
+    for n in (0, 5, 14):
+        b = torch.zeros(n, dtype=torch.int32)
+        for kw in (dict(weights=W, bias=b), dict(bias=b, weights=W)):
+            with pytest.raises(DashError, match="bias"):
+                Layer(EXPERTS, 1, 2, top_k=1, **kw)
+    assert not Layer(EXPERTS, 1, 2, top_k=1, weights=W, bias=None).c.bias
