@@ -185,6 +185,8 @@ class Layer:
         self.keep = []
         for k, v in kw.items():
             if isinstance(v, ExpertWeights):
+                if kind != EXPERTS:
+                    raise DashError("Layer: ExpertWeights are the weights of EXPERTS layers (one expert, no routing: a dense layer)")
                 self.keep.append(v)
                 self.c.weights, self.c.weight_format = v.data.data_ptr(), v.format
                 self.c.n_experts, self.c.out_c, self.c.in_c = v.n_experts, v.out_c, v.K

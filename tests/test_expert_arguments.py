@@ -79,3 +79,13 @@ def test_bias_has_an_entry_for_every_expert_and_output():
             with pytest.raises(DashError, match="bias"):
                 Layer(EXPERTS, 1, 2, top_k=1, **kw)
     assert not Layer(EXPERTS, 1, 2, top_k=1, weights=W, bias=None).c.bias
+
+
+def test_expert_weights_belong_to_expert_layers():
+    """a dense layer reads its weights as residues, k bytes a weight, past the end of these"""
+    from paper_2302_06361_amd import CONV2D, RELU
+    for kind in (DENSE, CONV2D, COMBINE, RELU):
+        for format in (0, 1):
+            with pytest.raises(DashError, match="EXPERTS"):
+                Layer(kind, 1, 2, weights=expert_weights(format, 1, 5, 7))
+    assert Layer(EXPERTS, 1, 2, top_k=1, weights=expert_weights(1, 1, 5, 7)).c.weight_format == 1
