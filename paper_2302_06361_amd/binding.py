@@ -119,7 +119,8 @@ class Labels:
 
     def c(self):
         s = CLabels()
-        _describe(self.tensors, C.addressof(s), self.n_elem)
+        t = self.tensors
+        _describe(t if type(t) is list else list(t), C.addressof(s), self.n_elem)
         return s
 
     def slice(self, e0, e1):
