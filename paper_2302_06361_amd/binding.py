@@ -73,16 +73,30 @@ def lib():
     return _lib
 
 
-def _describe(tensors, address, n_elem):
-    """The dash_labels of a list of tensors, through the host module built beside the library."""
+def _describe_plain(tensors, address, n_elem):
+    """The dash_labels at `address` of a list of tensors, one by one (12 of them: 6 us)."""
+    s = CLabels.from_address(address)
+    C.memset(address, 0, C.sizeof(s))
+    s.n_elem = n_elem
+    for i, t in enumerate(tensors):
+        if t is not None:
+            s.data[i] = t.data_ptr()
+            s.chunk_stride[i] = t.stride(0)
+
+
+def _describe_first(tensors, address, n_elem):
+    """The same through the host module built beside the library (0.2 us), where it is there."""
     global _describe
     import torch  # noqa: F401  (the module uses its libraries)
     try:
         from ._bundle import describe
-    except ImportError as e:
-        raise DashError("the binding's host module is missing: build it with `python -m paper_2302_06361_amd.build` (%s)" % e)
+    except ImportError:
+        describe = _describe_plain
     _describe = describe
     describe(tensors, address, n_elem)
+
+
+_describe = _describe_first
 
 
 def _check(st, what):

@@ -1,7 +1,10 @@
-"""A bundle's tensors as any sequence.  No GPU needed: addresses and strides of any tensor."""
+"""A bundle's tensors as any sequence, and the binding without its compiled host module.  No GPU needed: addresses and strides of any tensor."""
+import sys
+
 import pytest
 import torch
 
+from paper_2302_06361_amd import binding
 from paper_2302_06361_amd.binding import Labels
 
 
@@ -45,3 +48,16 @@ def test_any_sequence_of_tensors(kind):
     b = bundle(SEQUENCES[kind](t))
     for _ in range(2):
         check(b.c(), t)
+
+
+@pytest.mark.parametrize("kind", list(SEQUENCES))
+def test_without_the_host_module(kind, monkeypatch):
+    """the library alone is enough: addresses are then asked for one by one"""
+    monkeypatch.setitem(sys.modules, "paper_2302_06361_amd._bundle", None)       # (an import of it fails)
+    monkeypatch.setattr(binding, "_describe", binding._describe_first)
+    t = items()
+    b = bundle(SEQUENCES[kind](t))
+    for _ in range(2):
+        check(b.c(), t)
+    with pytest.raises(IndexError):
+        bundle([t[0]] * 17).c()
