@@ -315,6 +315,7 @@ constexpr int64_t kMaxLanes = 0x7fffffffll * kThreads;
 int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labels* in, dash_labels* out, hipStream_t s) {
     int st = layer_sizes(c, L, nullptr, nullptr, nullptr);
     if (st) return st;
+    if (L->n_elem == 0) return DASH_OK;         // (empty bundles and gates may have no address)
     if (!L->weights || ((uintptr_t)L->weights & 15) || (L->weight_format != DASH_W8 && L->weight_format != DASH_MX4)) return DASH_EINVAL;
     const int64_t n = L->n_elem, T = n / L->top_k;
     const int M = L->out_c, K = L->in_c, E = L->n_experts;
@@ -328,7 +329,6 @@ int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labe
         const uint64_t p1 = (uint64_t)c->prime[i] - 1, w = L->weight_format == DASH_W8 ? 256 : p1;
         if (w * p1 * (uint64_t)K + p1 >= (1ull << 31)) return DASH_ESIZE;
     }
-    if (n == 0) return DASH_OK;
     ExpertsCall call{(const uint8_t*)L->weights, L->bias, nullptr, n, M, K, E, L->top_k, L->weight_format, garble};
     RoutingView R;
     if (L->routing) { R = routing_view(c, L->routing->data, n, E); call.routing = &R; }
@@ -338,13 +338,13 @@ int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labe
 int combine_layer(dash_ctx* c, const dash_layer* L, const dash_labels* in, dash_labels* out, hipStream_t s) {
     int st = layer_sizes(c, L, nullptr, nullptr, nullptr);
     if (st) return st;
+    if (L->n_elem == 0) return DASH_OK;         // (empty bundles and gates may have no address)
     if (L->top_k > 1024) return DASH_ESIZE;            // (p - 1)^2 top_k below 2^24: one step to the residue
     const int64_t n = L->n_elem;
     const int V = L->in_c;
     if (!L->gates) return DASH_EINVAL;
     if (n > 0x7fffffff / V / L->top_k) return DASH_ESIZE;
     if ((st = check_bundle(c, in, n * L->top_k * V)) || (st = check_bundle(c, out, n * V))) return st;
-    if (n == 0) return DASH_OK;
     CombArgs A;
     memset(&A, 0, sizeof(A));
     A.mods = c->d_mods; A.gates = L->gates; A.n = n; A.V = V; A.top_k = L->top_k;
