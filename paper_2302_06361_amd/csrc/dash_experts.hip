@@ -13,6 +13,7 @@
 #include <string.h>
 
 #include "dash_experts.h"
+#include "dash_experts_rule.h"
 
 namespace dash {
 
@@ -113,7 +114,7 @@ struct PrepArgs8 {
 };
 // a lane per 16-byte piece of a tile
 __global__ __launch_bounds__(kThreads) void k_weights8_prepare(const PrepArgs8 A) {
-    const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x, tile = idx / (kW8Tile / 16);
+    const int64_t idx = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, tile = idx / (kW8Tile / 16);
     if (tile >= A.tiles) return;
     const int piece = (int)(idx % (kW8Tile / 16)), r = piece / 4, q = piece % 4;
     const int64_t kt = col_tiles(A.K), mt = row_tiles(A.M), e = tile / (mt * kt), at = tile - e * mt * kt;
@@ -181,7 +182,8 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
     typedef typename Q::T T;
     __shared__ __attribute__((aligned(16))) uint8_t to[kMx4Tile];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const uint32_t tile = blockIdx.x;
+    const uint32_t tile = blockIdx.y * gridDim.x + blockIdx.x;
+    if (tile >= A.tiles) return;
     const uint32_t kt = (uint32_t)col_tiles(A.K), mt = (uint32_t)row_tiles(A.M);
     const uint32_t rt = tile / kt, e = rt / mt;
     const int r0 = wave * (kTileRows / kWaves) + lane / kRowLanes;
@@ -282,12 +284,12 @@ struct CombArgs {
     int V, top_k;
     CombPrime pr[DASH_MAX_PRIMES];
 };
-// A lane per output word: the top_k words of its inputs are neighbours of its neighbours' and each is read once.  blockIdx.y = prime.  Bound by
-// HBM: four rows each of 128 batch elements, 4096 values, 12 primes, 1.64 GB, in 287 us (5.7 TB/s).
+// A lane per output word: the top_k words of its inputs are neighbours of its neighbours' and each is read once.  blockIdx.y = prime, blocks go on
+// in z.  Bound by HBM: four rows each of 128 batch elements, 4096 values, 12 primes, 1.64 GB, in 287 us (5.7 TB/s).
 __global__ __launch_bounds__(kThreads) void k_combine(const CombArgs A) {
     const CombPrime& P = A.pr[blockIdx.y];
     const ModInfo M = A.mods[P.p];
-    const int64_t idx = (int64_t)blockIdx.x * kThreads + threadIdx.x, per = A.n * A.V;
+    const int64_t idx = ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * kThreads + threadIdx.x, per = A.n * A.V;
     if (idx >= per * M.nchunk) return;
     const int64_t ch = idx / per, o = idx - ch * per, t = o / A.V, v = o - t * A.V;
     uint32_t acc[16] = {};
@@ -309,7 +311,7 @@ static int check_bundle(const dash_ctx* c, const dash_labels* t, int64_t n) {
         if (!t->data[i] || ((uintptr_t)t->data[i] & 15) || (t->chunk_stride[i] & 15) || t->chunk_stride[i] < 16 * n) return DASH_EINVAL;
     return DASH_OK;
 }
-static uint32_t blocks_of(int64_t lanes) { return (uint32_t)((lanes + kThreads - 1) / kThreads); }
+static BlockGrid grid_of(int64_t lanes) { return block_grid((lanes + kThreads - 1) / kThreads, kThreads, 1); }
 constexpr int64_t kMaxLanes = 0x7fffffffll * kThreads;
 
 int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labels* in, dash_labels* out, hipStream_t s) {
@@ -358,7 +360,8 @@ int combine_layer(dash_ctx* c, const dash_layer* L, const dash_labels* in, dash_
         bytes += (double)n * V * (L->top_k + 1) * Mi.lam;
     }
     ProfScope ps(c->prof, DASH_PROF_LINEAR, s, macs, bytes);
-    hipLaunchKernelGGL(k_combine, dim3(blocks_of(lanes), c->k), dim3(kThreads), 0, s, A);
+    const BlockGrid grid = grid_of(lanes);
+    hipLaunchKernelGGL(k_combine, dim3(grid.x, c->k, grid.y), dim3(kThreads), 0, s, A);
     DASH_HIP(hipGetLastError());
     return DASH_OK;
 }
@@ -388,7 +391,8 @@ int dash_weights8_prepare(dash_ctx* c, const int8_t* w, int64_t row_stride, int6
     const int64_t lanes = tiles * (kW8Tile / 16);
     if (lanes > kMaxLanes) return DASH_ESIZE;
     const PrepArgs8 A{w, row_stride, expert_stride, tiles, out_c, K, (uint8_t*)prepared};
-    hipLaunchKernelGGL(k_weights8_prepare, dim3(blocks_of(lanes)), dim3(kThreads), 0, (hipStream_t)stream, A);
+    const BlockGrid grid = grid_of(lanes);
+    hipLaunchKernelGGL(k_weights8_prepare, dim3(grid.x, grid.y), dim3(kThreads), 0, (hipStream_t)stream, A);
     DASH_HIP(hipGetLastError());
     return DASH_OK;
 }
@@ -403,7 +407,8 @@ int dash_mx4_quantise(dash_ctx* c, const void* w, int dtype, int64_t row_stride,
     if (tiles > 0x7fffffff) return DASH_ESIZE;
     const QuantArgs A{w, row_stride, expert_stride, tiles, out_c, K, base, max_shift, (uint8_t*)prepared, values};
     auto kernel = dtype == DASH_F32 ? k_mx4_quantise<QuantF32> : dtype == DASH_BF16 ? k_mx4_quantise<QuantBF16> : k_mx4_quantise<QuantF16>;
-    hipLaunchKernelGGL(kernel, dim3((uint32_t)tiles), dim3(kThreads), 0, (hipStream_t)stream, A);
+    const BlockGrid grid = block_grid(tiles, kThreads, 1);
+    hipLaunchKernelGGL(kernel, dim3(grid.x, grid.y), dim3(kThreads), 0, (hipStream_t)stream, A);
     DASH_HIP(hipGetLastError());
     return DASH_OK;
 }

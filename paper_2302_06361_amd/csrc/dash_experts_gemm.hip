@@ -198,10 +198,10 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         }
     };
     // the block's next tile with an expert
-    int seq = (int)(blockIdx.x >> 3) - (int)(gridDim.x >> 3);
+    int seq = (int)(blockIdx.x >> 3) + ((int)blockIdx.y - (int)gridDim.y) * (int)(gridDim.x >> 3);
     auto next_tile = [&](Tile& t) __attribute__((always_inline)) -> bool {
         for (;;) {
-            seq += (int)(gridDim.x >> 3);
+            seq += (int)gridDim.y * (int)(gridDim.x >> 3);
             if (!decode(seq, t)) return false;
             if (t.e < A.E) return true;
             zeros(t);
@@ -620,7 +620,8 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         const int64_t total = cols * A.row_blocks;
         if (cols * A.sty > 0x7fffffff || total > 0x7fffff00) return DASH_ESIZE;
         ProfScope ps(c->prof, DASH_PROF_LINEAR, s, macs, bytes);
-        hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3((uint32_t)(TL::PERSIST && total > kCus ? kCus : (total + 7) / 8 * 8)), dim3(TL::T), 0, s, A);
+        const BlockGrid grid = block_grid(TL::PERSIST && total > kCus ? kCus : total, TL::T, 8);
+        hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3(grid.x, grid.y), dim3(TL::T), 0, s, A);
         return DASH_OK;
     };
     ExpertsShape shape{L.n, L.E, L.M, L.K, L.format == DASH_MX4, c->k, {}};
