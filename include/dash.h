@@ -103,18 +103,27 @@ typedef struct {
     int32_t in_h, in_w, in_c, out_c, kh, kw, stride, pad;
     const void *weights;  /* device, written by dash_weights_prepare; EXPERTS: dash_weights8_prepare, dash_mx4_quantise */
     const int32_t *bias;  /* device int32 [out_c] (EXPERTS: [n_experts][out_c]) or NULL: added as bias * (constant-one wire) */
-    /* SCALE */
-    int32_t repeat;
+    /* Each kind reads its own names.  EXPERTS and COMBINE share places with SCALE and PROJ: the size of the descriptor and the places of
+       its fields stay as they were (arrays of it are passed by programs compiled before there were expert layers). */
+    union {
+        int32_t repeat;         /* SCALE */
+        int32_t top_k;          /* EXPERTS, COMBINE: rows per batch element, >= 1 (COMBINE: at most 1024) */
+    };
     /* PROJ: input tensor in->data[p_index], output tensor out->data[q_index] */
-    int32_t p_index, q_index;
-    const uint8_t *phi;   /* device, function tables, phi[g * phi_stride + a] in [0, q) */
-    int64_t phi_stride;   /* p (one table per gate) or 0 (one table for all gates) */
-    /* EXPERTS, COMBINE */
-    int32_t top_k;                 /* rows per batch element, >= 1 */
-    int32_t n_experts;             /* EXPERTS: matrices in `weights`, >= 1 */
-    int32_t weight_format;         /* EXPERTS: DASH_W8 or DASH_MX4 */
-    const dash_routing *routing;   /* EXPERTS: host pointer; NULL with n_experts = 1: every row takes the one matrix (a dense layer) */
-    const int32_t *gates;          /* COMBINE: device int32 [n_elem][top_k], public */
+    union {
+        int32_t p_index;
+        int32_t n_experts;      /* EXPERTS: matrices in `weights`, >= 1 */
+    };
+    union {
+        int32_t q_index;
+        int32_t weight_format;  /* EXPERTS: DASH_W8 or DASH_MX4 */
+    };
+    union {
+        const uint8_t *phi;           /* PROJ: device, function tables, phi[g * phi_stride + a] in [0, q) */
+        const dash_routing *routing;  /* EXPERTS: host pointer; NULL with n_experts = 1: every row takes the one matrix (a dense layer) */
+        const int32_t *gates;         /* COMBINE: device int32 [n_elem][top_k], public */
+    };
+    int64_t phi_stride;   /* PROJ: p (one table per gate) or 0 (one table for all gates) */
 } dash_layer;
 
 /* Create a context on GPU `hip_device`: the CRT base (distinct primes, primes[0] must be 2 for

@@ -33,14 +33,22 @@ class CLabels(C.Structure):
     _fields_ = [("data", C.c_void_p * MAX_PRIMES), ("chunk_stride", C.c_int64 * MAX_PRIMES), ("n_elem", C.c_int64)]
 
 
+def _shared(*fields):
+    """fields of different kinds of layers in one place"""
+    return type("CShared", (C.Union,), {"_fields_": list(fields)})
+
+
 class CLayer(C.Structure):
+    _anonymous_ = ("u0", "u1", "u2", "u3")
     _fields_ = [("kind", C.c_int32), ("layer_id", C.c_int32), ("elem_base", C.c_int64), ("n_elem", C.c_int64),
                 ("in_h", C.c_int32), ("in_w", C.c_int32), ("in_c", C.c_int32), ("out_c", C.c_int32),
                 ("kh", C.c_int32), ("kw", C.c_int32), ("stride", C.c_int32), ("pad", C.c_int32),
-                ("weights", C.c_void_p), ("bias", C.c_void_p), ("repeat", C.c_int32),
-                ("p_index", C.c_int32), ("q_index", C.c_int32), ("phi", C.c_void_p), ("phi_stride", C.c_int64),
-                ("top_k", C.c_int32), ("n_experts", C.c_int32), ("weight_format", C.c_int32), ("routing", C.c_void_p),
-                ("gates", C.c_void_p)]
+                ("weights", C.c_void_p), ("bias", C.c_void_p),
+                ("u0", _shared(("repeat", C.c_int32), ("top_k", C.c_int32))),
+                ("u1", _shared(("p_index", C.c_int32), ("n_experts", C.c_int32))),
+                ("u2", _shared(("q_index", C.c_int32), ("weight_format", C.c_int32))),
+                ("u3", _shared(("phi", C.c_void_p), ("routing", C.c_void_p), ("gates", C.c_void_p))),
+                ("phi_stride", C.c_int64)]
 
 
 class CRouting(C.Structure):
