@@ -620,7 +620,7 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
         const int64_t total = cols * A.row_blocks;
         if (cols * A.sty > 0x7fffffff || total > 0x7fffff00) return DASH_ESIZE;
         ProfScope ps(c->prof, DASH_PROF_LINEAR, s, macs, bytes);
-        const BlockGrid grid = block_grid(TL::PERSIST && total > kCus ? kCus : total, TL::T, 8);
+        const BlockGrid grid = block_grid(TL::PERSIST && total > kCus ? kCus : total, TL::T);
         hipLaunchKernelGGL((k_experts_mfma<decltype(fmt)::value, TL>), dim3(grid.x, grid.y), dim3(TL::T), 0, s, A);
         return DASH_OK;
     };

@@ -1,4 +1,4 @@
-// dash_experts_rule.h -- which tile the products of an expert layer take, as a function of its sizes alone, and the grids of launches (host code)
+// dash_experts_rule.h -- which tile the products of an expert layer take, as a function of its sizes alone, and the grid of the launch (host code)
 #pragma once
 #include <stdint.h>
 
@@ -69,11 +69,11 @@ inline ExpertsTile experts_tile(int forced, const ExpertsShape& S) {
     return (ExpertsTile)best;
 }
 
-// At least `blocks` blocks of `threads` threads as x times y, x a multiple of `multiple`: a direction of a grid holds fewer than 2^32 threads.
+// At least `blocks` blocks of `threads` threads as x times y, x a multiple of the 8 XCDs: a direction of a grid holds fewer than 2^32 threads.
 struct BlockGrid { uint32_t x, y; };
-inline BlockGrid block_grid(int64_t blocks, int threads, int multiple) {
-    const int64_t most = 0xffffffffll / threads / multiple * multiple, y = (blocks + most - 1) / most, x = (blocks + y - 1) / y;
-    return BlockGrid{(uint32_t)((x + multiple - 1) / multiple * multiple), (uint32_t)y};
+inline BlockGrid block_grid(int64_t blocks, int threads) {
+    const int64_t most = 0xffffffffll / threads / 8 * 8, y = (blocks + most - 1) / most, x = (blocks + y - 1) / y;
+    return BlockGrid{(uint32_t)((x + 7) / 8 * 8), (uint32_t)y};
 }
 
 }  // namespace dash
