@@ -31,20 +31,27 @@ inline double experts_tiles(const ExpertsShape& S, int groups) {
     return t * busy;
 }
 // Time in us: a launch, and on the fullest CU what a block takes beside its stages of 64 inputs, and the stages, at the rate of one block's
-// latency or of what shares the CU.  Constants from runs over 18 layers (rows x K -> M; us of repeated calls: bytes big, narrow | 4-bit big, narrow,
-// few, wide):
-//   1 x 4096 -> 4096: 37.4, 16 | 43, 26.8, 25.2, 33.8
-//   4: 41.4, 41.5 | 47.4, 50.1, 59.5, 53.6
-//   16: 131, 141 | 149, 158, 229, 140
-//   128: 991, 1230 | 1029, 1246, 1765, 1076
-//   1 x 784 -> 128, 8 primes: 12.7, 5.8 | 12.5, 7.7, 7, 10.8
-//   16 rows, 8 experts, 400 -> 120: 10.2, 5.2 | 11.2, 6.4, 6.2, 8.7
-//   256 rows, 32 experts, 1024 -> 2048: 325, 376 | 414, 425, 667, 355
-//   64 rows, 64 experts, 1024 -> 1024: 49.2, 50.6 | 109, 77.9, 102, 67
-//   256 x 2048 -> 64: 73.7, 60.6 | 88.7, 64, 76.8, 80.5
-//   200 rows, 8 experts, 100 -> 1500: 61.5, 86.4 | 79.9, 88.6, 171, 66.3
-//   64 rows, 12 experts, 4096 -> 256: 43.7, 43.7 | 52.8, 51.8, 69.4, 54.1
-// Over 441 drawn layers the choice took over 5 % more than the fastest tile in 25, over 10 % in 15, at most 37 %.
+// latency or of what shares the CU.  Constants fitted to runs over these 18 layers (us of repeated calls: bytes big, narrow | 4-bit big, narrow, few, wide):
+//   1 row, 784 -> 128, 8 primes: 12.7, 5.8 | 12.5, 7.7, 7, 10.8
+//   1 row, 4096 -> 4096, 12 primes: 37.4, 16 | 43, 26.8, 25.2, 33.8
+//   4 rows, 4096 -> 4096, 12 primes: 41.4, 41.5 | 47.4, 50.1, 59.5, 53.6
+//   16 rows, 4096 -> 4096, 12 primes: 131, 141 | 149, 158, 229, 140
+//   128 rows, 4096 -> 4096, 12 primes: 991, 1230 | 1029, 1246, 1765, 1076
+//   16 rows, 8 experts, 400 -> 120, 8 primes: 10.2, 5.2 | 11.2, 6.4, 6.2, 8.7
+//   256 rows, 32 experts, 1024 -> 2048, 12 primes: 325, 376 | 414, 425, 667, 355
+//   128 rows, 16 experts, 512 -> 768, 9 primes: 41.7, 41.8 | 48, 50.3, 80.5, 41.2
+//   64 rows, 12 experts, 4096 -> 256, 12 primes: 43.7, 43.7 | 52.8, 51.8, 69.4, 54.1
+//   64 rows, 64 experts, 1024 -> 1024, 12 primes: 49.2, 50.6 | 109, 77.9, 102, 67
+//   64 rows, 16 experts, 1024 -> 1024, 12 primes: 47.7, 48 | 62.5, 59.8, 91.1, 52.8
+//   2 rows, 2048 -> 2048, 12 primes: 22, 9.4 | 25.5, 14.1, 16.5, 19.6
+//   8 rows, 256 -> 4096, 8 primes: 11.3, 11.4 | 18.7, 13.4, 22.7, 11.6
+//   39 rows, 4 experts, 81 -> 29, 12 primes: 8.2, 4.6 | 8.3, 5.1, 6.6, 6.7
+//   65 rows, 4 experts, 228 -> 12, 7 primes: 8.9, 4.8 | 9.5, 5.6, 7.3, 7.7
+//   12 rows, 6 experts, 3833 -> 172, 9 primes: 35.6, 14.4 | 45.5, 22.3, 17.1, 32.4
+//   256 rows, 2048 -> 64, 12 primes: 73.7, 60.6 | 88.7, 64, 76.8, 80.5
+//   200 rows, 8 experts, 100 -> 1500, 9 primes: 61.5, 86.4 | 79.9, 88.6, 171, 66.3
+// Over 441 drawn layers, none of them fitted to, the choice took over 5 % more than the fastest tile in 25, over 10 % in 15, at most 37 % (bytes, 24 rows,
+// 15 experts, 1170 -> 570: 20.0 us with the big tile, 14.6 with the narrow one).
 inline double experts_us(const ExpertsShape& S, ExpertsTile tile) {
     const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_FEW ? 4 : 8, features = tile == EXPERTS_BIG || tile == EXPERTS_WIDE ? 256 : 128;
     double block, latency, rate, busy, resident = tile == EXPERTS_BIG ? 1 : tile == EXPERTS_FEW ? 1.3 : 2;       // (blocks that start side by side)
