@@ -159,7 +159,7 @@ int dash_ctx_one(const dash_ctx *ctx, int i, int which, uint8_t *host_out);
 int dash_ctx_digits(const dash_ctx *ctx, uint16_t *host_digits);
 
 /* Sizes of one layer call: output elements (values, or batch elements for the linear kinds:
- * then *out_elems is values per batch element), bytes of ciphertext tables, bytes of scratch.  The scratch of a
+ * then *out_elems is values per batch element, of an EXPERTS layer values per row), bytes of ciphertext tables, bytes of scratch.  The scratch of a
  * SCALE layer does not depend on its repetitions and grows with its values: one buffer serves smaller layers. */
 int dash_layer_sizes(const dash_ctx *ctx, const dash_layer *layer, int64_t *out_elems, size_t *table_bytes,
                      size_t *scratch_bytes);
@@ -172,6 +172,9 @@ int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void
 
 /* Layers whose matrix depends on the row (EXPERTS).  Which expert serves a row is public: a garbled circuit is fixed before its
  * inputs are known, so rows are routed by what is known then (the client, the task, a position), never by a label.
+ *
+ * Sums are held in 31 bits: in_c times 256 (p - 1) for DASH_W8, (p - 1)^2 for DASH_MX4, has to stay below 2^31 for the largest prime p,
+ * else DASH_ESIZE.
  *
  * Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] one after the other, 16-byte aligned, independent of the
  * primes.  A matrix is cut into tiles of 32 rows x 64 columns, row tiles outermost, zeros past out_c and K.
@@ -195,7 +198,8 @@ int dash_mx4_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_strid
 /* Sorts rows by expert: experts: device int32 [n], the expert of every row in [0, n_experts); any other number: no expert, the
  * row's outputs are all-zero labels on both sides (the value 0, no bias).  Fills *routing, which the caller keeps (with `data`) as long as layers refer
  * to it; one routing serves garbler and evaluator, and every layer over the same rows.  `experts` may be changed once the stream
- * has passed the call. */
+ * has passed the call.  dash_route_bytes is 0 for sizes that dash_route refuses (n times the 16-digit chunks of all primes and 64 more
+ * below 2^31, n_experts below 2^24 - 1). */
 size_t dash_route_bytes(const dash_ctx *ctx, int64_t n, int n_experts);
 int dash_route(dash_ctx *ctx, const int32_t *experts, int64_t n, int n_experts, void *data, dash_routing *routing,
                void *hip_stream);

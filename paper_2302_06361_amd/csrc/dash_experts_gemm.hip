@@ -12,7 +12,8 @@
 // LDS itself: ds_read_b64_tr_b8 gives lane l of 16 the byte l of 8 words.  A ring of S stages of 64 inputs, the loop unrolled over its
 // slots; each wave waits for its own loads of the stages ahead (vmcnt counts down in order, all stages issue the same number), then
 // one barrier a stage.  (With loads through registers and byte permutes, as the dense layers have them, the same product takes
-// 1 096 us; with the slots as run-time numbers small tiles issued twice the instructions: one row, 4096 -> 4096: 40 us, now 27.)
+// 1 096 us; with the slots as run-time numbers small tiles issued twice the instructions: one row, 4096 -> 4096: 40 us,
+// unrolled 27 at that step.)
 //
 // Weights.  Signed bytes are the operand as they are, for every prime: a tile goes across primes, the sums start at a multiple of p that
 // keeps them positive and are reduced once.  4-bit floats: 2 e2m1 2^shift mod p by table: the 8 magnitudes of a shift and their
@@ -22,9 +23,9 @@
 //
 // What bounds it (us).  128 rows, 4096 -> 4096, 12 primes: 960 to 1 025 with bytes from box to box (2.3 to 2.5 POP/s counted over the label digits, 2.6 to
 // 2.8 with the zero digits of the last chunks; a library's int8 product of 16384 reaches 2.4): power, the matrix pipe is busy 76 % of the cycles and the clock falls
-// from 2.7 to 1.6 GHz.  4-bit: 1 010 to 1 030, the expansion beside it.  32 experts, 256 rows, 1024 -> 2048, 4-bit: 358 with 128 x 256 tiles, two
-// blocks a CU (256 x 256, one block: 412): vector instructions of the expansion in 68 % of the cycles, the matrix pipe in 41 %.  One row,
-// 4096 -> 4096, 4-bit: 25; latency of the stages, about 110 instructions by one or two waves a SIMD.  One row, 784 -> 128, 4-bit: 7.0,
+// from 2.7 to 1.6 GHz.  4-bit: 1 010 to 1 060, the expansion beside it.  32 experts, 256 rows, 1024 -> 2048, 4-bit: 358 to 367 with 128 x 256 tiles, two
+// blocks a CU (256 x 256, one block: 412): vector instructions of the expansion in 65 % of the cycles, the matrix pipe in 39 %.  One row,
+// 4096 -> 4096, 4-bit: 26; latency of the stages, about 110 instructions by two to four waves a SIMD.  One row, 784 -> 128, 4-bit: 7.1 to 7.4,
 // 4.8 of them for a single stage: launch, the chain of loads to the first labels, results.
 #include <string.h>
 

@@ -50,7 +50,7 @@ inline double experts_tiles(const ExpertsShape& S, int groups) {
 //   12 rows, 6 experts, 3833 -> 172, 9 primes: 35.6, 14.4 | 45.5, 22.3, 17.1, 32.4
 //   256 rows, 2048 -> 64, 12 primes: 73.7, 60.6 | 88.7, 64, 76.8, 80.5
 //   200 rows, 8 experts, 100 -> 1500, 9 primes: 61.5, 86.4 | 79.9, 88.6, 171, 66.3
-// Over 441 drawn layers, none of them fitted to, the choice took over 5 % more than the fastest tile in 25, over 10 % in 15, at most 37 % (bytes, 24 rows,
+// Over 441 drawn layers the choice took over 5 % more than the fastest tile in 25, over 10 % in 15, at most 37 % (bytes, 24 rows,
 // 15 experts, 1170 -> 570: 20.0 us with the big tile, 14.6 with the narrow one).
 inline double experts_us(const ExpertsShape& S, ExpertsTile tile) {
     const int groups = tile == EXPERTS_BIG ? 16 : tile == EXPERTS_FEW ? 4 : 8, features = tile == EXPERTS_BIG || tile == EXPERTS_WIDE ? 256 : 128;
