@@ -71,7 +71,10 @@ def build(force=True, verbose=False):
         raise RuntimeError("hipcc failed")
     subprocess.check_call([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", SO] + objs)
     if force or not os.path.exists(bundle_so()) or os.path.getmtime(bundle_so()) < max(os.path.getmtime(BUNDLE_SRC), hdr_time):
-        build_bundle()
+        try:
+            build_bundle()
+        except (ImportError, OSError) as e:
+            print("no torch or no host compiler: the binding goes without its host module (%s)" % e)
     return SO
 
 
