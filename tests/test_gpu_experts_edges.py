@@ -14,6 +14,12 @@ def context(primes, **kw):
     return Context(primes, SEED, (2, 6), **kw)
 
 
+@pytest.fixture(autouse=True)
+def memory_goes_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 def test_calls_of_no_rows():
     """empty parts of bundles and empty gates have no address; a dense layer of no batch elements does nothing either"""
     from paper_2302_06361_amd import COMBINE, DENSE, EXPERTS, Labels, Layer
