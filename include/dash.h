@@ -68,9 +68,10 @@ enum {
     DASH_COMBINE = 9   /* out[t][v] = sum_j gate[t][j] * in[t * top_k + j][v]           free gates  */
 };
 
-/* Weights of an EXPERTS layer: signed bytes, or 4-bit floats with a shared power of two for every 32. */
-enum { DASH_W8 = 0, DASH_MX4 = 1 };
-/* Types of the weights that dash_mx4_quantise reads. */
+/* Weights of an EXPERTS layer: signed bytes, 4-bit floats with a shared power of two for every 32, or 8-bit floats with an integer
+ * scale for every block of 128 x 128. */
+enum { DASH_W8 = 0, DASH_MX4 = 1, DASH_F8 = 8 };
+/* Types of the weights that dash_mx4_quantise and dash_f8_quantise read. */
 enum { DASH_F32 = 0, DASH_BF16 = 1, DASH_F16 = 2 };
 
 typedef struct dash_ctx dash_ctx;
@@ -101,7 +102,7 @@ typedef struct {
                            EXPERTS: rows (batch elements * top_k); COMBINE: batch elements of the output */
     /* DENSE, EXPERTS (in_c = K inputs, out_c = M outputs), CONV2D, SUMPOOL (in_h, in_w, in_c), COMBINE (in_c values) */
     int32_t in_h, in_w, in_c, out_c, kh, kw, stride, pad;
-    const void *weights;  /* device, written by dash_weights_prepare; EXPERTS: dash_weights8_prepare, dash_mx4_quantise */
+    const void *weights;  /* device, written by dash_weights_prepare; EXPERTS: dash_weights8_prepare, dash_mx4_quantise, dash_f8_quantise, dash_f8_prepare */
     const int32_t *bias;  /* device int32 [out_c] (EXPERTS: [n_experts][out_c]) or NULL: added as bias * (constant-one wire) */
     /* Each kind reads its own names.  EXPERTS and COMBINE share places with SCALE and PROJ: the size of the descriptor and the places of
        its fields stay as they were (arrays of it are passed by programs compiled before there were expert layers). */
@@ -116,7 +117,7 @@ typedef struct {
     };
     union {
         int32_t q_index;
-        int32_t weight_format;  /* EXPERTS: DASH_W8 or DASH_MX4 */
+        int32_t weight_format;  /* EXPERTS: DASH_W8, DASH_MX4 or DASH_F8 */
     };
     union {
         const uint8_t *phi;           /* PROJ: device, function tables, phi[g * phi_stride + a] in [0, q) */
@@ -173,14 +174,18 @@ int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void
 /* Layers whose matrix depends on the row (EXPERTS).  Which expert serves a row is public: a garbled circuit is fixed before its
  * inputs are known, so rows are routed by what is known then (the client, the task, a position), never by a label.
  *
- * Sums are held in 31 bits: in_c times 256 (p - 1) for DASH_W8, (p - 1)^2 for DASH_MX4, has to stay below 2^31 for the largest prime p,
+ * Sums are held in 31 bits: in_c times 256 (p - 1) for DASH_W8, (p - 1)^2 for DASH_MX4 and DASH_F8, has to stay below 2^31 for the largest prime p,
  * else DASH_ESIZE.
  *
  * Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] one after the other, 16-byte aligned, independent of the
  * primes.  A matrix is cut into tiles of 32 rows x 64 columns, row tiles outermost, zeros past out_c and K.
  *   DASH_W8   2048 bytes a tile: weight (r, c) at 64 r + 16 ((c / 16) ^ f(r)) + c % 16, f(r) = (r / 2) % 4 ^ (r / 8) % 2
  *   DASH_MX4  1088 bytes a tile: the codes of (r, c) in byte 32 r + c % 32, low four bits where c < 32, else high; then the shifts, of (r, c) in byte 1024 + 2 r + c / 32.  A code is an e2m1 float: bit 3 the sign, bits 0..2
- *             the magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6; the weight that enters the layer is the integer 2 * e2m1 * 2^shift. */
+ *             the magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6; the weight that enters the layer is the integer 2 * e2m1 * 2^shift.
+ *   DASH_F8   tiles as DASH_W8's with codes in place of the weights; behind a matrix's tiles the scales, int32 [ceil(out_c / 128)][ceil(K / 128)],
+ *             padded to a multiple of 16 bytes.  A code is an e4m3 float: bit 7 the sign, bits 3..6 the exponent e, bits 0..2 the mantissa m,
+ *             (1 + m/8) 2^(e - 7), or m 2^-9 where e = 0; 0x7f and 0xff, not a number, count as 0.  The weight that enters the layer is the
+ *             integer 512 * e4m3 * scale. */
 size_t dash_expert_weights_bytes(int format, int n_experts, int out_c, int K);
 /* DASH_W8.  w: device int8, element (e, j, i) at w[e * expert_stride + j * row_stride + i] (row_stride >= K, expert_stride
  * >= 0). */
@@ -195,6 +200,17 @@ int dash_weights8_prepare(dash_ctx *ctx, const int8_t *w, int64_t row_stride, in
  * `dtype`, or NULL: the weights that the codes stand for, e2m1 * 2^E (float16 rounds those outside its range). */
 int dash_mx4_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_stride, int64_t expert_stride, int n_experts, int out_c,
                       int K, int base, int max_shift, void *prepared, void *values, void *hip_stream);
+/* DASH_F8, quantised on the device.  w, dtype, strides, values as for dash_mx4_quantise.  The weights of a block of 128 rows by 128 columns
+ * (fewer at the ends) with largest magnitude a get the scale S = ceil(a / (448 * 2^base)), brought into [1, max_scale] (-64 <= base <= 64, 1 <=
+ * max_scale <= 32767); each weight becomes the e4m3 value nearest to w / (S 2^base), ties to the even code, magnitudes past 448 the 448.  The
+ * layer multiplies by integers in units of 2^(base - 9), at most 229376 * max_scale of them.  A NaN counts as 0, an infinity as the
+ * largest float32; no sign on a zero.  values: e4m3 * S * 2^base, rounded once to `dtype`. */
+int dash_f8_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_stride, int64_t expert_stride, int n_experts, int out_c,
+                     int K, int base, int max_scale, void *prepared, void *values, void *hip_stream);
+/* DASH_F8 from codes and scales that exist already.  codes: device, e4m3 bytes, strides as above; scales: device int32, contiguous
+ * [n_experts][ceil(out_c / 128)][ceil(K / 128)], any values. */
+int dash_f8_prepare(dash_ctx *ctx, const uint8_t *codes, int64_t row_stride, int64_t expert_stride, const int32_t *scales, int n_experts,
+                    int out_c, int K, void *prepared, void *hip_stream);
 /* Sorts rows by expert: experts: device int32 [n], the expert of every row in [0, n_experts); any other number: no expert, the
  * row's outputs are all-zero labels on both sides (the value 0, no bias).  Fills *routing, which the caller keeps (with `data`) as long as layers refer
  * to it; one routing serves garbler and evaluator, and every layer over the same rows.  `experts` may be changed once the stream

@@ -5,6 +5,6 @@ This package is a thin binding: argument marshalling and device-buffer bookkeepi
 step of the path runs in the kernels of libdash.so; there is no CPU fallback.
 """
 from .binding import (Context, Labels, Layer, ExpertWeights, Routing, DashError, lib_path,  # noqa: F401
-                      DENSE, CONV2D, SUMPOOL, RELU, SCALE, SIGN, PROJ, EXPERTS, COMBINE, W8, MX4, LAMBDA_CEIL, LAMBDA_FLOOR)
+                      DENSE, CONV2D, SUMPOOL, RELU, SCALE, SIGN, PROJ, EXPERTS, COMBINE, W8, MX4, F8, LAMBDA_CEIL, LAMBDA_FLOOR)
 from .network import GarbledNetwork, StreamedNetwork  # noqa: F401
 from .grouped import ProjectionBatch  # noqa: F401

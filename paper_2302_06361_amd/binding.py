@@ -14,14 +14,14 @@ _SO = os.path.join(_HERE, "libdash.so")
 MAX_PRIMES = 16
 MAX_DIGITS = 16
 DENSE, CONV2D, SUMPOOL, RELU, SCALE, SIGN, PROJ, EXPERTS, COMBINE = 1, 2, 3, 4, 5, 6, 7, 8, 9
-W8, MX4 = 0, 1
+W8, MX4, F8 = 0, 1, 8
 F32, BF16, F16 = 0, 1, 2
 LAMBDA_CEIL, LAMBDA_FLOOR = 0, 1
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 SYMBOLS = ["dash_ctx_create", "dash_ctx_destroy", "dash_lambda", "dash_ctx_offset", "dash_ctx_one", "dash_ctx_digits",
            "dash_layer_sizes", "dash_weights_bytes", "dash_weights_prepare", "dash_expert_weights_bytes", "dash_weights8_prepare",
-           "dash_mx4_quantise", "dash_route_bytes", "dash_route", "dash_garble_layer", "dash_eval_layer",
+           "dash_mx4_quantise", "dash_f8_quantise", "dash_f8_prepare", "dash_route_bytes", "dash_route", "dash_garble_layer", "dash_eval_layer",
            "dash_garble_layers", "dash_eval_layers", "dash_eval_layer_noalloc", "dash_input_labels", "dash_encode", "dash_decode", "dash_labels_pack", "dash_labels_unpack", "dash_tables_packed_bytes", "dash_tables_pack", "dash_tables_unpack", "dash_strerror", "dash_profile_enable", "dash_profile_read", "dash_profile_aes"]
 
 
@@ -75,6 +75,8 @@ def lib():
         L.dash_tables_packed_bytes.restype = C.c_size_t
         L.dash_expert_weights_bytes.restype = C.c_size_t
         L.dash_mx4_quantise.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64] + [C.c_int] * 5 + [C.c_void_p] * 3
+        L.dash_f8_quantise.argtypes = L.dash_mx4_quantise.argtypes
+        L.dash_f8_prepare.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 2
         L.dash_route_bytes.restype = C.c_size_t
         L.dash_ctx_destroy.restype = None
         _lib = L
@@ -175,8 +177,8 @@ class Labels:
 
 
 class ExpertWeights:
-    """Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] in one device buffer, `format` W8 or MX4.  Filled by
-    Context.weights8_prepare or Context.mx4_quantise."""
+    """Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] in one device buffer, `format` W8, MX4 or F8.  Filled by
+    Context.weights8_prepare, Context.mx4_quantise, Context.f8_quantise or Context.f8_prepare."""
 
     def __init__(self, ctx, format, n_experts, out_c, K):
         import torch
@@ -354,18 +356,44 @@ class Context:
         """w: float32, bfloat16 or float16 tensor [n_experts][out_c][K] on the device -> ExpertWeights in the MX4 format: integers
         2 * e2m1 * 2^shift in units of 2^(base - 1), shift <= max_shift.  values: contiguous tensor like w that receives the
         weights the codes stand for."""
-        import torch
-        if self._types is None:
-            self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
-        w, shape, stride = self._expert_matrices(w, "mx4_quantise", self._types)
-        out = self._expert_out(out, MX4, shape, "mx4_quantise")
+        return self._quantise(self.L.dash_mx4_quantise, "mx4_quantise", MX4, w, base, max_shift, out, values)
+
+    def _quantise(self, call, what, format, w, base, most, out, values):
+        types = self._types or self._float_types()
+        w, shape, stride = self._expert_matrices(w, what, types)
+        out = self._expert_out(out, format, shape, what)
         dtype, to = w.dtype, None
         if values is not None:
             to = values.data_ptr()
             if values.dtype != dtype or values.numel() != shape[0] * shape[1] * shape[2] or not values.is_contiguous() or values.device != self.device:
-                raise DashError("mx4_quantise: `values` has to be contiguous and of the size and type of the weights")
-        _check(self.L.dash_mx4_quantise(self.h, w.data_ptr(), self._types[dtype], stride[1], stride[0], *shape, base, max_shift, out.data.data_ptr(), to, _stream()),
-               "dash_mx4_quantise")
+                raise DashError("%s: `values` has to be contiguous and of the size and type of the weights" % what)
+        st = call(self.h, w.data_ptr(), types[dtype], stride[1], stride[0], *shape, base, most, out.data.data_ptr(), to, _stream())
+        if st != 0:
+            _check(st, "dash_" + what)
+        return out
+
+    def _float_types(self):
+        import torch
+        self._types = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+        return self._types
+
+    def f8_quantise(self, w, base, max_scale=255, out=None, values=None):
+        """w: float32, bfloat16 or float16 tensor [n_experts][out_c][K] on the device -> ExpertWeights in the F8 format: integers
+        512 * e4m3 * scale in units of 2^(base - 9), a scale of at most max_scale for every block of 128 x 128.  values: contiguous tensor
+        like w that receives the weights the codes stand for."""
+        return self._quantise(self.L.dash_f8_quantise, "f8_quantise", F8, w, base, max_scale, out, values)
+
+    def f8_prepare(self, codes, scales, out=None):
+        """codes: e4m3 (uint8 or torch.float8_e4m3fn) tensor [n_experts][out_c][K] on the device, scales: contiguous int32 tensor
+        [n_experts][ceil(out_c / 128)][ceil(K / 128)] -> ExpertWeights in the F8 format"""
+        import torch
+        codes, shape, stride = self._expert_matrices(codes, "f8_prepare", (torch.uint8, torch.float8_e4m3fn))
+        E, M, K = shape
+        blocks = (E, (M + 127) // 128, (K + 127) // 128)
+        if scales.dtype != torch.int32 or scales.device != self.device or not scales.is_contiguous() or tuple(scales.shape) not in (blocks, blocks[1:] if E == 1 else blocks):
+            raise DashError("f8_prepare: contiguous int32 scales %s on %s expected, got %s %s on %s" % (list(blocks), self.device, scales.dtype, list(scales.shape), scales.device))
+        out = self._expert_out(out, F8, shape, "f8_prepare")
+        _check(self.L.dash_f8_prepare(self.h, codes.data_ptr(), stride[1], stride[0], scales.data_ptr(), *shape, out.data.data_ptr(), _stream()), "dash_f8_prepare")
         return out
 
     def route(self, experts, n_experts, out=None):

@@ -12,7 +12,19 @@ constexpr int kW8Tile = 2048, kMx4Codes = 1024, kMx4Tile = kMx4Codes + 64;
 __host__ __device__ inline int64_t row_tiles(int M) { return ((int64_t)M + kTileRows - 1) / kTileRows; }
 __host__ __device__ inline int64_t col_tiles(int K) { return ((int64_t)K + kTileCols - 1) / kTileCols; }
 __host__ __device__ inline int tile_bytes(int format) { return format == DASH_MX4 ? kMx4Tile : kW8Tile; }
-__host__ __device__ inline int64_t matrix_bytes(int format, int M, int K) { return row_tiles(M) * col_tiles(K) * tile_bytes(format); }
+// 8-bit floats: codes in the tiles of the bytes, behind a matrix's tiles an int32 scale for every 128 x 128 (row blocks outermost)
+constexpr int kScaleBlock = 128;
+__host__ __device__ inline int64_t scale_blocks(int n) { return ((int64_t)n + kScaleBlock - 1) / kScaleBlock; }
+__host__ __device__ inline int64_t scales_at(int M, int K) { return row_tiles(M) * col_tiles(K) * kW8Tile; }
+__host__ __device__ inline int64_t matrix_bytes(int format, int M, int K) {
+    const int64_t scales = format == DASH_F8 ? (4 * scale_blocks(M) * scale_blocks(K) + 15) / 16 * 16 : 0;
+    return row_tiles(M) * col_tiles(K) * tile_bytes(format) + scales;
+}
+// 512 times the e4m3 magnitude of a code's low seven bits (0x7f, not a number: 0)
+__host__ __device__ inline uint32_t f8_magnitude(uint32_t code) {
+    const uint32_t m = code & 7, e = code >> 3 & 15;
+    return (code & 0x7f) == 0x7f ? 0 : e ? (8 + m) << (e - 1) : m;
+}
 // Where the 16-byte piece of columns 16 q .. 16 q + 15 (q = 0..3) of a row stands among the row's four: the pieces of one q in 8 or 16
 // consecutive rows, which a wave reads together, then lie in different banks.
 __host__ __device__ inline int w8_piece(int row, int q) { return q ^ ((row >> 1) & 3) ^ ((row >> 3) & 1); }
@@ -72,5 +84,6 @@ struct ExpertsCall {
     bool garble;
 };
 int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, hipStream_t s);
+int experts_mfma_f8(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, hipStream_t s);      // (dash_experts_f8.hip)
 
 }  // namespace dash

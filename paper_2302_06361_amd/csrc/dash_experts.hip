@@ -8,8 +8,10 @@
 //   k_route_count / _scan / _fill : rows sorted by expert, in order inside an expert
 //   k_weights8_prepare            : signed bytes into the tiles of the products
 //   k_mx4_quantise                : weights to 4-bit floats with a power of two for every 32, into the tiles of the products
+//   k_f8_quantise, k_f8_scales    : weights to 8-bit floats with an integer scale for every 128 x 128, into the same tiles as bytes
 //   (the products: dash_experts_gemm.hip)
 //   k_combine                     : the weighted sums
+#include <math.h>
 #include <string.h>
 
 #include "dash_experts.h"
@@ -109,6 +111,7 @@ struct PrepArgs8 {
     const int8_t* w;
     int64_t row_stride, expert_stride, tiles;       // tiles of all experts
     int64_t first;                                  // the launch's first lane
+    int64_t expert_bytes;                           // of a prepared matrix
     int M, K;
     uint8_t* out;
 };
@@ -127,7 +130,7 @@ __global__ __launch_bounds__(kThreads) void k_weights8_prepare(const PrepArgs8 A
             for (int i = 0; i < 16; i++)
                 if (col + i < A.K) v[i / 4] |= (uint32_t)(uint8_t)src[i] << (8 * (i % 4));
     }
-    *(uint4*)(A.out + tile * kW8Tile + w8_at(r, 16 * q)) = make_uint4(v[0], v[1], v[2], v[3]);
+    *(uint4*)(A.out + e * A.expert_bytes + at * kW8Tile + w8_at(r, 16 * q)) = make_uint4(v[0], v[1], v[2], v[3]);
 }
 
 struct QuantArgs {
@@ -149,6 +152,7 @@ struct QuantF32 {
     typedef v4f VecAny __attribute__((aligned(4)));
     static __device__ __forceinline__ float to(float v) { return v; }
     static __device__ __forceinline__ float from(float v) { return v; }
+    static __device__ __forceinline__ float round(float v) { return v; }
 };
 struct QuantBF16 {
     static constexpr int V = 8;
@@ -157,6 +161,7 @@ struct QuantBF16 {
     typedef v8s VecAny __attribute__((aligned(2)));
     static __device__ __forceinline__ float to(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ uint16_t from(float v) { return (uint16_t)(__float_as_uint(v) >> 16); }       // two significant bits: exact
+    static __device__ __forceinline__ uint16_t round(float v) { const uint32_t b = __float_as_uint(v); return (uint16_t)((b + 0x7fffu + (b >> 16 & 1)) >> 16); }     // to the nearest, ties to the even
 };
 struct QuantF16 {
     static constexpr int V = 8;
@@ -165,6 +170,7 @@ struct QuantF16 {
     typedef v8s VecAny __attribute__((aligned(2)));
     static __device__ __forceinline__ float to(uint16_t v) { return (float)__builtin_bit_cast(_Float16, v); }
     static __device__ __forceinline__ uint16_t from(float v) { return __builtin_bit_cast(uint16_t, (_Float16)v); }
+    static __device__ __forceinline__ uint16_t round(float v) { return from(v); }
 };
 // nibbles 0..3 of n to the low halves of the four bytes
 __device__ __forceinline__ uint32_t spread4(uint32_t n) {
@@ -270,6 +276,72 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
     if (threadIdx.x < kMx4Tile / 16) *(uint4*)(dst + 16 * threadIdx.x) = *(const uint4*)(to + 16 * threadIdx.x);
 }
 
+struct QuantF8Args {
+    const void* w;
+    int64_t row_stride, expert_stride, expert_bytes;
+    uint32_t first;             // the launch's first block of 128 x 128
+    int M, K, max_scale;
+    float unit, inverse;        // 2^base, 2^-base
+    uint8_t* out;
+    void* values;
+};
+// A block per 128 x 128 weights.
+template <class Q>
+__global__ __launch_bounds__(kThreads) void k_f8_quantise(const QuantF8Args A) {
+    typedef typename Q::T T;
+    const uint32_t block = A.first + blockIdx.x, kb = (uint32_t)scale_blocks(A.K), mb = (uint32_t)scale_blocks(A.M);
+    const uint32_t rb = block / kb, e = rb / mb;
+    const int row0 = (int)(rb - e * mb) * kScaleBlock, col0 = (int)(block - rb * kb) * kScaleBlock;
+    const T* const src = (const T*)A.w + (int64_t)e * A.expert_stride;
+    __shared__ uint32_t part[kWaves];
+    auto weight = [&](int row, int col) {
+        float x = row < A.M && col < A.K ? Q::to(src[(int64_t)row * A.row_stride + col]) : 0.0f;
+        return x == x ? fminf(fmaxf(x, -3.4028234663852886e38f), 3.4028234663852886e38f) : 0.0f;
+    };
+    uint32_t amax = 0;
+    for (int i = threadIdx.x; i < kScaleBlock * kScaleBlock; i += kThreads) {
+        const uint32_t a = __float_as_uint(weight(row0 + i / kScaleBlock, col0 + i % kScaleBlock)) & 0x7fffffffu;
+        amax = a > amax ? a : amax;
+    }
+    for (int d = 32; d; d /= 2) { const uint32_t o = (uint32_t)__shfl_xor((int)amax, d); amax = o > amax ? o : amax; }
+    if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = amax;
+    __syncthreads();
+    for (int i = 0; i < kWaves; i++) amax = part[i] > amax ? part[i] : amax;
+    // the smallest S with 448 S >= a: 448 * 32767 < 2^24, so both sides are exact
+    const float a = __uint_as_float(amax) * A.inverse;
+    float S = fminf(ceilf(a / 448.0f), (float)A.max_scale);
+    if (S > 1 && 448.0f * (S - 1) >= a) S -= 1;
+    if (448.0f * S < a) S += 1;
+    S = fminf(fmaxf(S, 1.0f), (float)A.max_scale);
+    uint8_t* const out = A.out + (int64_t)e * A.expert_bytes;
+    if (threadIdx.x == 0) ((int32_t*)(out + scales_at(A.M, A.K)))[rb % mb * kb + block % kb] = (int32_t)S;
+    const int64_t kt = col_tiles(A.K);
+    for (int i = threadIdx.x; i < kScaleBlock * kScaleBlock; i += kThreads) {
+        const int row = row0 + i / kScaleBlock, col = col0 + i % kScaleBlock;
+        if (row / kTileRows >= row_tiles(A.M) || col / kTileCols >= kt) continue;
+        // the quotient of 24 bits by 15 rounds to the middle of two e4m3 values only where it is that
+        const float q = fminf(fmaxf(weight(row, col) * A.inverse / S, -448.0f), 448.0f);
+        uint32_t code = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q, q, 0, false) & 0xffu;
+        if (!(code & 0x7f)) code = 0;
+        out[(row / kTileRows * kt + col / kTileCols) * kW8Tile + w8_at(row % kTileRows, col % kTileCols)] = (uint8_t)code;
+        if (A.values && row < A.M && col < A.K)
+            ((T*)A.values)[((int64_t)e * A.M + row) * A.K + col] = Q::round((code & 0x80 ? -1.0f : 1.0f) * (float)f8_magnitude(code & 0x7f) * S * (A.unit / 512.0f));
+    }
+}
+struct ScalesArgs {
+    const int32_t* scales;
+    int64_t at, expert_bytes;   // of the scales in a matrix; bytes of a matrix
+    int64_t first, total;
+    uint32_t blocks;            // of a matrix
+    uint8_t* out;
+};
+__global__ __launch_bounds__(kThreads) void k_f8_scales(const ScalesArgs A) {
+    const int64_t i = A.first + (int64_t)blockIdx.x * kThreads + threadIdx.x;
+    if (i >= A.total) return;
+    const int64_t e = i / A.blocks;
+    ((int32_t*)(A.out + e * A.expert_bytes + A.at))[i - e * A.blocks] = A.scales[i];
+}
+
 __device__ __forceinline__ uint32_t signed_mod(int32_t v, const ModInfo& M) {
     const int32_t r = v % (int32_t)M.m;
     return (uint32_t)(r < 0 ? r + (int32_t)M.m : r);
@@ -319,11 +391,13 @@ template <class Launch> static void in_launches(int64_t blocks, Launch launch) {
     for (int64_t first = 0; first < blocks; first += most) launch(first, (uint32_t)(blocks - first < most ? blocks - first : most));
 }
 
+static bool weight_format(int f) { return f == DASH_W8 || f == DASH_MX4 || f == DASH_F8; }
+
 int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labels* in, dash_labels* out, hipStream_t s) {
     int st = layer_sizes(c, L, nullptr, nullptr, nullptr);
     if (st) return st;
     if (L->n_elem == 0) return DASH_OK;         // (empty bundles and gates may have no address)
-    if (!L->weights || ((uintptr_t)L->weights & 15) || (L->weight_format != DASH_W8 && L->weight_format != DASH_MX4)) return DASH_EINVAL;
+    if (!L->weights || ((uintptr_t)L->weights & 15) || !weight_format(L->weight_format)) return DASH_EINVAL;
     const int64_t n = L->n_elem, T = n / L->top_k;
     const int M = L->out_c, K = L->in_c, E = L->n_experts;
     if (T > 0x7fffffff / K || n > 0x7fffffff / M || K > 1 << 26) return DASH_ESIZE;        // (offsets inside a row of weights or a row's labels: 32 bits)
@@ -379,6 +453,19 @@ static int64_t weight_tiles(const void* w, int64_t row_stride, int64_t expert_st
     return row_tiles(out_c) * col_tiles(K) * n_experts;
 }
 
+// bytes, or 8-bit codes, into their tiles
+static int lay_out_bytes(int format, const int8_t* w, int64_t row_stride, int64_t expert_stride, int64_t tiles, int out_c, int K, void* prepared, hipStream_t s) {
+    const int64_t lanes = tiles * (kW8Tile / 16);
+    if (lanes > kMaxLanes) return DASH_ESIZE;
+    PrepArgs8 A{w, row_stride, expert_stride, tiles, 0, matrix_bytes(format, out_c, K), out_c, K, (uint8_t*)prepared};
+    in_launches((lanes + kThreads - 1) / kThreads, [&](int64_t first, uint32_t blocks) {
+        A.first = first * kThreads;
+        hipLaunchKernelGGL(k_weights8_prepare, dim3(blocks), dim3(kThreads), 0, s, A);
+    });
+    DASH_HIP(hipGetLastError());
+    return DASH_OK;
+}
+
 }  // namespace dash
 
 using namespace dash;
@@ -386,7 +473,7 @@ using namespace dash;
 extern "C" {
 
 size_t dash_expert_weights_bytes(int format, int n_experts, int out_c, int K) {
-    if ((format != DASH_W8 && format != DASH_MX4) || n_experts < 1 || out_c < 1 || K < 1) return 0;
+    if (!weight_format(format) || n_experts < 1 || out_c < 1 || K < 1) return 0;
     return (size_t)n_experts * (size_t)matrix_bytes(format, out_c, K);
 }
 
@@ -395,12 +482,40 @@ int dash_weights8_prepare(dash_ctx* c, const int8_t* w, int64_t row_stride, int6
     if (!c) return DASH_EINVAL;
     const int64_t tiles = weight_tiles(w, row_stride, expert_stride, n_experts, out_c, K, prepared);
     if (!tiles) return DASH_EINVAL;
-    const int64_t lanes = tiles * (kW8Tile / 16);
-    if (lanes > kMaxLanes) return DASH_ESIZE;
-    PrepArgs8 A{w, row_stride, expert_stride, tiles, 0, out_c, K, (uint8_t*)prepared};
-    in_launches((lanes + kThreads - 1) / kThreads, [&](int64_t first, uint32_t blocks) {
+    return lay_out_bytes(DASH_W8, w, row_stride, expert_stride, tiles, out_c, K, prepared, (hipStream_t)stream);
+}
+
+int dash_f8_prepare(dash_ctx* c, const uint8_t* codes, int64_t row_stride, int64_t expert_stride, const int32_t* scales, int n_experts, int out_c, int K,
+                    void* prepared, void* stream) {
+    if (!c || !scales || ((uintptr_t)scales & 3)) return DASH_EINVAL;
+    const int64_t tiles = weight_tiles(codes, row_stride, expert_stride, n_experts, out_c, K, prepared);
+    if (!tiles) return DASH_EINVAL;
+    const int64_t per = scale_blocks(out_c) * scale_blocks(K);
+    if (per > 0x7fffffff) return DASH_ESIZE;
+    const int st = lay_out_bytes(DASH_F8, (const int8_t*)codes, row_stride, expert_stride, tiles, out_c, K, prepared, (hipStream_t)stream);
+    if (st) return st;
+    ScalesArgs A{scales, scales_at(out_c, K), matrix_bytes(DASH_F8, out_c, K), 0, per * n_experts, (uint32_t)per, (uint8_t*)prepared};
+    in_launches((A.total + kThreads - 1) / kThreads, [&](int64_t first, uint32_t blocks) {
         A.first = first * kThreads;
-        hipLaunchKernelGGL(k_weights8_prepare, dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, A);
+        hipLaunchKernelGGL(k_f8_scales, dim3(blocks), dim3(kThreads), 0, (hipStream_t)stream, A);
+    });
+    DASH_HIP(hipGetLastError());
+    return DASH_OK;
+}
+
+int dash_f8_quantise(dash_ctx* c, const void* w, int dtype, int64_t row_stride, int64_t expert_stride, int n_experts, int out_c, int K, int base,
+                     int max_scale, void* prepared, void* values, void* stream) {
+    if (!c || dtype < DASH_F32 || dtype > DASH_F16 || base < -64 || base > 64 || max_scale < 1 || max_scale > 32767) return DASH_EINVAL;
+    const uintptr_t unaligned = dtype == DASH_F32 ? 3 : 1;
+    if (((uintptr_t)w & unaligned) || ((uintptr_t)values & unaligned)) return DASH_EINVAL;
+    if (!weight_tiles(w, row_stride, expert_stride, n_experts, out_c, K, prepared)) return DASH_EINVAL;
+    const int64_t blocks = scale_blocks(out_c) * scale_blocks(K) * n_experts;
+    if (blocks > 0x7fffffff) return DASH_ESIZE;
+    QuantF8Args A{w, row_stride, expert_stride, matrix_bytes(DASH_F8, out_c, K), 0, out_c, K, max_scale, ldexpf(1.0f, base), ldexpf(1.0f, -base), (uint8_t*)prepared, values};
+    auto kernel = dtype == DASH_F32 ? k_f8_quantise<QuantF32> : dtype == DASH_BF16 ? k_f8_quantise<QuantBF16> : k_f8_quantise<QuantF16>;
+    in_launches(blocks, [&](int64_t first, uint32_t n) {
+        A.first = (uint32_t)first;
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, (hipStream_t)stream, A);
     });
     DASH_HIP(hipGetLastError());
     return DASH_OK;
