@@ -71,7 +71,7 @@ enum {
 /* Weights of an EXPERTS layer: signed bytes, 4-bit floats with a shared power of two for every 32, or 8-bit floats with an integer
  * scale for every block of 128 x 128. */
 enum { DASH_W8 = 0, DASH_MX4 = 1, DASH_F8 = 8 };
-/* Types of the weights that dash_mx4_quantise and dash_f8_quantise read. */
+/* Types of the weights that dash_mx4_quantise and dash_f8_quantise read, and of the logits that dash_choose reads. */
 enum { DASH_F32 = 0, DASH_BF16 = 1, DASH_F16 = 2 };
 
 typedef struct dash_ctx dash_ctx;
@@ -211,6 +211,33 @@ int dash_f8_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_stride
  * [n_experts][ceil(out_c / 128)][ceil(K / 128)], any values. */
 int dash_f8_prepare(dash_ctx *ctx, const uint8_t *codes, int64_t row_stride, int64_t expert_stride, const int32_t *scales, int n_experts,
                     int out_c, int K, void *prepared, void *hip_stream);
+/* Experts and gates from a router's logits, public values as everything that a circuit is routed by. */
+enum { DASH_SOFTMAX = 0, DASH_SIGMOID = 1 };
+enum { DASH_GROUP_MAX = 0, DASH_GROUP_PAIR = 1 };
+#define DASH_MAX_ROUTED 1024    /* experts */
+#define DASH_MAX_TOP_K 32
+typedef struct {
+    int32_t n_experts, top_k;
+    int32_t score;                      /* DASH_SOFTMAX (over the experts of a row) or DASH_SIGMOID */
+    int32_t n_groups, top_groups;       /* equal groups of neighbouring experts (at most 64), and how many of them experts are chosen from */
+    int32_t group_score;                /* a group counts as its largest choice value, or the sum of its two largest (DASH_GROUP_PAIR) */
+    int32_t renormalise;                /* != 0: weights are divided by the sum of a row's chosen scores */
+    int32_t gate_bits;                  /* 0..30; scale * 2^gate_bits at most 2^30 */
+    float scale;                        /* > 0 */
+    const float *bias;                  /* device [n_experts] or NULL: added to the scores for the choice, not in the weights */
+} dash_router;
+/* logits: device, n rows of n_experts `dtype` elements (DASH_F32, DASH_BF16, DASH_F16), row_stride (>= n_experts) elements apart.  Of every row: scores s = softmax(l)
+ * or sigmoid(l); choice values c = s + bias, without a bias the order of l (groups of DASH_GROUP_PAIR: sums of s); the top_groups groups
+ * with the largest value; of their experts the top_k with the largest c, in descending order.  Ties go to the lower number.  Weights w =
+ * scale * s (renormalise: / sum of the chosen s, zero if that is zero), gates = w * 2^gate_bits to the nearest integer, ties to the even.  Scores, sums, choice
+ * values and weights are held in 64 bits.
+ * A logit that is not a number counts as -infinity, infinity as the largest float32.  Experts whose logit is -infinity, or whose choice value is -infinity or no number, are
+ * never chosen; groups without any other are not either.  valid: device, a byte for every row, 0: no expert is chosen (NULL: all rows are valid).  What is missing of
+ * top_k: expert -1, weight and gate 0.
+ * experts, gates, weights: device [n][top_k]; gates and weights may be NULL.  experts is what dash_route takes (rows n * top_k), gates what COMBINE does.
+ * DASH_ESIZE: more than DASH_MAX_ROUTED experts, DASH_MAX_TOP_K of them chosen or 64 groups. */
+int dash_choose(dash_ctx *ctx, const dash_router *router, const void *logits, int dtype, int64_t row_stride, int64_t n, const uint8_t *valid,
+                int32_t *experts, int32_t *gates, float *weights, void *hip_stream);
 /* Sorts rows by expert: experts: device int32 [n], the expert of every row in [0, n_experts); any other number: no expert, the
  * row's outputs are all-zero labels on both sides (the value 0, no bias).  Fills *routing, which the caller keeps (with `data`) as long as layers refer
  * to it; one routing serves garbler and evaluator, and every layer over the same rows.  `experts` may be changed once the stream

@@ -16,12 +16,14 @@ MAX_DIGITS = 16
 DENSE, CONV2D, SUMPOOL, RELU, SCALE, SIGN, PROJ, EXPERTS, COMBINE = 1, 2, 3, 4, 5, 6, 7, 8, 9
 W8, MX4, F8 = 0, 1, 8
 F32, BF16, F16 = 0, 1, 2
+SOFTMAX, SIGMOID = 0, 1
+GROUP_MAX, GROUP_PAIR = 0, 1
 LAMBDA_CEIL, LAMBDA_FLOOR = 0, 1
 NOALLOC_SCRATCH_BYTES = 32 << 20
 
 SYMBOLS = ["dash_ctx_create", "dash_ctx_destroy", "dash_lambda", "dash_ctx_offset", "dash_ctx_one", "dash_ctx_digits",
            "dash_layer_sizes", "dash_weights_bytes", "dash_weights_prepare", "dash_expert_weights_bytes", "dash_weights8_prepare",
-           "dash_mx4_quantise", "dash_f8_quantise", "dash_f8_prepare", "dash_route_bytes", "dash_route", "dash_garble_layer", "dash_eval_layer",
+           "dash_mx4_quantise", "dash_f8_quantise", "dash_f8_prepare", "dash_choose", "dash_route_bytes", "dash_route", "dash_garble_layer", "dash_eval_layer",
            "dash_garble_layers", "dash_eval_layers", "dash_eval_layer_noalloc", "dash_input_labels", "dash_encode", "dash_decode", "dash_labels_pack", "dash_labels_unpack", "dash_tables_packed_bytes", "dash_tables_pack", "dash_tables_unpack", "dash_strerror", "dash_profile_enable", "dash_profile_read", "dash_profile_aes"]
 
 
@@ -55,6 +57,11 @@ class CRouting(C.Structure):
     _fields_ = [("data", C.c_void_p), ("ctx", C.c_void_p), ("n", C.c_int64), ("n_experts", C.c_int32)]
 
 
+class CRouter(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_experts", "top_k", "score", "n_groups", "top_groups", "group_score", "renormalise", "gate_bits")] + \
+               [("scale", C.c_float), ("bias", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -77,6 +84,7 @@ def lib():
         L.dash_mx4_quantise.argtypes = [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64] + [C.c_int] * 5 + [C.c_void_p] * 3
         L.dash_f8_quantise.argtypes = L.dash_mx4_quantise.argtypes
         L.dash_f8_prepare.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 2
+        L.dash_choose.argtypes = [C.c_void_p] * 3 + [C.c_int, C.c_int64, C.c_int64] + [C.c_void_p] * 5
         L.dash_route_bytes.restype = C.c_size_t
         L.dash_ctx_destroy.restype = None
         _lib = L
@@ -199,6 +207,30 @@ class Routing:
 
     def address(self):
         return C.addressof(self.c)
+
+
+class Router:
+    """A dash_router: how Context.choose takes top_k of n_experts from a row's logits.  bias: float32 tensor [n_experts] on the device, added to
+    the scores for the choice; groups: equal groups of experts, of which the top_groups best ones (group_score) are chosen from."""
+
+    def __init__(self, n_experts, top_k, score=SOFTMAX, bias=None, groups=1, top_groups=1, group_score=GROUP_MAX, renormalise=True, scale=1.0, gate_bits=8):
+        self.c = CRouter(int(n_experts), int(top_k), int(score), int(groups), int(top_groups), int(group_score), int(bool(renormalise)), int(gate_bits), float(scale))
+        self.n_experts, self.top_k, self.bias = int(n_experts), int(top_k), bias
+        if bias is not None:
+            import torch
+            if bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != self.n_experts:
+                raise DashError("Router: bias has to be a contiguous float32 tensor [n_experts]")
+            self.c.bias = bias.data_ptr()
+
+
+class Choice:
+    """What Context.choose fills for n rows: experts (int32 [n][top_k], -1: none), gates (int32, what COMBINE layers take), weights (float32)."""
+
+    def __init__(self, ctx, n, top_k):
+        import torch
+        self.n, self.top_k = int(n), int(top_k)
+        self.experts, self.gates = (torch.empty((self.n, self.top_k), dtype=torch.int32, device=ctx.device) for _ in range(2))
+        self.weights = torch.empty((self.n, self.top_k), dtype=torch.float32, device=ctx.device)
 
 
 class Layer:
@@ -394,6 +426,29 @@ class Context:
             raise DashError("f8_prepare: contiguous int32 scales %s on %s expected, got %s %s on %s" % (list(blocks), self.device, scales.dtype, list(scales.shape), scales.device))
         out = self._expert_out(out, F8, shape, "f8_prepare")
         _check(self.L.dash_f8_prepare(self.h, codes.data_ptr(), stride[1], stride[0], scales.data_ptr(), *shape, out.data.data_ptr(), _stream()), "dash_f8_prepare")
+        return out
+
+    def choose(self, router, logits, valid=None, out=None):
+        """logits: float32, bfloat16 or float16 tensor [n][n_experts] on the device, rows contiguous; valid: bytes or truth values [n], rows of no
+        expert false -> Choice"""
+        types = self._types or self._float_types()
+        shape, stride = logits.shape, logits.stride()
+        E = router.n_experts
+        if len(shape) != 2 or shape[1] != E or logits.dtype not in types or logits.device != self.device or (stride[1] != 1 and E > 1) or (stride[0] < E and shape[0] > 1):
+            raise DashError("choose: logits [n][%d] with contiguous rows on %s expected, got %s %s on %s" % (E, self.device, logits.dtype, tuple(shape), logits.device))
+        n = shape[0]
+        if router.bias is not None and router.bias.device != self.device:
+            raise DashError("choose: the router's bias is on %s" % router.bias.device)
+        if valid is not None and (valid.itemsize != 1 or valid.numel() != n or valid.device != self.device or not valid.is_contiguous()):
+            raise DashError("choose: `valid` has to be a contiguous tensor of %d bytes or truth values on %s" % (n, self.device))
+        if out is None:
+            out = Choice(self, n, router.top_k)
+        elif out.n != n or out.top_k != router.top_k or out.experts.device != self.device:
+            raise DashError("choose: `out` was made for another number of rows or experts")
+        st = self.L.dash_choose(self.h, C.addressof(router.c), logits.data_ptr(), types[logits.dtype], max(stride[0], E), n, None if valid is None else valid.data_ptr(),
+                                out.experts.data_ptr(), out.gates.data_ptr(), out.weights.data_ptr(), _stream())
+        if st != 0:
+            _check(st, "dash_choose")
         return out
 
     def route(self, experts, n_experts, out=None):
