@@ -33,7 +33,11 @@ def build_layers(ctx, net, b, batch_base):
             lay.per_batch_element = n
         elif kind == "experts":
             # rows of a batch element, each through the matrix of its (public) expert
-            if L.get("base") is None:
+            if L.get("scales") is not None:
+                w = ctx.f8_prepare(torch.as_tensor(_integers(L["codes"], np.uint8, "codes")).to(ctx.device), torch.as_tensor(_integers(L["scales"], np.int32, "scales")).to(ctx.device))
+            elif L.get("max_scale") is not None:
+                w = ctx.f8_quantise(torch.as_tensor(np.ascontiguousarray(L["W"], dtype=np.float32)).to(ctx.device), L["base"], L["max_scale"])
+            elif L.get("base") is None:
                 w = ctx.weights8_prepare(torch.as_tensor(_integers(L["W"], np.int8, "W")).to(ctx.device))
             else:
                 w = ctx.mx4_quantise(torch.as_tensor(np.ascontiguousarray(L["W"], dtype=np.float32)).to(ctx.device), L["base"], L["max_shift"])
@@ -41,7 +45,11 @@ def build_layers(ctx, net, b, batch_base):
             if L.get("bias") is not None:
                 bias = torch.as_tensor(_integers(L["bias"], np.int32, "bias")).to(ctx.device)
             routing = None
-            if L.get("route") is not None:
+            if L.get("router") is not None:
+                routing = _Routed(L["router"], L["rows"], ctx, b, "experts")
+                if routing.router.n_experts != w.n_experts:
+                    raise ValueError("router: logits of %d experts, the layer has %d" % (routing.router.n_experts, w.n_experts))
+            elif L.get("route") is not None:
                 routing = _PerBatch(L["route"], L["rows"], ctx, "route")
             lay = B.Layer(B.EXPERTS, L["id"], b * L["rows"], top_k=L["top_k"], weights=w, bias=bias)
             if routing is not None:
@@ -49,7 +57,7 @@ def build_layers(ctx, net, b, batch_base):
                 lay.c.routing = lay.routing.address()
                 lay.rebase = lambda base, lay=lay, r=routing, e=w.n_experts: ctx.route(r.part(base, b), e, out=lay.routing)
         elif kind == "combine":
-            gates = _PerBatch(L["gates"], L["rows"] * L["top_k"], ctx, "gates")
+            gates = _Routed(L["router"], L["rows"] * L["top_k"], ctx, b, "gates") if L.get("router") is not None else _PerBatch(L["gates"], L["rows"] * L["top_k"], ctx, "gates")
             part = gates.part(batch_base, b).clone()
             lay = B.Layer(B.COMBINE, L["id"], b * L["rows"], in_c=L["V"], top_k=L["top_k"], gates=part)
             lay.rebase = lambda base, part=part, g=gates: part.copy_(g.part(base, b))
@@ -91,6 +99,30 @@ class _PerBatch:
         if (base + b) * self.per > self.all.numel():
             raise ValueError("experts or gates of batch elements %d..%d are missing" % (base, base + b - 1))
         return self.all[base * self.per:(base + b) * self.per]
+
+
+class _Routed:
+    """experts or gates that a router chooses from the logits of the whole batch, top_k for every batch element"""
+
+    def __init__(self, router, per, ctx, b, what):
+        import torch
+        given = dict(router)
+        logits, bias, valid = given.pop("logits"), given.pop("bias", None), given.pop("valid", None)
+        self.ctx, self.what, self.b = ctx, what, b
+        self.logits = torch.as_tensor(np.ascontiguousarray(logits, dtype=np.float32)).to(ctx.device)
+        self.valid = None if valid is None else torch.as_tensor(np.ascontiguousarray(valid, dtype=np.uint8)).to(ctx.device)
+        if bias is not None:
+            bias = torch.as_tensor(np.ascontiguousarray(bias, dtype=np.float32)).to(ctx.device)
+        self.router = B.Router(self.logits.shape[1], bias=bias, **given)
+        if self.router.top_k != per:
+            raise ValueError("router: top_k is %d, the layer takes %d rows of a batch element" % (self.router.top_k, per))
+        self.choice = B.Choice(ctx, b, per)
+
+    def part(self, base, b):
+        if base + b > len(self.logits) or (self.valid is not None and base + b > len(self.valid)) or b != self.b:
+            raise ValueError("router: logits of batch elements %d..%d are missing" % (base, base + b - 1))
+        valid = None if self.valid is None else self.valid[base:base + b]
+        return getattr(self.ctx.choose(self.router, self.logits[base:base + b], valid=valid, out=self.choice), self.what).view(-1)
 
 
 class GarbledNetwork:

@@ -88,3 +88,22 @@ def test_binding_refuses(monkeypatch):
         with pytest.raises(DashError, match="out"):
             call(r, good, out=out)
     assert ctx.calls == calls
+
+
+def test_network_refuses_routers_of_another_size():
+    import numpy as np
+    from paper_2302_06361_amd import network
+    from test_expert_arguments import Weights
+    ctx = Weights()
+    ctx.choose = ctx.route = lambda *a, **k: None
+    ctx.weights8_prepare = lambda w: type("W", (), dict(n_experts=3, data_ptr=lambda: 16))
+    ctx.device = torch.device("cpu")
+    layer = dict(kind="experts", id=1, rows=2, top_k=2, W=np.zeros((3, 4, 3), np.int8), router=dict(logits=np.zeros((5, 3)), top_k=1))
+    with pytest.raises(ValueError, match="top_k"):
+        network.build_layers(ctx, dict(n_in=3, layers=[layer]), 5, 0)
+    layer["router"] = dict(logits=np.zeros((5, 4)), top_k=2)
+    with pytest.raises(ValueError, match="experts"):
+        network.build_layers(ctx, dict(n_in=3, layers=[layer]), 5, 0)
+    layer["router"] = dict(logits=np.zeros((5, 3)), top_k=2)
+    with pytest.raises(ValueError, match="logits"):
+        network.build_layers(ctx, dict(n_in=3, layers=[layer]), 6, 0)

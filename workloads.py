@@ -176,9 +176,10 @@ def tiny_cnn(seed=8, k=4, batch=2, repeat=1):
     return b.net
 
 
-def mixture(seed=9, batch=4, k=8, n_in=48, hidden=32, n_out=10, experts=4, top_k=2, repeat=3, mx4=True):
+def mixture(seed=9, batch=4, k=8, n_in=48, hidden=32, n_out=10, experts=4, top_k=2, repeat=3, mx4=True, f8=False, router=None):
     """A mixture of experts with public routing: dense, ReLU, scale, then per batch element top_k two-layer experts (4-bit or
-    8-bit weights, ReLU and scale between), joined with integer gates, dense.  One row has no expert."""
+    8-bit weights, ReLU and scale between), joined with integer gates, dense.  One row has no expert.  f8: 8-bit floating point weights, which take the 12-prime
+    base and longer scales.  router: how experts and gates are chosen from logits (the arguments of Router and, by default, random logits) instead."""
     b = _Builder(seed, k, batch, n_in, -7, 7)
     g = b.g
     b.net["x"] = g.integers(0, 16, batch * n_in).astype(np.int64)
@@ -188,17 +189,23 @@ def mixture(seed=9, batch=4, k=8, n_in=48, hidden=32, n_out=10, experts=4, top_k
         route[3] = -1
 
     def matrices(M, K):
+        if f8:
+            return dict(W=g.standard_normal((experts, M, K)).astype(np.float32), base=-8, max_scale=255)
         if not mx4:
             return dict(W=g.integers(-8, 8, (experts, M, K)).astype(np.int8))
         return dict(W=g.standard_normal((experts, M, K)).astype(np.float32), base=-2, max_shift=2)
-    b._add(dict(kind="experts", id=b.lid(), rows=top_k, top_k=top_k, route=route, **matrices(2 * hidden, hidden)))
+    routed = dict(route=route)
+    if router is not None:
+        router = dict(dict(logits=g.standard_normal((batch, experts)).astype(np.float32), top_k=top_k, gate_bits=4), **router)
+        routed = dict(router=router)
+    b._add(dict(kind="experts", id=b.lid(), rows=top_k, top_k=top_k, **routed, **matrices(2 * hidden, hidden)))
     b.n = top_k * 2 * hidden
-    b.relu(); b.scale(repeat)
-    b._add(dict(kind="experts", id=b.lid(), rows=top_k, top_k=1, route=route, bias=g.integers(-20, 20, (experts, hidden)).astype(np.int32),
+    b.relu(); b.scale(16 if f8 else repeat)
+    b._add(dict(kind="experts", id=b.lid(), rows=top_k, top_k=1, bias=g.integers(-20, 20, (experts, hidden)).astype(np.int32), **routed,
                 **matrices(hidden, 2 * hidden)))
-    b._add(dict(kind="combine", id=b.lid(), rows=1, top_k=top_k, V=hidden, gates=g.integers(0, 4, (batch, top_k)).astype(np.int32)))
+    b._add(dict(kind="combine", id=b.lid(), rows=1, top_k=top_k, V=hidden, **(routed if router is not None else dict(gates=g.integers(0, 4, (batch, top_k)).astype(np.int32)))))
     b.n = hidden
-    b.relu(); b.scale(repeat)
+    b.relu(); b.scale(20 if f8 else repeat)
     b.dense(n_out)
     return b.net
 
