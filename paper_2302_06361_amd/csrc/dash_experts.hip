@@ -276,6 +276,7 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
     if (threadIdx.x < kMx4Tile / 16) *(uint4*)(dst + 16 * threadIdx.x) = *(const uint4*)(to + 16 * threadIdx.x);
 }
 
+constexpr int kF8Threads = 512;
 struct QuantF8Args {
     const void* w;
     int64_t row_stride, expert_stride, expert_bytes;
@@ -285,47 +286,100 @@ struct QuantF8Args {
     uint8_t* out;
     void* values;
 };
-// A block per 128 x 128 weights.
+// A block per 128 x 128 weights: they are read once, 16 bytes a lane, all loads out before the first is waited for, and stay in registers while the block finds its largest
+// magnitude.  Quotients: with y = 1 / S rounded to nearest, q = x y and the remainder x - q S, exact, q + (x - q S) y is x / S rounded to nearest (Markstein); of 24 bits by
+// 15 that is the middle of two e4m3 values only where x / S is.  v_cvt_pk_fp8_f32 rounds two at a time (nearest, ties to even); a lane's codes are neighbours in their tile.
 template <class Q>
-__global__ __launch_bounds__(kThreads) void k_f8_quantise(const QuantF8Args A) {
+__global__ __launch_bounds__(kF8Threads) void k_f8_quantise(const QuantF8Args A) {
+    constexpr int V = Q::V, kRowLanes = kScaleBlock / V, kRows = kF8Threads / kRowLanes, kSteps = kScaleBlock / kRows;
     typedef typename Q::T T;
+    typedef typename Q::VecAny VecAny;
     const uint32_t block = A.first + blockIdx.x, kb = (uint32_t)scale_blocks(A.K), mb = (uint32_t)scale_blocks(A.M);
     const uint32_t rb = block / kb, e = rb / mb;
     const int row0 = (int)(rb - e * mb) * kScaleBlock, col0 = (int)(block - rb * kb) * kScaleBlock;
-    const T* const src = (const T*)A.w + (int64_t)e * A.expert_stride;
-    __shared__ uint32_t part[kWaves];
-    auto weight = [&](int row, int col) {
-        float x = row < A.M && col < A.K ? Q::to(src[(int64_t)row * A.row_stride + col]) : 0.0f;
-        return x == x ? fminf(fmaxf(x, -3.4028234663852886e38f), 3.4028234663852886e38f) : 0.0f;
-    };
-    uint32_t amax = 0;
-    for (int i = threadIdx.x; i < kScaleBlock * kScaleBlock; i += kThreads) {
-        const uint32_t a = __float_as_uint(weight(row0 + i / kScaleBlock, col0 + i % kScaleBlock)) & 0x7fffffffu;
-        amax = a > amax ? a : amax;
+    const int r0 = threadIdx.x / kRowLanes, col = col0 + (int)threadIdx.x % kRowLanes * V, have = A.K - col;
+    const int rows = A.M - row0 < kScaleBlock ? A.M - row0 : kScaleBlock;
+    const T* const src = (const T*)A.w + (int64_t)e * A.expert_stride + (int64_t)row0 * A.row_stride;
+    __shared__ uint32_t part[kF8Threads / 64];
+    typename Q::Vec in[kSteps];
+    if (col0 + kScaleBlock <= A.K) {
+#pragma unroll
+        for (int s = 0; s < kSteps; s++)
+            if (s * kRows < rows) in[s] = *(const VecAny*)(src + (int64_t)(r0 + s * kRows < rows ? r0 + s * kRows : rows - 1) * A.row_stride + col);
+    } else {
+#pragma unroll
+        for (int s = 0; s < kSteps; s++)
+            if (s * kRows < rows) {
+#pragma unroll
+                for (int i = 0; i < V; i++) in[s][i] = src[(int64_t)(r0 + s * kRows < rows ? r0 + s * kRows : rows - 1) * A.row_stride + (i < have ? col + i : A.K - 1)];
+            }
     }
-    for (int d = 32; d; d /= 2) { const uint32_t o = (uint32_t)__shfl_xor((int)amax, d); amax = o > amax ? o : amax; }
+    // (rows and columns past the end repeat others: the magnitude is theirs)
+    auto number = [](float x) __attribute__((always_inline)) { return x == x ? x : 0.0f; };
+    float top = 0;
+#pragma unroll
+    for (int s = 0; s < kSteps; s++)
+        if (s * kRows < rows) {
+#pragma unroll
+            for (int i = 0; i < V; i++) top = fmaxf(top, fabsf(Q::to(in[s][i])));       // (fmaxf leaves out what is not a number)
+        }
+    uint32_t amax = __float_as_uint(top);
+#pragma unroll
+    for (int d = 32; d; d /= 2) {
+        const uint32_t o = d == 2 ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0x4E, 0xf, 0xf, true) : d == 1 ? (uint32_t)__builtin_amdgcn_update_dpp(0, (int)amax, 0xB1, 0xf, 0xf, true)
+                         : (uint32_t)__shfl_xor((int)amax, d);
+        amax = o > amax ? o : amax;
+    }
     if (threadIdx.x % 64 == 0) part[threadIdx.x / 64] = amax;
     __syncthreads();
-    for (int i = 0; i < kWaves; i++) amax = part[i] > amax ? part[i] : amax;
+#pragma unroll
+    for (int i = 0; i < kF8Threads / 64; i++) amax = part[i] > amax ? part[i] : amax;
+    amax = (uint32_t)__builtin_amdgcn_readfirstlane((int)amax);
     // the smallest S with 448 S >= a: 448 * 32767 < 2^24, so both sides are exact
-    const float a = __uint_as_float(amax) * A.inverse;
+    const float a = fminf(__uint_as_float(amax), 3.4028234663852886e38f) * A.inverse;
     float S = fminf(ceilf(a / 448.0f), (float)A.max_scale);
     if (S > 1 && 448.0f * (S - 1) >= a) S -= 1;
     if (448.0f * S < a) S += 1;
     S = fminf(fmaxf(S, 1.0f), (float)A.max_scale);
     uint8_t* const out = A.out + (int64_t)e * A.expert_bytes;
-    if (threadIdx.x == 0) ((int32_t*)(out + scales_at(A.M, A.K)))[rb % mb * kb + block % kb] = (int32_t)S;
+    if (threadIdx.x == 0) ((int32_t*)(out + scales_at(A.M, A.K)))[(rb - e * mb) * kb + (block - rb * kb)] = (int32_t)S;
     const int64_t kt = col_tiles(A.K);
-    for (int i = threadIdx.x; i < kScaleBlock * kScaleBlock; i += kThreads) {
-        const int row = row0 + i / kScaleBlock, col = col0 + i % kScaleBlock;
-        if (row / kTileRows >= row_tiles(A.M) || col / kTileCols >= kt) continue;
-        // the quotient of 24 bits by 15 rounds to the middle of two e4m3 values only where it is that
-        const float q = fminf(fmaxf(weight(row, col) * A.inverse / S, -448.0f), 448.0f);
-        uint32_t code = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q, q, 0, false) & 0xffu;
-        if (!(code & 0x7f)) code = 0;
-        out[(row / kTileRows * kt + col / kTileCols) * kW8Tile + w8_at(row % kTileRows, col % kTileCols)] = (uint8_t)code;
-        if (A.values && row < A.M && col < A.K)
-            ((T*)A.values)[((int64_t)e * A.M + row) * A.K + col] = Q::round((code & 0x80 ? -1.0f : 1.0f) * (float)f8_magnitude(code & 0x7f) * S * (A.unit / 512.0f));
+    const float y = 1.0f / S, most = 448.0f * S, unit = S * A.unit;
+    const int tile_rows = (rows + kTileRows - 1) / kTileRows * kTileRows;
+    const bool tile_there = col / kTileCols < kt;
+    T* const values = A.values ? (T*)A.values + ((int64_t)e * A.M + row0) * A.K + col : nullptr;
+#pragma unroll
+    for (int s = 0; s < kSteps; s++) {
+        if (s * kRows >= tile_rows) break;
+        const int r = r0 + s * kRows;
+        uint32_t n[V / 4];
+#pragma unroll
+        for (int i = 0; i < V; i += 4) {
+            float q[4];
+#pragma unroll
+            for (int j = 0; j < 4; j++) {
+                const float w = number(Q::to(in[s][i + j])), x = fminf(fmaxf((i + j < have && r < rows ? w : 0.0f) * A.inverse, -most), most), q0 = x * y;
+                q[j] = fmaf(fmaf(-q0, S, x), y, q0);
+            }
+            uint32_t c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+            c = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], (int)c, true);
+            n[i / 4] = c & (0x7f7f7f7fu | ((c & 0x7f7f7f7fu) + 0x7f7f7f7fu));          // no sign of a zero
+        }
+        if (r < tile_rows && tile_there)
+            __builtin_memcpy(out + ((int64_t)((row0 + r) / kTileRows) * kt + col / kTileCols) * kW8Tile + w8_at(r % kTileRows, col % kTileCols), n, V);
+        if (values && r < rows) {
+            typename Q::Vec v;
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                const v2f lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)n[i / 4], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)n[i / 4], true);
+                v[i] = Q::round(lo[0] * unit); v[i + 1] = Q::round(lo[1] * unit); v[i + 2] = Q::round(hi[0] * unit); v[i + 3] = Q::round(hi[1] * unit);
+            }
+            T* const p = values + (int64_t)r * A.K;
+            if (have >= V) *(VecAny*)p = v;
+            else
+#pragma unroll
+                for (int i = 0; i < V - 1; i++) if (i < have) p[i] = v[i];
+        }
     }
 }
 struct ScalesArgs {
@@ -515,7 +569,7 @@ int dash_f8_quantise(dash_ctx* c, const void* w, int dtype, int64_t row_stride, 
     auto kernel = dtype == DASH_F32 ? k_f8_quantise<QuantF32> : dtype == DASH_BF16 ? k_f8_quantise<QuantBF16> : k_f8_quantise<QuantF16>;
     in_launches(blocks, [&](int64_t first, uint32_t n) {
         A.first = (uint32_t)first;
-        hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, (hipStream_t)stream, A);
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(kF8Threads), 0, (hipStream_t)stream, A);
     });
     DASH_HIP(hipGetLastError());
     return DASH_OK;

@@ -2,6 +2,12 @@
 import numpy as np
 
 
+def exp_of(a):
+    """e^a, a <= 0; what is below 2^-995.5 counts as zero (64 bits do not hold all its digits from 2^-1022 on, and 1 / (1 + e^-x) is zero from x = -709.8 on)"""
+    a = np.maximum(a, -800.0)
+    return np.where(np.rint(a * np.log2(np.e)) < -995, 0.0, np.exp(a))
+
+
 def choose(logits, top_k, sigmoid=False, bias=None, groups=1, top_groups=1, pair=False, renormalise=True, scale=1.0, gate_bits=8, valid=None):
     """logits float64 [n][E] -> (experts, gates, weights float64) [n][top_k]"""
     n, E = logits.shape
@@ -13,9 +19,10 @@ def choose(logits, top_k, sigmoid=False, bias=None, groups=1, top_groups=1, pair
         x = l[t]
         with np.errstate(over="ignore"):
             if sigmoid:
-                s = 1 / (1 + np.exp(-x))
+                y = exp_of(-np.abs(x))
+                s = np.where(x >= 0, 1, y) / (1 + y)
             else:
-                e = np.exp(x - x.max()) if x.max() > -np.inf else np.zeros(E)
+                e = exp_of(x - x.max()) if x.max() > -np.inf else np.zeros(E)
                 s = e / e.sum() if e.sum() > 0 else e
         c = x if bias is None else s + bias.astype(np.float64)
         able = (x > -np.inf) & ~np.isnan(c) & (c > -np.inf)
