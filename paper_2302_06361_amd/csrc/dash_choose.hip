@@ -60,16 +60,22 @@ __device__ __forceinline__ double row_sum(double v) {
 }
 // e^a for a <= 0: a = n ln 2 + r, |r| <= ln 2 / 2, and the series of e^r up to r^13 / 13! (what follows is below 2^-57); off by 1.5 units in the last place at most.
 // What is below 2^-995.5 counts as zero: quotients of scores hold all their bits.
-// (The library's: 65536 rows of 256 experts 6 us more.)
-__device__ __forceinline__ double exp_of(double a) {
-    a = fmax(a, -800.0);
+// The coefficients stand in registers: as literals each costs two moves in front of its sum.
+struct Series {
+    double c[13];
+    __device__ __forceinline__ Series() : c{1.0 / 6227020800.0, 1.0 / 479001600, 1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0} {
+#pragma unroll
+        for (int i = 0; i < 11; i++) asm("" : "+v"(c[i]));
+    }
+};
+__device__ __forceinline__ double exp_of(double a, const Series& S) {
+    a = a > -800.0 ? a : -800.0;
     const double n = rint(a * 1.4426950408889634074);
     double r = fma(n, -0x1.62e42fefa39efp-1, a);            // ln 2 to 53 bits, and what is left of it
     r = fma(n, -0x1.abc9e3b39803fp-56, r);
-    double s = 1.0 / 6227020800.0;
-    constexpr double kInverse[12] = {1.0 / 479001600, 1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0};
+    double s = S.c[0];
 #pragma unroll
-    for (int i = 0; i < 12; i++) s = fma(s, r, kInverse[i]);
+    for (int i = 1; i < 13; i++) s = fma(s, r, S.c[i]);
     s = fma(s, r, 1.0);
     return ldexp(s, n < -995.0 ? -3000 : (int)n);
 }
@@ -95,7 +101,6 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
     constexpr int T = V == 64 ? 64 : 256, R = T / kRowLanes, P = V + (V > 1 ? 1 : 0);      // P: a run and a word, against bank conflicts
     constexpr Key kNone = -(Key)INFINITY;
     __shared__ Key s_key[R][P * kRowLanes];
-    __shared__ float s_logit[R][V * kRowLanes + 1];
     const int lane = threadIdx.x % kRowLanes, rr = threadIdx.x / kRowLanes;
     const int64_t row_ = A.first + (int64_t)blockIdx.x * R + rr, row = row_ < A.n ? row_ : A.n - 1;
     const bool use = !A.valid || A.valid[row];
@@ -128,15 +133,21 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
     m = row_max(m);
     const double top = m > -INFINITY ? (double)m : 0.0;
     double common = 1;                          // of all softmax scores
+    const Series series;
     auto score = [&](float x) __attribute__((always_inline)) -> double {
-        if (!A.sigmoid) return exp_of((double)x - top) * common;
-        const double t = exp_of(-fabs((double)x));
+        if (!A.sigmoid) return exp_of((double)x - top, series) * common;
+        const double t = exp_of(-fabs((double)x), series);
         return (x >= 0 ? 1.0 : t) * inverse_of(1 + t);
     };
     const bool sum_wanted = !A.sigmoid && (BIAS || A.pair || !A.renormalise);     // (renormalised and of no other use: any common factor)
     Key best = kNone;
     if constexpr (BIAS) {
         double s[V], sum = 0;
+        float b[V];
+        if (A.E - lane * V >= V) __builtin_memcpy(b, A.bias + lane * V, sizeof(b));
+        else
+#pragma unroll
+            for (int v = 0; v < V; v++) b[v] = A.bias[lane * V + v < A.E ? lane * V + v : A.E - 1];
 #pragma unroll
         for (int v = 0; v < V; v++) { s[v] = score(l[v]); sum += s[v]; }
         if (sum_wanted) {
@@ -145,18 +156,16 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
         }
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            const int e = lane * V + v;
-            const double c = fma(s[v], common, (double)A.bias[e < A.E ? e : A.E - 1]);
+            const double c = fma(s[v], common, (double)b[v]);
             const Key k = use && l[v] > -INFINITY && c == c ? c : kNone;
             s_key[rr][lane * P + v] = k;
-            s_logit[rr][lane * V + v] = l[v];
             best = larger(best, k);
         }
     } else {
         if (sum_wanted) {
             double sum = 0;
 #pragma unroll
-            for (int v = 0; v < V; v++) sum += exp_of((double)l[v] - top);
+            for (int v = 0; v < V; v++) sum += exp_of((double)l[v] - top, series);
             sum = row_sum(sum);
             common = sum > 0 ? inverse_of(sum) : 0.0;
         }
@@ -243,8 +252,10 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
 #pragma unroll
     for (int i = 0; i < 2; i++) {
         s[i] = 0;
-        if (mine[i] >= 0) s[i] = score(BIAS ? s_logit[rr][mine[i]] : clean_logit(A.dtype == DASH_F32 ? ((const float*)A.logits)[row * A.row_stride + mine[i]]
-                                                                               : half_logit(((const uint16_t*)A.logits)[row * A.row_stride + mine[i]], A.dtype)));
+        if (mine[i] >= 0) {
+            const int64_t at = row * A.row_stride + mine[i];
+            s[i] = score(clean_logit(A.dtype == DASH_F32 ? ((const float*)A.logits)[at] : half_logit(((const uint16_t*)A.logits)[at], A.dtype)));
+        }
     }
     double factor = A.scale;
     if (A.renormalise) {
