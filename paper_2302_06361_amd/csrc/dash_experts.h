@@ -32,13 +32,14 @@ __host__ __device__ inline int w8_at(int row, int col) { return 64 * row + 16 * 
 
 // ---- routing: rows sorted by expert, and the tiles of the products ----
 // A group is 16 digits (a chunk) of one row.  The groups of an expert are numbered prime by prime, chunk by chunk, row by row.  A tile is up to
-// `groups` consecutive ones of one expert (byte weights: the operand is the same for every prime) or of one expert and prime (4-bit weights);
-// tiles are sorted by expert and first group.
-struct TileKind { int groups; bool one_prime; };
-constexpr int kTileKinds = 5;
-constexpr TileKind kTileKind[kTileKinds] = {{16, false}, {8, false}, {16, true}, {8, true}, {4, true}};
+// `groups` consecutive ones of one expert (byte weights: the operand is the same for every prime), of one expert and prime (4-bit weights) or of one expert and
+// class of primes (8-bit floats; the primes in the order of the classes); tiles are sorted by expert and first group.
+enum TileParts { PARTS_NONE = 0, PARTS_PRIMES = 1, PARTS_CLASSES = 2 };
+struct TileKind { int groups; TileParts parts; };
+constexpr int kTileKinds = 7;
+constexpr TileKind kTileKind[kTileKinds] = {{16, PARTS_NONE}, {8, PARTS_NONE}, {16, PARTS_PRIMES}, {8, PARTS_PRIMES}, {4, PARTS_PRIMES}, {8, PARTS_CLASSES}, {32, PARTS_CLASSES}};
 struct RouteTile {          // (read as a uint4)
-    uint32_t expert_prime;  // expert (n_experts: none) | index of the prime << 24 (one_prime; else 0)
+    uint32_t expert_prime;  // expert (n_experts: none) | index of the prime or class << 24
     int32_t start, count;   // the expert's rows: rows[start .. start + count - 1]
     int32_t first;          // first group
 };
@@ -57,16 +58,47 @@ inline int64_t total_chunks(const dash_ctx* c) {
     for (int i = 0; i < c->k; i++) n += c->mods[c->prime[i]].nchunk;
     return n;
 }
+// Residues of a weight modulo a product m of primes serve all of these primes: with m <= 255, between -127 and 127, they are signed bytes.  Classes: the largest prime that is left, and
+// as many more as fit, large ones first (2 to 37: 37 5, 31 7, 29 3 2, 23 11, 19 13, 17; one row of these is 7 tiles of 8 groups instead of the primes' 12).
+struct PrimeClasses {
+    int n;                                  // classes
+    int order[DASH_MAX_PRIMES];             // indexes of the primes, class after class
+    int modulus[DASH_MAX_PRIMES];
+    int prime_first[DASH_MAX_PRIMES + 1];   // of a class, in `order`
+    int chunk_first[DASH_MAX_PRIMES + 1];   // first chunk of a class, in the numbering of all
+};
+inline PrimeClasses prime_classes(const dash_ctx* c) {
+    PrimeClasses r = {};
+    bool done[DASH_MAX_PRIMES] = {};
+    for (int at = 0; at < c->k;) {
+        int m = 1, chunks = 0;
+        for (;;) {
+            int best = -1;
+            for (int i = 0; i < c->k; i++)
+                if (!done[i] && m * c->prime[i] <= 255 && (best < 0 || c->prime[i] > c->prime[best])) best = i;
+            if (best < 0) break;
+            done[best] = true;
+            r.order[at++] = best;
+            m *= c->prime[best];
+            chunks += (int)c->mods[c->prime[best]].nchunk;
+        }
+        r.modulus[r.n] = m;
+        r.prime_first[r.n + 1] = at;
+        r.chunk_first[r.n + 1] = r.chunk_first[r.n] + chunks;
+        r.n++;
+    }
+    return r;
+}
 inline RoutingView routing_view(const dash_ctx* c, void* data, int64_t n, int E) {
     RoutingView v;
     size_t at = 0;
     auto take = [&](size_t bytes) { uint8_t* p = (uint8_t*)data + at; at += (bytes + 63) / 64 * 64; return p; };
     v.offsets = (int32_t*)take(sizeof(int32_t) * (size_t)(E + 2));
     v.rows = (int32_t*)take(sizeof(int32_t) * (size_t)n);
-    // an expert with rows leaves at most one tile (one_prime: one a prime) partly filled
+    // an expert with rows leaves at most one tile (one a prime or class) partly filled
     const int64_t busy = n < (int64_t)E + 1 ? n : (int64_t)E + 1, chunks = total_chunks(c);
     for (int s = 0; s < kTileKinds; s++) {
-        v.max_tiles[s] = chunks * n / kTileKind[s].groups + busy * (kTileKind[s].one_prime ? c->k : 1);
+        v.max_tiles[s] = chunks * n / kTileKind[s].groups + busy * (kTileKind[s].parts == PARTS_NONE ? 1 : c->k);
         v.first_tile[s] = (int32_t*)take(sizeof(int32_t) * (size_t)(E + 2));
         v.tiles[s] = (RouteTile*)take(sizeof(RouteTile) * (size_t)v.max_tiles[s]);
     }

@@ -25,8 +25,8 @@ constexpr int kWaves = kThreads / 64;
 struct RouteArgs {
     const int32_t* experts;
     int64_t n;
-    int E, k;
-    int chunk_first[DASH_MAX_PRIMES + 1];       // first chunk of every prime in the numbering of all
+    int E;
+    int parts[3], chunk_first[3][DASH_MAX_PRIMES + 1];      // by TileParts: the parts, and the first chunk of each in the numbering of all
     RoutingView to;
 };
 __device__ __forceinline__ bool route_match(int32_t id, int e, int E) { return e < E ? id == e : (uint32_t)id >= (uint32_t)E; }
@@ -47,9 +47,9 @@ __device__ __forceinline__ int32_t route_tiles(int32_t rows, int first, int last
     return (int32_t)(((int64_t)rows * (last - first) + kTileKind[s].groups - 1) / kTileKind[s].groups);
 }
 __device__ __forceinline__ int32_t route_tiles(const RouteArgs& A, int32_t rows, int s) {
-    if (!kTileKind[s].one_prime) return route_tiles(rows, 0, A.chunk_first[A.k], s);
+    const int parts = kTileKind[s].parts;
     int32_t t = 0;
-    for (int i = 0; i < A.k; i++) t += route_tiles(rows, A.chunk_first[i], A.chunk_first[i + 1], s);
+    for (int i = 0; i < A.parts[parts]; i++) t += route_tiles(rows, A.chunk_first[parts][i], A.chunk_first[parts][i + 1], s);
     return t;
 }
 // One block: counts to offsets and to first tiles.
@@ -95,9 +95,9 @@ __global__ __launch_bounds__(kThreads) void k_route_fill(const RouteArgs A) {
     }
     for (int s = 0; s < kTileKinds; s++) {
         int32_t t0 = A.to.first_tile[s][e];
-        const bool one = kTileKind[s].one_prime;
-        for (int i = 0; i < (one ? A.k : 1); i++) {
-            const int c0 = one ? A.chunk_first[i] : 0, c1 = one ? A.chunk_first[i + 1] : A.chunk_first[A.k];
+        const int parts = kTileKind[s].parts;
+        for (int i = 0; i < A.parts[parts]; i++) {
+            const int c0 = A.chunk_first[parts][i], c1 = A.chunk_first[parts][i + 1];
             const int32_t tiles = route_tiles(count, c0, c1, s);
             for (int32_t t = lane; t < tiles; t += 64)
                 A.to.tiles[s][t0 + t] = RouteTile{(uint32_t)e | (uint32_t)i << 24, start, count, c0 * count + t * kTileKind[s].groups};
@@ -461,7 +461,7 @@ int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labe
     if ((st = check_bundle(c, in, T * K)) || (st = check_bundle(c, out, n * M))) return st;
     // int32 accumulators must not overflow: bytes up to 128 in magnitude on an offset of as much, residues otherwise
     for (int i = 0; i < c->k; i++) {
-        const uint64_t p1 = (uint64_t)c->prime[i] - 1, w = L->weight_format == DASH_W8 ? 256 : p1;
+        const uint64_t p1 = (uint64_t)c->prime[i] - 1, w = L->weight_format == DASH_MX4 ? p1 : 256;
         if (w * p1 * (uint64_t)K + p1 >= (1ull << 31)) return DASH_ESIZE;
     }
     ExpertsCall call{(const uint8_t*)L->weights, L->bias, nullptr, n, M, K, E, L->top_k, L->weight_format, garble};
@@ -606,8 +606,12 @@ int dash_route(dash_ctx* c, const int32_t* experts, int64_t n, int n_experts, vo
     if (!dash_route_bytes(c, n, n_experts)) return DASH_ESIZE;
     RouteArgs A;
     memset(&A, 0, sizeof(A));
-    A.experts = experts; A.n = n; A.E = n_experts; A.k = c->k;
-    for (int i = 0; i < c->k; i++) A.chunk_first[i + 1] = A.chunk_first[i] + (int)c->mods[c->prime[i]].nchunk;
+    A.experts = experts; A.n = n; A.E = n_experts;
+    const PrimeClasses classes = prime_classes(c);
+    A.parts[PARTS_NONE] = 1; A.parts[PARTS_PRIMES] = c->k; A.parts[PARTS_CLASSES] = classes.n;
+    for (int i = 0; i < c->k; i++) A.chunk_first[PARTS_PRIMES][i + 1] = A.chunk_first[PARTS_PRIMES][i] + (int)c->mods[c->prime[i]].nchunk;
+    A.chunk_first[PARTS_NONE][1] = A.chunk_first[PARTS_PRIMES][c->k];
+    for (int i = 0; i < classes.n; i++) A.chunk_first[PARTS_CLASSES][i + 1] = classes.chunk_first[i + 1];
     A.to = routing_view(c, data, n, n_experts);
     const dim3 grid((uint32_t)((n_experts + 1 + kWaves - 1) / kWaves));
     hipLaunchKernelGGL(k_route_count, grid, dim3(kThreads), 0, (hipStream_t)stream, A);

@@ -58,7 +58,8 @@ struct ETile {
     static constexpr int G = 2 * WD * DA;            // groups per block
     static constexpr int FT = WF * FB, F = 32 * FT;  // feature tiles, features per block
     static constexpr int GP = G / NW, WT = FT / NW;  // groups and tiles of weights that a wave loads
-    static_assert(G == kTileKind[KIND].groups && GP * NW == G && WT * NW == FT, "loader roles");
+    static constexpr bool HALF = FT * 2 == NW;       // a wave loads half a tile of weights
+    static_assert(G == kTileKind[KIND].groups && GP * NW == G && (HALF || WT * NW == FT), "loader roles");
     static_assert(!PERSIST || WK == 1, "the sets' sums go through the slots");
 };
 
@@ -86,6 +87,9 @@ struct ExpArgs {
     int first[DASH_MAX_PRIMES + 1];     // without routing, 4-bit: first block along the groups of every prime
     int chunk_first[DASH_MAX_PRIMES + 1];   // first chunk of every prime in the numbering of all; past the last prime: a number no chunk has
     ExpPrime pr[DASH_MAX_PRIMES];
+    // 8-bit floats: the primes above stand in the order of their classes
+    int part_first[DASH_MAX_PRIMES + 1];    // first chunk of every class
+    struct { uint32_t m, magic, pow12; } part[DASH_MAX_PRIMES];     // a class's modulus, ceil(2^32 / m), 4096 mod m
 };
 
 // 16 (4) bytes a lane from offset `off` + At of the buffer to LDS at `to` + Slot + At + 16 (4) * lane; a lane whose offset lies past the end of
@@ -112,11 +116,13 @@ __device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 template <int FMT, class TL>
 __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
-    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::WT, FT = TL::FT, NW = TL::NW, WK = TL::WK;
+    constexpr int G = TL::G, DA = TL::DA, FB = TL::FB, S = TL::S, GP = TL::GP, WT = TL::HALF ? 1 : TL::WT, FT = TL::FT, NW = TL::NW, WK = TL::WK;
     constexpr bool kMx4 = FMT == DASH_MX4, kF8 = FMT == DASH_F8;
-    constexpr bool kPrime = kMx4 || kF8;                // residues of the weights: a tile is of one prime
-    constexpr bool kDirect = kPrime && TL::WD == 1;     // a wave's weights are its own: expanded in registers
-    static_assert(!kF8 || kDirect, "8-bit floats are expanded in registers");
+    constexpr bool kPart = kMx4 || kF8;                 // residues of the weights: a tile is of one prime or class
+    constexpr bool kDirect = kPart && TL::WD == 1;      // a wave's weights are its own: expanded in registers
+    constexpr bool kHalfTile = TL::HALF;
+    static_assert(!kHalfTile || (kF8 && !kDirect), "loader roles");
+    static_assert(!kF8 || kDirect || kHalfTile, "steps of the expansion");
     const int M = A.M, K = A.K, nk = (K + 63) / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave_ = __builtin_amdgcn_readfirstlane(tid >> 6), ws = wave_ / NW, wave = wave_ % NW;
     const int wd = wave / TL::WF, wf = wave % TL::WF;
@@ -141,17 +147,17 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
             t.e = (int)(ep & 0xffffffu); t.pi = (int)(ep >> 24);
             t.start = __builtin_amdgcn_readfirstlane(r.start); t.count = __builtin_amdgcn_readfirstlane(r.count);
             t.first = __builtin_amdgcn_readfirstlane(r.first);
-        } else if (kPrime) {
+        } else if (kPart) {
             while (bx >= A.first[t.pi + 1]) t.pi++;
-            t.first = A.chunk_first[t.pi] * t.count + (bx - A.first[t.pi]) * G;
+            t.first = (kF8 ? A.part_first : A.chunk_first)[t.pi] * t.count + (bx - A.first[t.pi]) * G;
         } else t.first = bx * G;
-        const int end = A.chunk_first[kPrime ? t.pi + 1 : A.k] * t.count;
+        const int end = (kF8 ? A.part_first[t.pi + 1] : A.chunk_first[kMx4 ? t.pi + 1 : A.k]) * t.count;
         t.n_groups = end - t.first < G ? end - t.first : G;
         return true;
     };
 
     constexpr int kDig = G * 1024, kRaw = kMx4 ? 1280 : 2048;       // bytes of a stage's labels; of a stage's weights per feature tile, as loaded
-    constexpr int kExp = kMx4 && !kDirect ? FT * 2048 : 0;          // 4-bit: bytes of an expanded stage
+    constexpr int kExp = kPart && !kDirect ? FT * 2048 : 0;         // bytes of an expanded stage
     // one array: its address goes into the loads, so that the compiler takes all of it to change at their waits and barriers
     constexpr int kSet = S * kDig + S * FT * kRaw + 2 * kExp;       // of a set of waves
     __shared__ __attribute__((aligned(1024))) uint8_t smem[WK * kSet];
@@ -219,31 +225,31 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         const uint8_t* const wexp = A.w + (int64_t)t.e * A.expert_bytes;
 #pragma unroll
         for (int i = 0; i < WT; i++) {                              // (tiles past the last: empty buffers)
-            const int rt = t.by * FT + wave * WT + i;
+            const int rt = t.by * FT + (kHalfTile ? wave >> 1 : wave * WT + i);
             wgt[i] = buffer_of(wexp + (int64_t)rt * nk * kTileBytes, rt < (M + 31) / 32 ? (uint32_t)(nk * kTileBytes) : 0u);
         }
-        off_w = 16u * lane + ws * kTileBytes; off_s = 4u * (lane & 15) + kMx4Codes + ws * kTileBytes;
+        off_w = 16u * lane + ws * kTileBytes + (kHalfTile ? (wave & 1) * 1024u : 0u); off_s = 4u * (lane & 15) + kMx4Codes + ws * kTileBytes;
     };
     auto open_labels = [&](const Tile& t, const Groups& g) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < GP; i++) lab[i] = buffer_of((const uint8_t*)lane_of(g.src, wave * GP + i), wave * GP + i < t.n_groups ? (uint32_t)K * 16u : 0u);
         off_l = (16u * lane ^ (GP % 2 ? (wave & 1) * 128u : 0u)) + ws * 1024;
     };
-    const uint32_t dig0 = (uint32_t)(uintptr_t)(lds_ptr)s_dig + wave * GP * 1024, raw0 = (uint32_t)(uintptr_t)(lds_ptr)s_raw + wave * WT * kRaw;
+    const uint32_t dig0 = (uint32_t)(uintptr_t)(lds_ptr)s_dig + wave * GP * 1024, raw0 = (uint32_t)(uintptr_t)(lds_ptr)s_raw + (kHalfTile ? wave * 1024 : wave * WT * kRaw);
     // A set takes every WK-th stage of 64 inputs: its stage t, the inputs from 64 (WK t + ws), goes into slot t % S.  Stages past the end load nothing (their offsets lie past the buffers) but count.  A
     // lane's offsets run along with the stages.
     // Words 8 .. 15 of every 16 of a group with an odd number stand before words 0 .. 7: the reads of two groups meet different banks.
-    constexpr int kParts = 2 * WT + GP;                             // loads of a stage: weights, then labels
+    constexpr int kWLoads = kHalfTile ? 1 : 2 * WT, kParts = kWLoads + GP;       // loads of a stage: weights, then labels
     auto load_weights = [&](auto slot, int i) __attribute__((always_inline)) {
-        constexpr int kSlot = decltype(slot)::value * FT * kRaw;
+        constexpr int kSlot = decltype(slot)::value % S * FT * kRaw;
         const uint32_t to = raw0 + i / 2 * kRaw;
         if (i % 2 == 0) load_lds16<kSlot, 0>(to, wgt[i / 2], off_w);
         else if constexpr (kMx4) load_lds4<kSlot + kMx4Codes>(to, wgt[i / 2], off_s);
         else load_lds16<kSlot, 1024>(to, wgt[i / 2], off_w);
-        if (i == 2 * WT - 1) { off_w += WK * kTileBytes; off_s += WK * kTileBytes; }
+        if (i == kWLoads - 1) { off_w += WK * kTileBytes; off_s += WK * kTileBytes; }
     };
     auto load_labels = [&](auto slot, int i) __attribute__((always_inline)) {
-        constexpr int kSlot = decltype(slot)::value * kDig;
+        constexpr int kSlot = decltype(slot)::value % S * kDig;
         load_lds16<kSlot, 0>(dig0 + i * 1024, lab[i], i % 2 ? off_l ^ 128u : off_l);          // (the wave's second group has an odd number; with one group a wave, see open)
         if (i == GP - 1) off_l += WK * 1024;
     };
@@ -273,25 +279,23 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         }
     };
     // ---- 8-bit floats ----
-    // Code c under the scale S: 512 e4m3(c) S mod p, a byte of a table of 256 for every row of scales of the block and 128 inputs.  Thread c (mod 256) keeps its
-    // code's residue and multiplies it by the scale's.
+    // Code c under the scale S: 512 e4m3(c) S mod m, m the product of the primes of the tile's class, a signed byte of a table of 256 for every row of scales of the block and 128
+    // inputs.  Thread c (mod 256) keeps its code's residue and multiplies it by the scale's.
     uint32_t f8_residue = 0;
     scalar_ptr f8_scales = nullptr;
-    int f8_p = 0;
     constexpr int kTabRounds = kF8 ? (kTabs * 256 + TL::T - 1) / TL::T : 0;
     auto open_table = [&](const Tile& t) __attribute__((always_inline)) {
         if constexpr (kF8) {
-            const uint32_t prime = A.pr[t.pi].p, mag = f8_magnitude(tid & 0x7f) % prime;
-            f8_residue = (tid & 0x80) && mag ? prime - mag : mag;
+            const uint32_t mod = A.part[t.pi].m, mag = f8_magnitude(tid & 0x7f) % mod;
+            f8_residue = (tid & 0x80) && mag ? mod - mag : mag;
             f8_scales = (scalar_ptr)(A.w + (int64_t)t.e * A.expert_bytes + scales_at(M, K));
-            f8_p = t.pi;
         }
     };
     // the tables of inputs 128 kb .. 128 kb + 127 (past the end: any)
     auto make_f8 = [&](const Tile& t, int kb) __attribute__((always_inline)) {
         if constexpr (kF8) {
             const int kblocks = (K + kScaleBlock - 1) / kScaleBlock, rows = (M + kScaleBlock - 1) / kScaleBlock, at = kb < kblocks ? kb : kblocks - 1;
-            const uint32_t prime = A.pr[f8_p].p, mmagic = A.pr[f8_p].mmagic, pow12 = A.pr[f8_p].pow12;
+            const uint32_t mod = A.part[t.pi].m, magic = A.part[t.pi].magic, pow12 = A.part[t.pi].pow12;
 #pragma unroll
             for (int i = 0; i < kTabRounds; i++) {
                 const int at256 = __builtin_amdgcn_readfirstlane(tid >> 8) + i * (TL::T / 256);      // (a wave's threads share a table)
@@ -300,9 +304,9 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                 const int32_t S = f8_scales[(int64_t)(rb < rows ? rb : rows - 1) * kblocks + at];
                 // |S| below 2^31 in two steps
                 const uint32_t a = S < 0 ? 0u - (uint32_t)S : (uint32_t)S;
-                auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - mul24(mulhi(v, mmagic), prime); };
-                const uint32_t hi = red1(a >> 12), s0 = red1(hi * pow12 + (a & 4095u)), s1 = S < 0 && s0 ? prime - s0 : s0;
-                s_f8[((kb & 1) * kTabs + at256) * 256 + (tid & 255)] = (uint8_t)red1(f8_residue * s1);
+                auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - mul24(mulhi(v, magic), mod); };
+                const uint32_t hi = red1(a >> 12), s0 = red1(hi * pow12 + (a & 4095u)), s1 = S < 0 && s0 ? mod - s0 : s0, r = red1(f8_residue * s1);
+                s_f8[((kb & 1) * kTabs + at256) * 256 + (tid & 255)] = (uint8_t)(2 * r > mod ? r - mod : r);
             }
         }
     };
@@ -313,6 +317,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     };
     auto join4 = [&](const uint32_t (&r)[4]) __attribute__((always_inline)) -> uint32_t { return (r[0] | r[1] << 8) | (r[2] | r[3] << 8) << 16; };
     const uint32_t f8_base = (uint32_t)(uintptr_t)(lds_ptr)s_f8;
+    constexpr int kUnroll = S == 3 ? (kDirect ? 3 : 6) : S;         // stages of a round of the loop: slots and parities are known in each
     // A lane's 16 bytes of codes are 16 weights of a row's first block of 32 and 16 of its second (low and high halves of the bytes); shifts of
     // both blocks, table entries of both, then four weights at a time as bytes.
     // In registers (a wave's weights are its own: kDirect): lane (j32, h) holds what it multiplies, two stages in the making.
@@ -323,9 +328,11 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     const uint8_t* const raw_codes = s_raw + wave * WT * kRaw + 16 * (kDirect ? 2 * j32 + h : lane);
     const uint8_t* const raw_shifts = s_raw + wave * WT * kRaw + kMx4Codes + 2 * (kDirect ? j32 : lane >> 1);
     // (8-bit floats: the codes of half `b` of a stage)
-    const uint8_t* const raw_f8 = s_raw + wave * WT * kRaw + 64 * j32;
+    // (through LDS: the lane's 16 codes of the stage)
+    const uint8_t* const raw_f8 = kHalfTile ? s_raw + wave * 1024 + 16 * lane : s_raw + wave * WT * kRaw + 64 * j32;
     auto fetch_codes = [&](auto slot, int b) __attribute__((always_inline)) {
-        if constexpr (kF8) {
+        if constexpr (kF8 && !kDirect) code[0][0] = *(const u32x4*)(raw_f8 + decltype(slot)::value % S * FT * kRaw);
+        else if constexpr (kF8) {
 #pragma unroll
             for (int i = 0; i < WT; i++) code[b][i] = *(const u32x4*)(raw_f8 + 16 * w8_piece(j32, 2 * b + h) + (decltype(slot)::value % S * FT + i) * kRaw);
         }
@@ -350,7 +357,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         const uint32_t sel = (block ? x >> 4 : x) & 0x07070707u, sign = __builtin_amdgcn_bitop3_b32(block ? x >> 5 : x >> 1, 0x04040404u, k3210, 0xea);     // a & b | c
         return __builtin_amdgcn_perm(__builtin_amdgcn_perm(l[3], l[2], sel), __builtin_amdgcn_perm(l[1], l[0], sel), sign);
     };
-    constexpr int kSteps = 8 * WT;
+    constexpr int kSteps = kHalfTile ? 4 : 8 * WT;
     uint8_t* const exp_to0 = s_exp + wave * WT * 2048 + 64 * (lane >> 1) + 16 * w8_piece(lane >> 1, lane & 1);
     uint8_t* const exp_to1 = s_exp + wave * WT * 2048 + 64 * (lane >> 1) + 16 * w8_piece(lane >> 1, 2 + (lane & 1));
     // (steps of the first block of every tile, then of the second)
@@ -362,12 +369,25 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         }
     };
 
+    uint8_t* const exp8_to = s_exp + wave * 1024 + 16 * lane;
+    auto expand8 = [&](int parity, uint32_t base) __attribute__((always_inline)) {
+        if constexpr (kF8 && !kDirect) {
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                uint32_t look[4];
+                look4(look, code[0][0][i], base);
+                bytes[0][i] = join4(look);
+            }
+            *(u32x4*)(exp8_to + parity * kExp) = bytes[0];
+        }
+    };
+
     // ---- products ----
     const int odd = (lane >> 4) & 1;
     const uint8_t* const da = s_dig + wd * DA * 2048 + odd * 1024 + h * 256 + (l16 >> 1) * 16 + (l16 & 1) * 8;
     const uint8_t* const da0 = da + odd * 128;
     const uint8_t* const da1 = da + 128 - odd * 128;
-    const uint8_t* const fb = (kMx4 ? s_exp : s_raw) + wf * FB * 2048 + 64 * j32;
+    const uint8_t* const fb = (kPart ? s_exp : s_raw) + wf * FB * 2048 + 64 * j32;
     const uint8_t* const fb0 = fb + 16 * w8_piece(j32, h);
     const uint8_t* const fb1 = fb + 16 * w8_piece(j32, 2 + h);
     // operands of one half (32 inputs) of a stage, in FB + 2 DA reads
@@ -375,10 +395,10 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     auto read = [&](Operands& o, auto slot, int half, int i) __attribute__((always_inline)) {
         constexpr int kSlot = decltype(slot)::value;
         if (i < FB) {
-            if constexpr (!kDirect) o.b[i] = *(const v4i*)((half ? fb1 : fb0) + (kMx4 ? (kSlot & 1) * kExp : kSlot * FT * kRaw) + i * 2048);
+            if constexpr (!kDirect) o.b[i] = *(const v4i*)((half ? fb1 : fb0) + (kPart ? (kSlot & 1) * kExp : kSlot * FT * kRaw) + i * 2048);
         } else {
             const int d = (i - FB) / 2, second = (i - FB) % 2;
-            o.a[d][second] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)((second ? da1 : da0) + kSlot * kDig + half * 512 + d * 2048));
+            o.a[d][second] = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_v2i)((second ? da1 : da0) + kSlot % S * kDig + half * 512 + d * 2048));
         }
     };
     // Stage t in two halves of 32 inputs; the operands of its first half are in registers when it starts:
@@ -398,12 +418,12 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr integral_constant<int, 1> k1{};
     // loads that may be in flight at the barrier of stage t: those behind the labels of stage t + 1, 4-bit: behind the weights of stage t + 2
     static_assert(S == 4 || (kF8 && S == 3), "the loop's slots; parities of stages follow from slots; the waits of the first stages");
-    constexpr int kInFlight = kPrime ? (S - 3) * kParts + GP : (S - 2) * kParts;
+    constexpr int kInFlight = kPart ? (S - 3) * kParts + GP : (S - 2) * kParts;
     // the first stages: all weights, then labels (these wait for the rows' numbers), but for the labels of stage S - 1
     auto fill_weights = [&](auto self, auto u) __attribute__((always_inline)) -> void {
         if constexpr (decltype(u)::value < S) {
 #pragma unroll
-            for (int i = 0; i < 2 * WT; i++) load_weights(u, i);
+            for (int i = 0; i < kWLoads; i++) load_weights(u, i);
             self(self, integral_constant<int, decltype(u)::value + 1>{});
         }
     };
@@ -428,11 +448,12 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         if (more) begun = begin(next);
         wait_loads<(S - 2) * GP>();         // all weights and the labels of stage 0
         lds_barrier();
-        if constexpr (kMx4 && !kDirect) {
+        if constexpr (kPart && !kDirect) {
             fetch_codes(k0, 0);
             fetch_table(0); fetch_table(1);
 #pragma unroll
             for (int i = 0; i < kSteps; i++) expand(0, i);
+            if constexpr (kF8) expand8(0, f8_base);
             lds_barrier();
         }
         int zero = 0;
@@ -441,7 +462,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
 #pragma unroll
         for (int d = 0; d < dn; d++) {
             const int g0 = (wd * DA + d) * 2;
-            const int s0 = kPrime || ws ? zero : (int)lane_of(g.start, g0), s1 = kPrime || ws ? zero : (int)lane_of(g.start, g0 + 1);
+            const int s0 = kMx4 || ws ? zero : (int)lane_of(g.start, g0), s1 = kMx4 || ws ? zero : (int)lane_of(g.start, g0 + 1);
 #pragma unroll
             for (int f = 0; f < FB; f++)
 #pragma unroll
@@ -455,18 +476,30 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         Operands o0, o1;
         int t = 0;
         auto half = [&](const Operands& now, Operands& next, bool there, auto u, auto second) __attribute__((always_inline)) {
-            constexpr int U = decltype(u)::value, kHalf = decltype(second)::value, kLoads = kHalf ? 2 * WT : GP;
-            constexpr integral_constant<int, (U + 1) % S> u1{};
-            constexpr integral_constant<int, (U + 2) % S> u2{};
+            constexpr int U = decltype(u)::value, kHalf = decltype(second)::value, kLoads = kHalf ? kWLoads : GP;
+            constexpr integral_constant<int, (U + 1) % kUnroll> u1{};
+            constexpr integral_constant<int, (U + 2) % kUnroll> u2{};
             constexpr integral_constant<int, (U + S - 1) % S> before{};
-            uint32_t look[kF8 ? 4 * FB : 1][4];
+            uint32_t look[kF8 && kDirect ? 4 * FB : 2][4];
 #pragma unroll
             for (int m = 0; m < kSlots; m++) {
                 if (m < kProducts && there) multiply(now, m);
 #pragma unroll
                 for (int i = 0; i < kReads; i++)
                     if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) { if constexpr (kHalf) read(next, u1, 0, i); else read(next, u, 1, i); }
-                if constexpr (kF8) {
+                if constexpr (kF8 && !kDirect) {
+                    // As with 4-bit weights, half of the lane's 16 codes in each half; the tables of the 128 inputs that stage t + 2 (even) begins are made in the first half.
+                    if (m == 0 && !kHalf && !(t & 1)) make_f8(tile, (t >> 1) + 1);
+                    if (kHalf && m == 0) fetch_codes(u2, 0);
+                    const uint32_t base = f8_base + ((uint32_t)(t + kHalf + 1) >> 1 & 1) * 256;         // of stage t + 2, in the first half of stage t + 1
+#pragma unroll
+                    for (int i = 0; i < 2; i++) {
+                        const int s = kHalf ? kSlots / 4 + i * kSlots / 4 : i * kSlots / 4;
+                        if (s == m) look4(look[i], code[0][0][2 * !kHalf + i], base);
+                        if (s + kSlots / 4 == m || (s + kSlots / 4 >= kSlots && m == kSlots - 1 && s != m)) bytes[0][2 * !kHalf + i] = join4(look[i]);
+                    }
+                    if (!kHalf && m == kSlots - 2) *(u32x4*)(exp8_to + ((U + 1) & 1) * kExp) = bytes[0];
+                } else if constexpr (kF8) {
                     // Codes of the next stage's half of the same number, and the bytes of the half whose codes are there.  The tables of the 128 inputs that
                     // the next stage begins are made in the first half, in front of the barrier.
                     static_assert(FB == WT, "a wave expands what it multiplies");
@@ -511,7 +544,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
             // (of the first stages the weights went out first: fewer loads stand behind the labels of stage t + 1)
             constexpr int U = decltype(u)::value;
             if (U == 0 && t == 0) wait_loads<(S - 2) * GP>();
-            else if (U == 1 && !kPrime && t == 1) wait_loads<(S - 2) * GP + 2 * WT>();
+            else if (U == 1 && !kPart && t == 1) wait_loads<(S - 2) * GP + 2 * WT>();
             else wait_loads<kInFlight>();
             lds_barrier();
             half(o1, o0, there, u, k1);
@@ -519,7 +552,15 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         };
 #pragma unroll
         for (int i = 0; i < kReads; i++) read(o0, k0, 0, i);
-        if constexpr (kF8) {
+        if constexpr (kF8 && !kDirect) {
+            fetch_codes(k1, 0);
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                uint32_t look[4];
+                look4(look, code[0][0][i], f8_base);
+                bytes[0][i] = join4(look);
+            }
+        } else if constexpr (kF8) {
             fetch_codes(k0, 0);
             fetch_codes(k0, 1);
 #pragma unroll
@@ -539,8 +580,11 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
 #pragma unroll
             for (int i = 0; i < kSteps / 2; i++) expand(1, i);
         }
-        if constexpr (S == 3) while (stage(k0) && stage(k1) && stage(integral_constant<int, 2>{})) {}
-        else while (stage(k0) && stage(k1) && stage(integral_constant<int, 2>{}) && stage(integral_constant<int, 3>{})) {}
+        constexpr integral_constant<int, 2> k2{};
+        constexpr integral_constant<int, 3> k3{};
+        if constexpr (kUnroll == 6) while (stage(k0) && stage(k1) && stage(k2) && stage(k3) && stage(integral_constant<int, 4>{}) && stage(integral_constant<int, 5>{})) {}
+        else if constexpr (kUnroll == 3) while (stage(k0) && stage(k1) && stage(k2)) {}
+        else while (stage(k0) && stage(k1) && stage(k2) && stage(k3)) {}
         wait_loads<0>();
         if constexpr (WK > 1) {
             // the sums of the other sets come through LDS
@@ -642,7 +686,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
 }
 
 // what the launches of every tile share; work and bytes for the profile
-struct ExpWork { ExpArgs A; double macs, bytes; };
+struct ExpWork { ExpArgs A; double macs, bytes; PrimeClasses classes; };
 inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, ExpWork& work) {
     ExpArgs& A = work.A;
     memset(&A, 0, sizeof(A));
@@ -654,17 +698,27 @@ inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labe
     A.plain = L.bias == nullptr;
     for (int i = 0; i <= DASH_MAX_PRIMES; i++) A.chunk_first[i] = 0x7fffffff;
     A.chunk_first[0] = 0;
-    for (int i = 0; i < c->k; i++) {
-        ExpPrime& P = A.pr[i];
+    const bool by_class = L.format == DASH_F8;
+    if (by_class) {
+        const PrimeClasses& C = work.classes = prime_classes(c);
+        for (int i = 0; i <= C.n; i++) A.part_first[i] = C.chunk_first[i];
+        for (int i = 0; i < C.n; i++) {
+            const uint32_t m = (uint32_t)C.modulus[i];
+            A.part[i] = {m, (uint32_t)(((1ull << 32) + m - 1) / m), 4096u % m};
+        }
+    }
+    for (int at = 0; at < c->k; at++) {
+        const int i = by_class ? work.classes.order[at] : at;
+        ExpPrime& P = A.pr[at];
         const ModInfo& Mi = c->mods[c->prime[i]];
-        A.chunk_first[i + 1] = A.chunk_first[i] + (int)Mi.nchunk;
-        P.chunk_first = A.chunk_first[i];
+        A.chunk_first[at + 1] = A.chunk_first[at] + (int)Mi.nchunk;
+        P.chunk_first = A.chunk_first[at];
         P.p = c->prime[i]; P.mmagic = Mi.mmagic; P.pow12 = 4096u % P.p;
         P.one = L.bias ? (L.garble ? c->d_one0[i] : c->d_one[i]) : nullptr;
         P.in = view_of(in, i); P.out = view_of(out, i);
         const uint64_t p1 = P.p - 1;
         uint64_t vmax = p1 * p1 * (uint64_t)L.K;
-        if (L.format == DASH_W8) {
+        if (L.format != DASH_MX4) {
             P.start = (uint32_t)((128 * p1 * (uint64_t)L.K + P.p - 1) / P.p * P.p);
             vmax = P.start + 127 * p1 * (uint64_t)L.K;
         }
@@ -678,19 +732,21 @@ inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labe
 }
 template <int FMT, class TL> int launch_experts(dash_ctx* c, const ExpertsCall& L, ExpWork& work, hipStream_t s) {
     ExpArgs& A = work.A;
-    constexpr bool one_prime = FMT != DASH_W8;
+    constexpr TileParts parts = FMT == DASH_W8 ? PARTS_NONE : FMT == DASH_MX4 ? PARTS_PRIMES : PARTS_CLASSES;
     int64_t cols = 0;
     if (L.routing) {
         constexpr int s = TL::KIND;
-        static_assert(kTileKind[s].one_prime == one_prime, "tiles of the format");
+        static_assert(kTileKind[s].parts == parts, "tiles of the format");
         cols = L.routing->max_tiles[s];
         A.rows = L.routing->rows; A.tiles = L.routing->tiles[s]; A.n_tiles = L.routing->first_tile[s] + L.E + 1;
-    } else if (one_prime)
-        for (int i = 0; i < c->k; i++) {
+    } else if (parts != PARTS_NONE) {
+        const int* const chunks = parts == PARTS_CLASSES ? A.part_first : A.chunk_first;
+        for (int i = 0; i < (parts == PARTS_CLASSES ? work.classes.n : c->k); i++) {
             A.first[i] = (int)cols;
-            cols += ((int64_t)(A.chunk_first[i + 1] - A.chunk_first[i]) * L.n + TL::G - 1) / TL::G;
+            cols += ((int64_t)(chunks[i + 1] - chunks[i]) * L.n + TL::G - 1) / TL::G;
             A.first[i + 1] = (int)cols;
         }
+    }
     else cols = ((int64_t)A.chunk_first[c->k] * L.n + TL::G - 1) / TL::G;
     A.cols = (int)cols;
     A.row_blocks = (L.M + TL::F - 1) / TL::F;
