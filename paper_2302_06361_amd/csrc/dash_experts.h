@@ -33,11 +33,11 @@ __host__ __device__ inline int w8_at(int row, int col) { return 64 * row + 16 * 
 // ---- routing: rows sorted by expert, and the tiles of the products ----
 // A group is 16 digits (a chunk) of one row.  The groups of an expert are numbered prime by prime, chunk by chunk, row by row.  A tile is up to
 // `groups` consecutive ones of one expert (byte weights: the operand is the same for every prime), of one expert and prime (4-bit weights) or of one expert and
-// class of primes (8-bit floats; the primes in the order of the classes); tiles are sorted by expert and first group.
+// class of primes (8-bit floats and few rows; the primes in the order of the classes); tiles are sorted by expert and first group.
 enum TileParts { PARTS_NONE = 0, PARTS_PRIMES = 1, PARTS_CLASSES = 2 };
 struct TileKind { int groups; TileParts parts; };
-constexpr int kTileKinds = 7;
-constexpr TileKind kTileKind[kTileKinds] = {{16, PARTS_NONE}, {8, PARTS_NONE}, {16, PARTS_PRIMES}, {8, PARTS_PRIMES}, {4, PARTS_PRIMES}, {8, PARTS_CLASSES}, {32, PARTS_CLASSES}};
+constexpr int kTileKinds = 8;
+constexpr TileKind kTileKind[kTileKinds] = {{16, PARTS_NONE}, {8, PARTS_NONE}, {16, PARTS_PRIMES}, {8, PARTS_PRIMES}, {4, PARTS_PRIMES}, {8, PARTS_CLASSES}, {32, PARTS_PRIMES}, {32, PARTS_CLASSES}};
 struct RouteTile {          // (read as a uint4)
     uint32_t expert_prime;  // expert (n_experts: none) | index of the prime or class << 24
     int32_t start, count;   // the expert's rows: rows[start .. start + count - 1]

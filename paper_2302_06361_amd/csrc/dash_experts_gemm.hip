@@ -15,7 +15,7 @@ int experts_mfma(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_
     ExpWork W;
     const int st = experts_args(c, L, in, out, W);
     if (st) return st;
-    const ExpertsTile tile = experts_tile(c->experts_tile, experts_shape(c, L, W.A));
+    const ExpertsTile tile = experts_tile(c->experts_tile, experts_shape(c, L));
     if (L.format == DASH_W8) return tile == EXPERTS_BIG ? launch_experts<DASH_W8, EBig>(c, L, W, s) : launch_experts<DASH_W8, ENarrow>(c, L, W, s);
     return tile == EXPERTS_BIG ? launch_experts<DASH_MX4, EBig4>(c, L, W, s) : tile == EXPERTS_FEW ? launch_experts<DASH_MX4, EFew4>(c, L, W, s)
          : tile == EXPERTS_WIDE ? launch_experts<DASH_MX4, EWide4>(c, L, W, s) : launch_experts<DASH_MX4, ENarrow4>(c, L, W, s);

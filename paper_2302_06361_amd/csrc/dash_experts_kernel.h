@@ -46,7 +46,6 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 typedef __attribute__((address_space(3))) v2i* lds_v2i;
-typedef const __attribute__((address_space(4))) int32_t* scalar_ptr;
 
 // WK sets of WD x WF waves (along the inputs; along digits, along features), a wave DA x FB tiles of 32 digits x 32 features; S stages of 64
 // inputs in LDS for each set; KIND: tiles of the routing; PERSIST: a block takes tile after tile (one block per CU)
@@ -87,9 +86,9 @@ struct ExpArgs {
     int first[DASH_MAX_PRIMES + 1];     // without routing, 4-bit: first block along the groups of every prime
     int chunk_first[DASH_MAX_PRIMES + 1];   // first chunk of every prime in the numbering of all; past the last prime: a number no chunk has
     ExpPrime pr[DASH_MAX_PRIMES];
-    // 8-bit floats: the primes above stand in the order of their classes
-    int part_first[DASH_MAX_PRIMES + 1];    // first chunk of every class
-    struct { uint32_t m, magic, pow12; } part[DASH_MAX_PRIMES];     // a class's modulus, ceil(2^32 / m), 4096 mod m
+    // 8-bit floats: the parts, primes or classes of them (the primes above then stand in their order)
+    int part_first[DASH_MAX_PRIMES + 1];    // first chunk of every part
+    struct { uint32_t m, magic; } part[DASH_MAX_PRIMES];     // a part's modulus and ceil(2^32 / m)
 };
 
 // 16 (4) bytes a lane from offset `off` + At of the buffer to LDS at `to` + Slot + At + 16 (4) * lane; a lane whose offset lies past the end of
@@ -121,6 +120,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr bool kPart = kMx4 || kF8;                 // residues of the weights: a tile is of one prime or class
     constexpr bool kDirect = kPart && TL::WD == 1;      // a wave's weights are its own: expanded in registers
     constexpr bool kHalfTile = TL::HALF;
+    constexpr bool kSigned = kTileKind[TL::KIND].parts == PARTS_CLASSES;       // residues of either sign
     static_assert(!kHalfTile || (kF8 && !kDirect), "loader roles");
     static_assert(!kF8 || kDirect || kHalfTile, "steps of the expansion");
     const int M = A.M, K = A.K, nk = (K + 63) / 64;
@@ -166,9 +166,8 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     uint8_t* const s_raw = s_dig + S * kDig;
     uint8_t* const s_exp = s_raw + S * FT * kRaw;
     __shared__ u32x4 s_lut[kMx4 ? 256 : 1];
-    constexpr int kTabs = kF8 ? TL::F / kScaleBlock : 1;            // tables of a stage: the block's rows of scales
-    static_assert(!kF8 || TL::F % kScaleBlock == 0, "a block's features are whole rows of scales");
-    __shared__ __attribute__((aligned(512))) uint8_t s_f8[kF8 ? 2 * kTabs * 256 : 16];      // of two blocks of 128 inputs
+    static_assert(!kF8 || TL::F == kScaleBlock, "a block's features have one row of scales");
+    __shared__ __attribute__((aligned(512))) uint8_t s_f8[kF8 ? 512 : 16];      // tables of two blocks of 128 inputs
 
     // the primes, for lanes that each want another
     struct PrimeLds { uint64_t in, in_cs, out, out_cs, one; uint32_t p, mmagic, pow12, start, chunk_first, pad; };
@@ -279,34 +278,48 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         }
     };
     // ---- 8-bit floats ----
-    // Code c under the scale S: 512 e4m3(c) S mod m, m the product of the primes of the tile's class, a signed byte of a table of 256 for every row of scales of the block and 128
-    // inputs.  Thread c (mod 256) keeps its code's residue and multiplies it by the scale's.
-    uint32_t f8_residue = 0;
-    scalar_ptr f8_scales = nullptr;
-    constexpr int kTabRounds = kF8 ? (kTabs * 256 + TL::T - 1) / TL::T : 0;
-    auto open_table = [&](const Tile& t) __attribute__((always_inline)) {
+    // Code c under the scale S: 512 e4m3(c) S mod m, m the prime of the tile or the product of the primes of its class, a byte of a table of 256 for every 128 inputs.  Thread c
+    // keeps its code's residue and multiplies it by the scale's; lane l of every wave keeps the residue of scale l of 64.  (Scales by scalar loads where they are
+    // wanted: waits for memory in front of the barriers, 128 rows, 4096 -> 4096: 1158 us.)
+    uint32_t f8_residue = 0, f8_mod = 0, f8_magic = 0, f8_scale = 0;
+    const int32_t* f8_scales = nullptr;
+    const int f8_blocks = (K + kScaleBlock - 1) / kScaleBlock;
+    int32_t f8_loaded = 0;
+    // scales 64 i .. 64 i + 63 of the tile's row of them (past the end: the last), a load in flight
+    auto load_scales = [&](int i) __attribute__((always_inline)) {
+        if constexpr (kF8) f8_loaded = f8_scales[64 * i + lane < f8_blocks ? 64 * i + lane : f8_blocks - 1];
+    };
+    auto open_scales = [&](const Tile& t) __attribute__((always_inline)) {
         if constexpr (kF8) {
-            const uint32_t mod = A.part[t.pi].m, mag = f8_magnitude(tid & 0x7f) % mod;
-            f8_residue = (tid & 0x80) && mag ? mod - mag : mag;
-            f8_scales = (scalar_ptr)(A.w + (int64_t)t.e * A.expert_bytes + scales_at(M, K));
+            f8_scales = (const int32_t*)(A.w + (int64_t)t.e * A.expert_bytes + scales_at(M, K)) + (int64_t)t.by * f8_blocks;
+            load_scales(0);
         }
     };
-    // the tables of inputs 128 kb .. 128 kb + 127 (past the end: any)
-    auto make_f8 = [&](const Tile& t, int kb) __attribute__((always_inline)) {
+    auto take_scales = [&]() __attribute__((always_inline)) {
         if constexpr (kF8) {
-            const int kblocks = (K + kScaleBlock - 1) / kScaleBlock, rows = (M + kScaleBlock - 1) / kScaleBlock, at = kb < kblocks ? kb : kblocks - 1;
-            const uint32_t mod = A.part[t.pi].m, magic = A.part[t.pi].magic, pow12 = A.part[t.pi].pow12;
-#pragma unroll
-            for (int i = 0; i < kTabRounds; i++) {
-                const int at256 = __builtin_amdgcn_readfirstlane(tid >> 8) + i * (TL::T / 256);      // (a wave's threads share a table)
-                if (at256 >= kTabs) break;
-                const int rb = t.by * kTabs + at256;
-                const int32_t S = f8_scales[(int64_t)(rb < rows ? rb : rows - 1) * kblocks + at];
-                // |S| below 2^31 in two steps
-                const uint32_t a = S < 0 ? 0u - (uint32_t)S : (uint32_t)S;
-                auto red1 = [&](uint32_t v) __attribute__((always_inline)) { return v - mul24(mulhi(v, magic), mod); };
-                const uint32_t hi = red1(a >> 12), s0 = red1(hi * pow12 + (a & 4095u)), s1 = S < 0 && s0 ? mod - s0 : s0, r = red1(f8_residue * s1);
-                s_f8[((kb & 1) * kTabs + at256) * 256 + (tid & 255)] = (uint8_t)(2 * r > mod ? r - mod : r);
+            // |S| up to 2^31 in two steps
+            const int32_t v = f8_loaded;
+            const uint32_t a = v < 0 ? 0u - (uint32_t)v : (uint32_t)v, pow12 = 4096u - mul24(mulhi(4096u, f8_magic), f8_mod);
+            auto red1 = [&](uint32_t n) __attribute__((always_inline)) { return n - mul24(mulhi(n, f8_magic), f8_mod); };
+            const uint32_t r = red1(mul24(red1(a >> 12), pow12) + (a & 4095u));
+            f8_scale = v < 0 && r ? f8_mod - r : r;
+        }
+    };
+    auto open_table = [&](const Tile& t) __attribute__((always_inline)) {
+        if constexpr (kF8) {
+            f8_mod = A.part[t.pi].m; f8_magic = A.part[t.pi].magic;
+            const uint32_t mag = f8_magnitude(tid & 0x7f) % f8_mod;
+            f8_residue = (tid & 0x80) && mag ? f8_mod - mag : mag;
+            take_scales();
+        }
+    };
+    // the table of inputs 128 kb .. 128 kb + 127 (past the end: any)
+    auto make_f8 = [&](int kb) __attribute__((always_inline)) {
+        if constexpr (kF8) {
+            if ((kb & 63) == 0 && kb) { load_scales(kb >> 6); take_scales(); }
+            if (wave_ < 4) {
+                const uint32_t v = mul24(f8_residue, lane_of(f8_scale, kb & 63)), r = v - mul24(mulhi(v, f8_magic), f8_mod);
+                s_f8[(kb & 1) * 256 + tid] = (uint8_t)(kSigned && 2 * r > f8_mod ? r - f8_mod : r);
             }
         }
     };
@@ -443,7 +456,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         constexpr int kProducts = dn * FB, kReads = FB + 2 * dn, kSlots = kProducts > 4 ? kProducts : 4;
         Tile next = tile;
         Begun begun = {0, 0};
-        make_table(tile.pi); open_table(tile); make_f8(tile, 0);        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
+        make_table(tile.pi); open_table(tile); make_f8(0);        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
         more = TL::PERSIST && next_tile(next);
         if (more) begun = begin(next);
         wait_loads<(S - 2) * GP>();         // all weights and the labels of stage 0
@@ -475,12 +488,12 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         };
         Operands o0, o1;
         int t = 0;
+        uint32_t look[kF8 && kDirect ? 4 * FB : 4][4];
         auto half = [&](const Operands& now, Operands& next, bool there, auto u, auto second) __attribute__((always_inline)) {
             constexpr int U = decltype(u)::value, kHalf = decltype(second)::value, kLoads = kHalf ? kWLoads : GP;
             constexpr integral_constant<int, (U + 1) % kUnroll> u1{};
             constexpr integral_constant<int, (U + 2) % kUnroll> u2{};
             constexpr integral_constant<int, (U + S - 1) % S> before{};
-            uint32_t look[kF8 && kDirect ? 4 * FB : 2][4];
 #pragma unroll
             for (int m = 0; m < kSlots; m++) {
                 if (m < kProducts && there) multiply(now, m);
@@ -488,30 +501,32 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                 for (int i = 0; i < kReads; i++)
                     if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) { if constexpr (kHalf) read(next, u1, 0, i); else read(next, u, 1, i); }
                 if constexpr (kF8 && !kDirect) {
-                    // As with 4-bit weights, half of the lane's 16 codes in each half; the tables of the 128 inputs that stage t + 2 (even) begins are made in the first half.
-                    if (m == 0 && !kHalf && !(t & 1)) make_f8(tile, (t >> 1) + 1);
+                    // The lane's 16 codes of stage t + 2 come in the second half of stage t, are looked up from its end to the first slots of stage t + 1, and their bytes go out at the
+                    // end of its first half; the tables of the 128 inputs that stage t + 2 (even) begins are made in the first half of stage t.
+                    if (m == 0 && !kHalf && !(t & 1)) make_f8((t >> 1) + 1);
                     if (kHalf && m == 0) fetch_codes(u2, 0);
                     const uint32_t base = f8_base + ((uint32_t)(t + kHalf + 1) >> 1 & 1) * 256;         // of stage t + 2, in the first half of stage t + 1
 #pragma unroll
-                    for (int i = 0; i < 2; i++) {
-                        const int s = kHalf ? kSlots / 4 + i * kSlots / 4 : i * kSlots / 4;
-                        if (s == m) look4(look[i], code[0][0][2 * !kHalf + i], base);
-                        if (s + kSlots / 4 == m || (s + kSlots / 4 >= kSlots && m == kSlots - 1 && s != m)) bytes[0][2 * !kHalf + i] = join4(look[i]);
+                    for (int i = 0; i < 2; i++)
+                        if (m == (kHalf ? kSlots * 5 / 8 + i * kSlots / 4 : i * kSlots / 4)) look4(look[2 * !kHalf + i], code[0][0][2 * !kHalf + i], base);
+                    if (!kHalf && m == kSlots - 2) {
+#pragma unroll
+                        for (int i = 0; i < 4; i++) bytes[0][i] = join4(look[i]);
+                        *(u32x4*)(exp8_to + ((U + 1) & 1) * kExp) = bytes[0];
                     }
-                    if (!kHalf && m == kSlots - 2) *(u32x4*)(exp8_to + ((U + 1) & 1) * kExp) = bytes[0];
                 } else if constexpr (kF8) {
                     // Codes of the next stage's half of the same number, and the bytes of the half whose codes are there.  The tables of the 128 inputs that
                     // the next stage begins are made in the first half, in front of the barrier.
                     static_assert(FB == WT, "a wave expands what it multiplies");
                     if (m == 0) fetch_codes(u1, kHalf);
-                    if (m == 0 && !kHalf && (WK == 2 || (t & 1))) make_f8(tile, WK == 2 ? t + 1 : (t + 1) >> 1);
+                    if (m == 0 && !kHalf && (WK == 2 || (t & 1))) make_f8(WK == 2 ? t + 1 : (t + 1) >> 1);
                     const uint32_t kb = WK == 2 ? (uint32_t)(t + kHalf) : (uint32_t)(t + kHalf) >> 1;      // of the half that is expanded
                     // (in the first slots, the results taken some slots later)
 #pragma unroll
                     for (int i = 0; i < 4 * FB; i++) {
                         const int s = i * kSlots / (8 * FB);
-                        if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + ((kb & 1) * kTabs + wf * FB * 32 / kScaleBlock) * 256);
-                        if (s + kSlots / 4 == m) next.b[i / 4][i % 4] = (int)join4(look[i]);
+                        if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + (kb & 1) * 256);
+                        if (s + kSlots / 2 == m) next.b[i / 4][i % 4] = (int)join4(look[i]);
                     }
                 } else if constexpr (kDirect) {
                     static_assert(FB == WT, "a wave expands what it multiplies");
@@ -555,18 +570,14 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         if constexpr (kF8 && !kDirect) {
             fetch_codes(k1, 0);
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                uint32_t look[4];
-                look4(look, code[0][0][i], f8_base);
-                bytes[0][i] = join4(look);
-            }
+            for (int i = 0; i < 2; i++) look4(look[i], code[0][0][i], f8_base);
         } else if constexpr (kF8) {
             fetch_codes(k0, 0);
             fetch_codes(k0, 1);
 #pragma unroll
             for (int i = 0; i < 4 * FB; i++) {
                 uint32_t look[4];
-                look4(look, code[0][i / 4][i % 4], f8_base + wf * FB * 32 / kScaleBlock * 256);
+                look4(look, code[0][i / 4][i % 4], f8_base);
                 o0.b[i / 4][i % 4] = (int)join4(look);
             }
         } else if constexpr (kDirect) {
@@ -671,6 +682,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     __syncthreads();
     if (!next_tile(tile)) return;
     const Begun begun0 = begin(tile);
+    open_scales(tile);
     open_weights(tile);
     fill_weights(fill_weights, k0);
     g = groups_of(begun0);
@@ -687,7 +699,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
 
 // what the launches of every tile share; work and bytes for the profile
 struct ExpWork { ExpArgs A; double macs, bytes; PrimeClasses classes; };
-inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, ExpWork& work) {
+inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, ExpWork& work, bool by_class = false) {
     ExpArgs& A = work.A;
     memset(&A, 0, sizeof(A));
     A.w = L.w; A.expert_bytes = matrix_bytes(L.format, L.M, L.K); A.bias = L.bias;
@@ -698,13 +710,13 @@ inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labe
     A.plain = L.bias == nullptr;
     for (int i = 0; i <= DASH_MAX_PRIMES; i++) A.chunk_first[i] = 0x7fffffff;
     A.chunk_first[0] = 0;
-    const bool by_class = L.format == DASH_F8;
+    work.classes = {};
     if (by_class) {
         const PrimeClasses& C = work.classes = prime_classes(c);
         for (int i = 0; i <= C.n; i++) A.part_first[i] = C.chunk_first[i];
         for (int i = 0; i < C.n; i++) {
             const uint32_t m = (uint32_t)C.modulus[i];
-            A.part[i] = {m, (uint32_t)(((1ull << 32) + m - 1) / m), 4096u % m};
+            A.part[i] = {m, (uint32_t)(((1ull << 32) + m - 1) / m)};
         }
     }
     for (int at = 0; at < c->k; at++) {
@@ -714,6 +726,10 @@ inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labe
         A.chunk_first[at + 1] = A.chunk_first[at] + (int)Mi.nchunk;
         P.chunk_first = A.chunk_first[at];
         P.p = c->prime[i]; P.mmagic = Mi.mmagic; P.pow12 = 4096u % P.p;
+        if (!by_class) {
+            A.part_first[at + 1] = A.chunk_first[at + 1];
+            A.part[at] = {P.p, P.mmagic};
+        }
         P.one = L.bias ? (L.garble ? c->d_one0[i] : c->d_one[i]) : nullptr;
         P.in = view_of(in, i); P.out = view_of(out, i);
         const uint64_t p1 = P.p - 1;
@@ -732,11 +748,11 @@ inline int experts_args(const dash_ctx* c, const ExpertsCall& L, const dash_labe
 }
 template <int FMT, class TL> int launch_experts(dash_ctx* c, const ExpertsCall& L, ExpWork& work, hipStream_t s) {
     ExpArgs& A = work.A;
-    constexpr TileParts parts = FMT == DASH_W8 ? PARTS_NONE : FMT == DASH_MX4 ? PARTS_PRIMES : PARTS_CLASSES;
+    constexpr TileParts parts = kTileKind[TL::KIND].parts;
+    static_assert((FMT == DASH_W8) == (parts == PARTS_NONE) && (FMT != DASH_MX4 || parts == PARTS_PRIMES), "tiles of the format");
     int64_t cols = 0;
     if (L.routing) {
         constexpr int s = TL::KIND;
-        static_assert(kTileKind[s].parts == parts, "tiles of the format");
         cols = L.routing->max_tiles[s];
         A.rows = L.routing->rows; A.tiles = L.routing->tiles[s]; A.n_tiles = L.routing->first_tile[s] + L.E + 1;
     } else if (parts != PARTS_NONE) {
@@ -759,9 +775,9 @@ template <int FMT, class TL> int launch_experts(dash_ctx* c, const ExpertsCall& 
     DASH_HIP(hipGetLastError());
     return DASH_OK;
 }
-inline ExpertsShape experts_shape(const dash_ctx* c, const ExpertsCall& L, const ExpArgs& A) {
+inline ExpertsShape experts_shape(const dash_ctx* c, const ExpertsCall& L) {
     ExpertsShape shape{L.n, L.E, L.M, L.K, L.format != DASH_W8, c->k, {}};
-    for (int i = 0; i < c->k; i++) shape.chunks[i] = A.chunk_first[i + 1] - A.chunk_first[i];
+    for (int i = 0; i < c->k; i++) shape.chunks[i] = (int)c->mods[c->prime[i]].nchunk;
     return shape;
 }
 
