@@ -316,11 +316,9 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     // the table of inputs 128 kb .. 128 kb + 127 (past the end: any)
     auto make_f8 = [&](int kb) __attribute__((always_inline)) {
         if constexpr (kF8) {
-            if ((kb & 63) == 0 && kb) { load_scales(kb >> 6); take_scales(); }
-            if (wave_ < 4) {
-                const uint32_t v = mul24(f8_residue, lane_of(f8_scale, kb & 63)), r = v - mul24(mulhi(v, f8_magic), f8_mod);
-                s_f8[(kb & 1) * 256 + tid] = (uint8_t)(kSigned && 2 * r > f8_mod ? r - f8_mod : r);
-            }
+            // (without a branch for the waves past the fourth, which write the same again: a branch amid the products makes the reads around it be waited for)
+            const uint32_t v = mul24(f8_residue, lane_of(f8_scale, kb & 63)), r = v - mul24(mulhi(v, f8_magic), f8_mod);
+            s_f8[(kb & 1) * 256 + (tid & 255)] = (uint8_t)(kSigned && 2 * r > f8_mod ? r - f8_mod : r);
         }
     };
     // four codes' bytes; base: the table's address in LDS (a multiple of 256, below 2^24)
@@ -328,9 +326,11 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
 #pragma unroll
         for (int i = 0; i < 4; i++) r[i] = *(lds_ptr)(uintptr_t)__builtin_amdgcn_perm(x, base, 0x0c020104u + (uint32_t)i);
     };
-    auto join4 = [&](const uint32_t (&r)[4]) __attribute__((always_inline)) -> uint32_t { return (r[0] | r[1] << 8) | (r[2] | r[3] << 8) << 16; };
+    auto join4 = [&](const uint32_t (&r)[4]) __attribute__((always_inline)) -> uint32_t {
+        return __builtin_amdgcn_perm(r[1], r[0], 0x0c0c0400u) | __builtin_amdgcn_perm(r[3], r[2], 0x04000c0cu);
+    };
     const uint32_t f8_base = (uint32_t)(uintptr_t)(lds_ptr)s_f8;
-    constexpr int kUnroll = S == 3 ? (kDirect ? 3 : 6) : S;         // stages of a round of the loop: slots and parities are known in each
+    constexpr int kUnroll = S == 3 ? 6 : S;         // stages of a round of the loop: slots and parities are known in each
     // A lane's 16 bytes of codes are 16 weights of a row's first block of 32 and 16 of its second (low and high halves of the bytes); shifts of
     // both blocks, table entries of both, then four weights at a time as bytes.
     // In registers (a wave's weights are its own: kDirect): lane (j32, h) holds what it multiplies, two stages in the making.
@@ -501,32 +501,37 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                 for (int i = 0; i < kReads; i++)
                     if (i / 2 == m || (m == kSlots - 1 && i / 2 > m)) { if constexpr (kHalf) read(next, u1, 0, i); else read(next, u, 1, i); }
                 if constexpr (kF8 && !kDirect) {
-                    // The lane's 16 codes of stage t + 2 come in the second half of stage t, are looked up from its end to the first slots of stage t + 1, and their bytes go out at the
-                    // end of its first half; the tables of the 128 inputs that stage t + 2 (even) begins are made in the first half of stage t.
-                    if (m == 0 && !kHalf && !(t & 1)) make_f8((t >> 1) + 1);
+                    // The lane's 16 codes of stage t + 2 come in the second half of stage t, half of them are looked up in it, half in the first half of stage t + 1, at the end of
+                    // which their bytes go out; the tables of the 128 inputs that stage t + 2 (even) begins are made in the first half of stage t.
+                    if (m == 0 && !kHalf && !(U & 1)) make_f8((t >> 1) + 1);
                     if (kHalf && m == 0) fetch_codes(u2, 0);
                     const uint32_t base = f8_base + ((uint32_t)(t + kHalf + 1) >> 1 & 1) * 256;         // of stage t + 2, in the first half of stage t + 1
 #pragma unroll
-                    for (int i = 0; i < 2; i++)
-                        if (m == (kHalf ? kSlots * 5 / 8 + i * kSlots / 4 : i * kSlots / 4)) look4(look[2 * !kHalf + i], code[0][0][2 * !kHalf + i], base);
-                    if (!kHalf && m == kSlots - 2) {
-#pragma unroll
-                        for (int i = 0; i < 4; i++) bytes[0][i] = join4(look[i]);
-                        *(u32x4*)(exp8_to + ((U + 1) & 1) * kExp) = bytes[0];
+                    for (int i = 0; i < 2; i++) {
+                        const int dword = 2 * !kHalf + i;
+                        if (m == (kHalf ? kSlots * 3 / 8 : 0) + i * kSlots / 8) look4(look[i], code[0][0][dword], base);
+                        if (m == (kHalf ? kSlots - 1 : kSlots * 5 / 8)) {
+                            bytes[0][dword] = join4(look[i]);
+                            if (kHalf) asm volatile("" : "+v"(bytes[0][dword]));          // (here, not in the next stage, where it would be waited for at once)
+                        }
                     }
+                    if (!kHalf && m == kSlots - 2) *(u32x4*)(exp8_to + ((U + 1) & 1) * kExp) = bytes[0];
                 } else if constexpr (kF8) {
                     // Codes of the next stage's half of the same number, and the bytes of the half whose codes are there.  The tables of the 128 inputs that
                     // the next stage begins are made in the first half, in front of the barrier.
                     static_assert(FB == WT, "a wave expands what it multiplies");
                     if (m == 0) fetch_codes(u1, kHalf);
-                    if (m == 0 && !kHalf && (WK == 2 || (t & 1))) make_f8(WK == 2 ? t + 1 : (t + 1) >> 1);
+                    if (m == 0 && !kHalf && (WK == 2 || (U & 1))) make_f8(WK == 2 ? t + 1 : (t + 1) >> 1);
                     const uint32_t kb = WK == 2 ? (uint32_t)(t + kHalf) : (uint32_t)(t + kHalf) >> 1;      // of the half that is expanded
                     // (in the first slots, the results taken some slots later)
 #pragma unroll
                     for (int i = 0; i < 4 * FB; i++) {
                         const int s = i * kSlots / (8 * FB);
                         if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + (kb & 1) * 256);
-                        if (s + kSlots / 2 == m) next.b[i / 4][i % 4] = (int)join4(look[i]);
+                        if (s + kSlots / 2 == m) {
+                            next.b[i / 4][i % 4] = (int)join4(look[i]);
+                            if (kHalf) asm volatile("" : "+v"(next.b[i / 4][i % 4]));
+                        }
                     }
                 } else if constexpr (kDirect) {
                     static_assert(FB == WT, "a wave expands what it multiplies");
@@ -563,14 +568,23 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
             else wait_loads<kInFlight>();
             lds_barrier();
             half(o1, o0, there, u, k1);
-            return ++t < (nk + WK - 1) / WK;
+            t++;
+            if constexpr (kF8) {
+                // the table that stage t makes is the first of 64 more
+                constexpr int kPer = WK == 2 ? 64 : 128, kAt = WK == 2 ? 63 : kDirect ? 127 : 126;
+                if (__builtin_expect((t & (kPer - 1)) == kAt, 0)) { load_scales(t / kPer + 1); take_scales(); }
+            }
+            return t < (nk + WK - 1) / WK;
         };
 #pragma unroll
         for (int i = 0; i < kReads; i++) read(o0, k0, 0, i);
         if constexpr (kF8 && !kDirect) {
             fetch_codes(k1, 0);
 #pragma unroll
-            for (int i = 0; i < 2; i++) look4(look[i], code[0][0][i], f8_base);
+            for (int i = 0; i < 2; i++) {
+                look4(look[i], code[0][0][i], f8_base);
+                bytes[0][i] = join4(look[i]);
+            }
         } else if constexpr (kF8) {
             fetch_codes(k0, 0);
             fetch_codes(k0, 1);
@@ -594,7 +608,6 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         constexpr integral_constant<int, 2> k2{};
         constexpr integral_constant<int, 3> k3{};
         if constexpr (kUnroll == 6) while (stage(k0) && stage(k1) && stage(k2) && stage(k3) && stage(integral_constant<int, 4>{}) && stage(integral_constant<int, 5>{})) {}
-        else if constexpr (kUnroll == 3) while (stage(k0) && stage(k1) && stage(k2)) {}
         else while (stage(k0) && stage(k1) && stage(k2) && stage(k3)) {}
         wait_loads<0>();
         if constexpr (WK > 1) {
