@@ -58,8 +58,8 @@ inline int64_t total_chunks(const dash_ctx* c) {
     for (int i = 0; i < c->k; i++) n += c->mods[c->prime[i]].nchunk;
     return n;
 }
-// Residues of a weight modulo a product m of primes serve all of these primes: with m <= 255, between -127 and 127, they are signed bytes.  Classes: the largest prime that is left, and
-// as many more as fit, large ones first (2 to 37: 37 5, 31 7, 29 3 2, 23 11, 19 13, 17; one row of these is 7 tiles of 8 groups instead of the primes' 12).
+// Residues of a weight modulo a product m of primes serve all of these primes: with m <= 240, less than 128 from zero, they are signed bytes.  Classes: the largest prime that is left, and
+// as many more as fit, large ones first (2 to 37: 37 5, 31 7, 29 3 2, 23, 19 11, 17 13; one row of these is 7 tiles of 8 groups instead of the primes' 12).
 struct PrimeClasses {
     int n;                                  // classes
     int order[DASH_MAX_PRIMES];             // indexes of the primes, class after class
@@ -75,7 +75,7 @@ inline PrimeClasses prime_classes(const dash_ctx* c) {
         for (;;) {
             int best = -1;
             for (int i = 0; i < c->k; i++)
-                if (!done[i] && m * c->prime[i] <= 255 && (best < 0 || c->prime[i] > c->prime[best])) best = i;
+                if (!done[i] && m * c->prime[i] <= 240 && (best < 0 || c->prime[i] > c->prime[best])) best = i;
             if (best < 0) break;
             done[best] = true;
             r.order[at++] = best;

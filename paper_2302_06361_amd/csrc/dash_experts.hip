@@ -112,7 +112,7 @@ struct PrepArgs8 {
     int64_t row_stride, expert_stride, tiles;       // tiles of all experts
     int64_t first;                                  // the launch's first lane
     int64_t expert_bytes;                           // of a prepared matrix
-    int M, K;
+    int M, K, f8;
     uint8_t* out;
 };
 // a lane per 16-byte piece of a tile
@@ -129,6 +129,12 @@ __global__ __launch_bounds__(kThreads) void k_weights8_prepare(const PrepArgs8 A
         else
             for (int i = 0; i < 16; i++)
                 if (col + i < A.K) v[i / 4] |= (uint32_t)(uint8_t)src[i] << (8 * (i % 4));
+        if (A.f8)
+            for (int i = 0; i < 4; i++) {
+                // codes of no number (all seven bits) to zeros: the carry of 1 to the sign's place, and 0x80 - 1 with it
+                const uint32_t none = ((v[i] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+                v[i] &= ~(none | (none - (none >> 7)));
+            }
     }
     *(uint4*)(A.out + e * A.expert_bytes + at * kW8Tile + w8_at(r, 16 * q)) = make_uint4(v[0], v[1], v[2], v[3]);
 }
@@ -511,7 +517,7 @@ static int64_t weight_tiles(const void* w, int64_t row_stride, int64_t expert_st
 static int lay_out_bytes(int format, const int8_t* w, int64_t row_stride, int64_t expert_stride, int64_t tiles, int out_c, int K, void* prepared, hipStream_t s) {
     const int64_t lanes = tiles * (kW8Tile / 16);
     if (lanes > kMaxLanes) return DASH_ESIZE;
-    PrepArgs8 A{w, row_stride, expert_stride, tiles, 0, matrix_bytes(format, out_c, K), out_c, K, (uint8_t*)prepared};
+    PrepArgs8 A{w, row_stride, expert_stride, tiles, 0, matrix_bytes(format, out_c, K), out_c, K, format == DASH_F8, (uint8_t*)prepared};
     in_launches((lanes + kThreads - 1) / kThreads, [&](int64_t first, uint32_t blocks) {
         A.first = first * kThreads;
         hipLaunchKernelGGL(k_weights8_prepare, dim3(blocks), dim3(kThreads), 0, s, A);

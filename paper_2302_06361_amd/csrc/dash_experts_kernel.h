@@ -46,6 +46,10 @@ typedef int v16i __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) uint8_t* lds_ptr;
 typedef __attribute__((address_space(3))) v2i* lds_v2i;
+// addresses that come as numbers are device memory's (of accesses that could be LDS the compiler waits for all of LDS, lgkmcnt(0), from there on)
+typedef __attribute__((address_space(1))) uint8_t* global_ptr;
+typedef __attribute__((address_space(1))) u32x4* global_u32x4;
+typedef const __attribute__((address_space(1))) uint32_t* global_u32;
 
 // WK sets of WD x WF waves (along the inputs; along digits, along features), a wave DA x FB tiles of 32 digits x 32 features; S stages of 64
 // inputs in LDS for each set; KIND: tiles of the routing; PERSIST: a block takes tile after tile (one block per CU)
@@ -109,8 +113,12 @@ __device__ __forceinline__ v4i buffer_of(const uint8_t* p, uint32_t bytes) {
 }
 __device__ __forceinline__ uint32_t lane_of(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
 __device__ __forceinline__ uint64_t lane_of(uint64_t v, int lane) { return lane_of((uint32_t)v, lane) | (uint64_t)lane_of((uint32_t)(v >> 32), lane) << 32; }
-// the wave's LDS accesses done, then the block's barrier (loads stay in flight)
-__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// The wave's LDS accesses done, then the block's barrier (loads stay in flight).  The wait behind it has nothing to wait for: it tells the compiler, which does not see the other,
+// that no scalar load is out, whose end it would have to expect before every LDS result (lgkmcnt(0) everywhere, fresh reads waited for in front of products).
+__device__ __forceinline__ void lds_barrier() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);
+}
 // at most N loads of the wave outstanding
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 template <int FMT, class TL>
@@ -120,7 +128,8 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr bool kPart = kMx4 || kF8;                 // residues of the weights: a tile is of one prime or class
     constexpr bool kDirect = kPart && TL::WD == 1;      // a wave's weights are its own: expanded in registers
     constexpr bool kHalfTile = TL::HALF;
-    constexpr bool kSigned = kTileKind[TL::KIND].parts == PARTS_CLASSES;       // residues of either sign
+    constexpr int kComputed = DASH_F8_COMPUTED;
+    constexpr bool kClass = kTileKind[TL::KIND].parts == PARTS_CLASSES;
     static_assert(!kHalfTile || (kF8 && !kDirect), "loader roles");
     static_assert(!kF8 || kDirect || kHalfTile, "steps of the expansion");
     const int M = A.M, K = A.K, nk = (K + 63) / 64;
@@ -201,8 +210,8 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     auto zeros = [&](const Tile& t) __attribute__((always_inline)) {
         const Groups z = groups_of(begin(t));
         for (int g = wave_; g < t.n_groups; g += NW * WK) {
-            uint8_t* const dst = (uint8_t*)lane_of(z.dst, g);
-            for (int j = t.by * TL::F + lane; j < M && j < t.by * TL::F + TL::F; j += 64) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
+            const global_ptr dst = (global_ptr)lane_of(z.dst, g);
+            for (int j = t.by * TL::F + lane; j < M && j < t.by * TL::F + TL::F; j += 64) *(global_u32x4)(dst + (int64_t)j * 16) = u32x4{0, 0, 0, 0};
         }
     };
     // the block's next tile with an expert
@@ -279,15 +288,19 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     };
     // ---- 8-bit floats ----
     // Code c under the scale S: 512 e4m3(c) S mod m, m the prime of the tile or the product of the primes of its class, a byte of a table of 256 for every 128 inputs.  Thread c
-    // keeps its code's residue and multiplies it by the scale's; lane l of every wave keeps the residue of scale l of 64.  (Scales by scalar loads where they are
+    // keeps its code's residue and multiplies it by the scale's; lane l of every wave keeps the residue of one of 64 scales.  (Scales by scalar loads where they are
     // wanted: waits for memory in front of the barriers, 128 rows, 4096 -> 4096: 1158 us.)
     uint32_t f8_residue = 0, f8_mod = 0, f8_magic = 0, f8_scale = 0;
+    float f8_quotient = 0, f8_factor = 0;       // of lane l: 512 a / m and 512 a (classes: 512), a the scale's residue next to zero
     const int32_t* f8_scales = nullptr;
     const int f8_blocks = (K + kScaleBlock - 1) / kScaleBlock;
     int32_t f8_loaded = 0;
-    // scales 64 i .. 64 i + 63 of the tile's row of them (past the end: the last), a load in flight
-    auto load_scales = [&](int i) __attribute__((always_inline)) {
-        if constexpr (kF8) f8_loaded = f8_scales[64 * i + lane < f8_blocks ? 64 * i + lane : f8_blocks - 1];
+    // 64 scales of the tile's row of them, from number `first` (past the end: the last), number i in lane i % 64; a load in flight
+    auto load_scales = [&](int first) __attribute__((always_inline)) {
+        if constexpr (kF8) {
+            const int i = first + ((lane - first) & 63);
+            f8_loaded = f8_scales[i < f8_blocks ? i : f8_blocks - 1];
+        }
     };
     auto open_scales = [&](const Tile& t) __attribute__((always_inline)) {
         if constexpr (kF8) {
@@ -303,6 +316,9 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
             auto red1 = [&](uint32_t n) __attribute__((always_inline)) { return n - mul24(mulhi(n, f8_magic), f8_mod); };
             const uint32_t r = red1(mul24(red1(a >> 12), pow12) + (a & 4095u));
             f8_scale = v < 0 && r ? f8_mod - r : r;
+            const float s = 512.0f * (float)((int32_t)f8_scale - (2 * f8_scale > f8_mod ? (int32_t)f8_mod : 0));
+            f8_quotient = s / (float)f8_mod;
+            f8_factor = s;
         }
     };
     auto open_table = [&](const Tile& t) __attribute__((always_inline)) {
@@ -318,7 +334,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         if constexpr (kF8) {
             // (without a branch for the waves past the fourth, which write the same again: a branch amid the products makes the reads around it be waited for)
             const uint32_t v = mul24(f8_residue, lane_of(f8_scale, kb & 63)), r = v - mul24(mulhi(v, f8_magic), f8_mod);
-            s_f8[(kb & 1) * 256 + (tid & 255)] = (uint8_t)(kSigned && 2 * r > f8_mod ? r - f8_mod : r);
+            s_f8[(kb & 1) * 256 + (tid & 255)] = (uint8_t)(kClass && 2 * r > f8_mod ? r - f8_mod : r);
         }
     };
     // four codes' bytes; base: the table's address in LDS (a multiple of 256, below 2^24)
@@ -328,6 +344,34 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     };
     auto join4 = [&](const uint32_t (&r)[4]) __attribute__((always_inline)) -> uint32_t {
         return __builtin_amdgcn_perm(r[1], r[0], 0x0c0c0400u) | __builtin_amdgcn_perm(r[3], r[2], 0x04000c0cu);
+    };
+    // The same by arithmetic: W = 512 e4m3 a, k the integer next to W / m, W - m k.  Of the sums with 1.5 2^23 the low bits are the integers next to the products; of the last only a byte
+    // is wanted, so that its 24-bit product may take them as they are.  Primes to 37: |a| <= 18, |W| < 2^22 stands in the sum as it is.  Else the low bits of 512 e4m3 times a.
+    // The quotient is off by at most 2^17 2^-24, the result at most by m / 2 + 1.5: below 128 with m <= 240.
+    float f8_k = 0, f8_w = 0;
+    uint32_t f8_a = 0;
+    auto set_scale = [&](int kb) __attribute__((always_inline)) {
+        if constexpr (kF8 && kDirect) {
+            f8_k = __uint_as_float(lane_of(__float_as_uint(f8_quotient), kb & 63));
+            f8_w = __uint_as_float(lane_of(__float_as_uint(f8_factor), kb & 63));
+            if constexpr (kClass) { f8_a = (uint32_t)((int)f8_w >> 9) & 0xffu; f8_w = 512.0f; }
+        }
+    };
+    float f8_one = 12582912.0f;
+    asm volatile("" : "+v"(f8_one));
+    auto compute4 = [&](uint32_t x) __attribute__((always_inline)) -> uint32_t {
+        typedef float v2f __attribute__((ext_vector_type(2)));
+        const v2f lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+        const float v[4] = {lo[0], lo[1], hi[0], hi[1]};
+        uint32_t r[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            const uint32_t k = __float_as_uint(fmaf(v[i], f8_k, f8_one));
+            uint32_t w = __float_as_uint(fmaf(v[i], f8_w, f8_one));
+            if constexpr (kClass) w = mul24(w & 0xffffffu, f8_a);
+            r[i] = mul24(k & 0xffffffu, 256u - f8_mod) + w;
+        }
+        return join4(r);
     };
     const uint32_t f8_base = (uint32_t)(uintptr_t)(lds_ptr)s_f8;
     constexpr int kUnroll = S == 3 ? 6 : S;         // stages of a round of the loop: slots and parities are known in each
@@ -430,7 +474,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr integral_constant<int, 0> k0{};
     constexpr integral_constant<int, 1> k1{};
     // loads that may be in flight at the barrier of stage t: those behind the labels of stage t + 1, 4-bit: behind the weights of stage t + 2
-    static_assert(S == 4 || (kF8 && S == 3), "the loop's slots; parities of stages follow from slots; the waits of the first stages");
+    static_assert(S == 4 || (kF8 && (S == 3 || S == 6)), "the loop's slots; parities of stages follow from slots; the waits of the first stages");
     constexpr int kInFlight = kPart ? (S - 3) * kParts + GP : (S - 2) * kParts;
     // the first stages: all weights, then labels (these wait for the rows' numbers), but for the labels of stage S - 1
     auto fill_weights = [&](auto self, auto u) __attribute__((always_inline)) -> void {
@@ -456,7 +500,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         constexpr int kProducts = dn * FB, kReads = FB + 2 * dn, kSlots = kProducts > 4 ? kProducts : 4;
         Tile next = tile;
         Begun begun = {0, 0};
-        make_table(tile.pi); open_table(tile); make_f8(0);        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
+        make_table(tile.pi); open_table(tile); make_f8(0); set_scale(0);        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
         more = TL::PERSIST && next_tile(next);
         if (more) begun = begin(next);
         wait_loads<(S - 2) * GP>();         // all weights and the labels of stage 0
@@ -523,9 +567,18 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                     if (m == 0) fetch_codes(u1, kHalf);
                     if (m == 0 && !kHalf && (WK == 2 || (U & 1))) make_f8(WK == 2 ? t + 1 : (t + 1) >> 1);
                     const uint32_t kb = WK == 2 ? (uint32_t)(t + kHalf) : (uint32_t)(t + kHalf) >> 1;      // of the half that is expanded
-                    // (in the first slots, the results taken some slots later)
+                    // (in the first slots, the results taken some slots later; the last kComputed of four by arithmetic)
+                    if (m == 0) set_scale((int)kb);
 #pragma unroll
                     for (int i = 0; i < 4 * FB; i++) {
+                        if (i % 4 >= 4 - kComputed) {
+                            const int c = i / 4 * kComputed + i % 4 - (4 - kComputed);
+                            if (c * kSlots / (kComputed * FB) == m) {
+                                next.b[i / 4][i % 4] = (int)compute4(code[!kHalf][i / 4][i % 4]);
+                                if (kHalf) asm volatile("" : "+v"(next.b[i / 4][i % 4]));
+                            }
+                            continue;
+                        }
                         const int s = i * kSlots / (8 * FB);
                         if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + (kb & 1) * 256);
                         if (s + kSlots / 2 == m) {
@@ -563,16 +616,16 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
             half(o0, o1, there, u, k0);
             // (of the first stages the weights went out first: fewer loads stand behind the labels of stage t + 1)
             constexpr int U = decltype(u)::value;
-            if (U == 0 && t == 0) wait_loads<(S - 2) * GP>();
-            else if (U == 1 && !kPart && t == 1) wait_loads<(S - 2) * GP + 2 * WT>();
+            constexpr int kEarly = kPart ? S - 3 : S - 2;
+            if (U < kEarly && t == U) wait_loads<(S - 2) * GP + (U < kEarly ? U : 0) * kWLoads>();
             else wait_loads<kInFlight>();
             lds_barrier();
             half(o1, o0, there, u, k1);
             t++;
             if constexpr (kF8) {
-                // the table that stage t makes is the first of 64 more
-                constexpr int kPer = WK == 2 ? 64 : 128, kAt = WK == 2 ? 63 : kDirect ? 127 : 126;
-                if (__builtin_expect((t & (kPer - 1)) == kAt, 0)) { load_scales(t / kPer + 1); take_scales(); }
+                // stage t makes the table of scale number 64, 96, 128 ...: that one and 31 behind it in place of the 32 oldest (the one before it is still in use)
+                constexpr int kPer = WK == 2 ? 32 : 64, kAt = WK == 2 ? 31 : kDirect ? 63 : 62;
+                if (__builtin_expect((t & (kPer - 1)) == kAt && t > kPer, 0)) { load_scales(32 * (t / kPer)); take_scales(); }
             }
             return t < (nk + WK - 1) / WK;
         };
@@ -655,7 +708,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                 const int g0 = (wd * DA + d) * 2;
                 if (g0 >= done.n_groups) break;
                 const uint64_t dst0 = lane_of(gd.dst, g0), dst1 = lane_of(gd.dst, g0 + 1);
-                uint8_t* const dst = (uint8_t*)(h ? dst1 : dst0);
+                const global_ptr dst = (global_ptr)(h ? dst1 : dst0);
                 const bool valid = g0 + h < done.n_groups;
 #pragma unroll
                 for (int f = 0; f < FB; f++) {
@@ -675,7 +728,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                             if (A.bias) {
                                 const int32_t b = j < M ? A.bias[(int64_t)done.e * M + j] % (int32_t)prime : 0;
                                 const uint32_t bm = (uint32_t)(b < 0 ? b + (int32_t)prime : b);
-                                const uint32_t* const one = (const uint32_t*)lane_of(gd.one, g0 + g);
+                                const global_u32 one = (global_u32)lane_of(gd.one, g0 + g);
 #pragma unroll
                                 for (int r = 0; r < 8; r++) v[r] = red1(v[r]) + __umul24(bm, (one[2 * (r / 4) + h] >> (8 * (r % 4))) & 0xffu);
                             }
@@ -685,7 +738,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                     }
                     // lanes 0-31 hold dwords 0, 2 of both groups, lanes 32-63 dwords 1, 3: after the swaps the first half holds the first group
                     const auto lo = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), hi = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-                    if (valid && j < M) *(u32x4*)(dst + (int64_t)j * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                    if (valid && j < M) *(global_u32x4)(dst + (int64_t)j * 16) = u32x4{lo[0], lo[1], hi[0], hi[1]};
                     __builtin_amdgcn_sched_barrier(0);      // (else all accumulators are read at once)
                 }
             }
