@@ -259,7 +259,7 @@ int dash_ctx_create(dash_ctx** out, const uint16_t* primes, int k, int lambda_ru
     c->pack_run_log2 = -1;
     if (const char* e = getenv("DASH_PACK_RUN_LOG2")) c->pack_run_log2 = e[0] >= '0' && e[0] <= '9' ? e[0] - '0' : -1;    // tuning and test hook
     if (const char* e = getenv("DASH_GEMM_TILE")) c->gemm_tile = e[0] == 'w' ? 2 : e[0] == 'b' ? 1 : 0;      // "wide" / "big"
-    if (const char* e = getenv("DASH_EXPERTS_TILE")) c->experts_tile = e[0] == 'b' ? 1 : e[0] == 'n' ? 2 : e[0] == 'f' ? 3 : e[0] == 'w' ? 4 : 0;         // "big" / "narrow" / "few" / "wide"
+    if (const char* e = getenv("DASH_EXPERTS_TILE")) c->experts_tile = e[0] == 'b' ? 1 : e[0] == 'n' ? 2 : e[0] == 'f' ? 3 : e[0] == 'w' ? 4 : e[0] == 'c' ? 5 : e[0] == 's' ? 6 : 0;         // "big" / "narrow" / "few" / "wide" / "class" / "small"
     c->prof = new (std::nothrow) ProfState();
     c->P = 1;
     for (int i = 0; i < k; i++) { c->prime[i] = primes[i]; c->P *= primes[i]; }

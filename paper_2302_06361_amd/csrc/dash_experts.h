@@ -37,7 +37,7 @@ __host__ __device__ inline int w8_at(int row, int col) { return 64 * row + 16 * 
 enum TileParts { PARTS_NONE = 0, PARTS_PRIMES = 1, PARTS_CLASSES = 2 };
 struct TileKind { int groups; TileParts parts; };
 constexpr int kTileKinds = 8;
-constexpr TileKind kTileKind[kTileKinds] = {{16, PARTS_NONE}, {8, PARTS_NONE}, {16, PARTS_PRIMES}, {8, PARTS_PRIMES}, {4, PARTS_PRIMES}, {8, PARTS_CLASSES}, {32, PARTS_PRIMES}, {32, PARTS_CLASSES}};
+constexpr TileKind kTileKind[kTileKinds] = {{16, PARTS_NONE}, {8, PARTS_NONE}, {16, PARTS_PRIMES}, {8, PARTS_PRIMES}, {4, PARTS_PRIMES}, {8, PARTS_CLASSES}, {32, PARTS_PRIMES}, {16, PARTS_CLASSES}};
 struct RouteTile {          // (read as a uint4)
     uint32_t expert_prime;  // expert (n_experts: none) | index of the prime or class << 24
     int32_t start, count;   // the expert's rows: rows[start .. start + count - 1]

@@ -1,5 +1,4 @@
 // dash_experts_gemm.hip -- tiles of the products of expert layers with byte and 4-bit weights (dash_experts_kernel.h has the kernel).
-#define DASH_F8_COMPUTED 2
 #include "dash_experts_kernel.h"
 
 namespace dash {

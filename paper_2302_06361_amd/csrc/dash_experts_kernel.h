@@ -128,7 +128,6 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr bool kPart = kMx4 || kF8;                 // residues of the weights: a tile is of one prime or class
     constexpr bool kDirect = kPart && TL::WD == 1;      // a wave's weights are its own: expanded in registers
     constexpr bool kHalfTile = TL::HALF;
-    constexpr int kComputed = DASH_F8_COMPUTED;
     constexpr bool kClass = kTileKind[TL::KIND].parts == PARTS_CLASSES;
     static_assert(!kHalfTile || (kF8 && !kDirect), "loader roles");
     static_assert(!kF8 || kDirect || kHalfTile, "steps of the expansion");
@@ -175,8 +174,9 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     uint8_t* const s_raw = s_dig + S * kDig;
     uint8_t* const s_exp = s_raw + S * FT * kRaw;
     __shared__ u32x4 s_lut[kMx4 ? 256 : 1];
-    static_assert(!kF8 || TL::F == kScaleBlock, "a block's features have one row of scales");
-    __shared__ __attribute__((aligned(512))) uint8_t s_f8[kF8 ? 512 : 16];      // tables of two blocks of 128 inputs
+    static_assert(!kF8 || kScaleBlock % TL::F == 0, "a block's features have one row of scales");
+    constexpr int kTabs = WK == 4 ? 2 : 1;                          // blocks of 128 inputs that a round of the sets' stages begins
+    __shared__ __attribute__((aligned(256))) uint8_t s_f8[kF8 ? 2 * kTabs * 256 : 16];     // their tables, of this round and the next
 
     // the primes, for lanes that each want another
     struct PrimeLds { uint64_t in, in_cs, out, out_cs, one; uint32_t p, mmagic, pow12, start, chunk_first, pad; };
@@ -291,7 +291,6 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     // keeps its code's residue and multiplies it by the scale's; lane l of every wave keeps the residue of one of 64 scales.  (Scales by scalar loads where they are
     // wanted: waits for memory in front of the barriers, 128 rows, 4096 -> 4096: 1158 us.)
     uint32_t f8_residue = 0, f8_mod = 0, f8_magic = 0, f8_scale = 0;
-    float f8_quotient = 0, f8_factor = 0;       // of lane l: 512 a / m and 512 a (classes: 512), a the scale's residue next to zero
     const int32_t* f8_scales = nullptr;
     const int f8_blocks = (K + kScaleBlock - 1) / kScaleBlock;
     int32_t f8_loaded = 0;
@@ -304,7 +303,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     };
     auto open_scales = [&](const Tile& t) __attribute__((always_inline)) {
         if constexpr (kF8) {
-            f8_scales = (const int32_t*)(A.w + (int64_t)t.e * A.expert_bytes + scales_at(M, K)) + (int64_t)t.by * f8_blocks;
+            f8_scales = (const int32_t*)(A.w + (int64_t)t.e * A.expert_bytes + scales_at(M, K)) + (int64_t)(t.by * TL::F / kScaleBlock) * f8_blocks;
             load_scales(0);
         }
     };
@@ -316,9 +315,6 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
             auto red1 = [&](uint32_t n) __attribute__((always_inline)) { return n - mul24(mulhi(n, f8_magic), f8_mod); };
             const uint32_t r = red1(mul24(red1(a >> 12), pow12) + (a & 4095u));
             f8_scale = v < 0 && r ? f8_mod - r : r;
-            const float s = 512.0f * (float)((int32_t)f8_scale - (2 * f8_scale > f8_mod ? (int32_t)f8_mod : 0));
-            f8_quotient = s / (float)f8_mod;
-            f8_factor = s;
         }
     };
     auto open_table = [&](const Tile& t) __attribute__((always_inline)) {
@@ -334,7 +330,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         if constexpr (kF8) {
             // (without a branch for the waves past the fourth, which write the same again: a branch amid the products makes the reads around it be waited for)
             const uint32_t v = mul24(f8_residue, lane_of(f8_scale, kb & 63)), r = v - mul24(mulhi(v, f8_magic), f8_mod);
-            s_f8[(kb & 1) * 256 + (tid & 255)] = (uint8_t)(kClass && 2 * r > f8_mod ? r - f8_mod : r);
+            s_f8[(kb & (2 * kTabs - 1)) * 256 + (tid & 255)] = (uint8_t)(kClass && 2 * r > f8_mod ? r - f8_mod : r);
         }
     };
     // four codes' bytes; base: the table's address in LDS (a multiple of 256, below 2^24)
@@ -344,34 +340,6 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     };
     auto join4 = [&](const uint32_t (&r)[4]) __attribute__((always_inline)) -> uint32_t {
         return __builtin_amdgcn_perm(r[1], r[0], 0x0c0c0400u) | __builtin_amdgcn_perm(r[3], r[2], 0x04000c0cu);
-    };
-    // The same by arithmetic: W = 512 e4m3 a, k the integer next to W / m, W - m k.  Of the sums with 1.5 2^23 the low bits are the integers next to the products; of the last only a byte
-    // is wanted, so that its 24-bit product may take them as they are.  Primes to 37: |a| <= 18, |W| < 2^22 stands in the sum as it is.  Else the low bits of 512 e4m3 times a.
-    // The quotient is off by at most 2^17 2^-24, the result at most by m / 2 + 1.5: below 128 with m <= 240.
-    float f8_k = 0, f8_w = 0;
-    uint32_t f8_a = 0;
-    auto set_scale = [&](int kb) __attribute__((always_inline)) {
-        if constexpr (kF8 && kDirect) {
-            f8_k = __uint_as_float(lane_of(__float_as_uint(f8_quotient), kb & 63));
-            f8_w = __uint_as_float(lane_of(__float_as_uint(f8_factor), kb & 63));
-            if constexpr (kClass) { f8_a = (uint32_t)((int)f8_w >> 9) & 0xffu; f8_w = 512.0f; }
-        }
-    };
-    float f8_one = 12582912.0f;
-    asm volatile("" : "+v"(f8_one));
-    auto compute4 = [&](uint32_t x) __attribute__((always_inline)) -> uint32_t {
-        typedef float v2f __attribute__((ext_vector_type(2)));
-        const v2f lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
-        const float v[4] = {lo[0], lo[1], hi[0], hi[1]};
-        uint32_t r[4];
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            const uint32_t k = __float_as_uint(fmaf(v[i], f8_k, f8_one));
-            uint32_t w = __float_as_uint(fmaf(v[i], f8_w, f8_one));
-            if constexpr (kClass) w = mul24(w & 0xffffffu, f8_a);
-            r[i] = mul24(k & 0xffffffu, 256u - f8_mod) + w;
-        }
-        return join4(r);
     };
     const uint32_t f8_base = (uint32_t)(uintptr_t)(lds_ptr)s_f8;
     constexpr int kUnroll = S == 3 ? 6 : S;         // stages of a round of the loop: slots and parities are known in each
@@ -500,7 +468,9 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         constexpr int kProducts = dn * FB, kReads = FB + 2 * dn, kSlots = kProducts > 4 ? kProducts : 4;
         Tile next = tile;
         Begun begun = {0, 0};
-        make_table(tile.pi); open_table(tile); make_f8(0); set_scale(0);        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
+        make_table(tile.pi); open_table(tile); make_f8(0);
+        if (kTabs == 2) make_f8(1);
+        // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
         more = TL::PERSIST && next_tile(next);
         if (more) begun = begin(next);
         wait_loads<(S - 2) * GP>();         // all weights and the labels of stage 0
@@ -565,22 +535,14 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                     // the next stage begins are made in the first half, in front of the barrier.
                     static_assert(FB == WT, "a wave expands what it multiplies");
                     if (m == 0) fetch_codes(u1, kHalf);
-                    if (m == 0 && !kHalf && (WK == 2 || (U & 1))) make_f8(WK == 2 ? t + 1 : (t + 1) >> 1);
-                    const uint32_t kb = WK == 2 ? (uint32_t)(t + kHalf) : (uint32_t)(t + kHalf) >> 1;      // of the half that is expanded
-                    // (in the first slots, the results taken some slots later; the last kComputed of four by arithmetic)
-                    if (m == 0) set_scale((int)kb);
+                    if (m == 0 && !kHalf && (WK > 1 || (U & 1))) make_f8((WK * (t + 1)) >> 1);
+                    if (m == 0 && !kHalf && kTabs == 2) make_f8(2 * t + 3);
+                    const uint32_t kb = (uint32_t)(WK * (t + kHalf) + ws) >> 1;            // of the half that is expanded
+                    // (in the first slots, the results taken some slots later)
 #pragma unroll
                     for (int i = 0; i < 4 * FB; i++) {
-                        if (i % 4 >= 4 - kComputed) {
-                            const int c = i / 4 * kComputed + i % 4 - (4 - kComputed);
-                            if (c * kSlots / (kComputed * FB) == m) {
-                                next.b[i / 4][i % 4] = (int)compute4(code[!kHalf][i / 4][i % 4]);
-                                if (kHalf) asm volatile("" : "+v"(next.b[i / 4][i % 4]));
-                            }
-                            continue;
-                        }
                         const int s = i * kSlots / (8 * FB);
-                        if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + (kb & 1) * 256);
+                        if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + (kb & (2 * kTabs - 1)) * 256);
                         if (s + kSlots / 2 == m) {
                             next.b[i / 4][i % 4] = (int)join4(look[i]);
                             if (kHalf) asm volatile("" : "+v"(next.b[i / 4][i % 4]));
@@ -624,7 +586,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
             t++;
             if constexpr (kF8) {
                 // stage t makes the table of scale number 64, 96, 128 ...: that one and 31 behind it in place of the 32 oldest (the one before it is still in use)
-                constexpr int kPer = WK == 2 ? 32 : 64, kAt = WK == 2 ? 31 : kDirect ? 63 : 62;
+                constexpr int kPer = 64 / WK, kAt = kPer - (kDirect ? 1 : 2);
                 if (__builtin_expect((t & (kPer - 1)) == kAt && t > kPer, 0)) { load_scales(32 * (t / kPer)); take_scales(); }
             }
             return t < (nk + WK - 1) / WK;
@@ -644,7 +606,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
 #pragma unroll
             for (int i = 0; i < 4 * FB; i++) {
                 uint32_t look[4];
-                look4(look, code[0][i / 4][i % 4], f8_base);
+                look4(look, code[0][i / 4][i % 4], f8_base + (ws >> 1) * 256);
                 o0.b[i / 4][i % 4] = (int)join4(look);
             }
         } else if constexpr (kDirect) {
@@ -757,7 +719,8 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     do {
         // waves whose digits lie past the tile's groups, in part or whole, leave out those products (large tiles are rarely short)
         const int mine = ((tile.n_groups + 1) >> 1) - wd * DA;
-        if (TL::PERSIST || mine > 2 || (DA == 2 && mine == 2)) work(integral_constant<int, DA>{});
+        if (DA > 4 && mine > 2 && mine <= 4) work(integral_constant<int, 4>{});
+        else if (TL::PERSIST || mine > 2 || (DA == 2 && mine == 2)) work(integral_constant<int, DA>{});
         else if (DA > 2 && mine == 2) work(integral_constant<int, 2>{});
         else work(k1);
     } while (more);

@@ -153,7 +153,7 @@ def test_prepare(E, M, K, pad):
 
 
 # ---- products ----
-@pytest.fixture(params=["rule", "big", "narrow", "few", "wide"])
+@pytest.fixture(params=["rule", "big", "narrow", "few", "wide", "class", "small"])
 def tile(request, monkeypatch):
     """the tile that the layer's sizes ask for, and each tile forced"""
     monkeypatch.setenv("DASH_EXPERTS_TILE", request.param)
