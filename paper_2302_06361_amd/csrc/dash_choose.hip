@@ -4,6 +4,7 @@
 //     of n_groups equal groups of experts the top_groups with the largest c (or the largest sum of two);  of their experts the top_k largest c;
 //     w = scale s (renormalise: / sum of the chosen s);  gate = w 2^gate_bits, to the nearest integer, ties to the even.
 // Everything that a comparison or a rounding decides on is held in 64 bits.
+#include <limits.h>
 #include <math.h>
 #include <string.h>
 
@@ -20,7 +21,7 @@ struct ChooseArgs {
     float* weights;
     int64_t row_stride, first, n;       // first: the launch's first row
     int E, top_k, n_groups, top_groups, dtype;
-    int sigmoid, pair, renormalise;
+    int pair, renormalise;
     double scale, two;                  // two: 2^gate_bits
 };
 constexpr int kRowLanes = 16;           // lanes of a row
@@ -39,6 +40,7 @@ template <class T> __device__ __forceinline__ T from_lane(T v, int step) {
     __builtin_memcpy(&v, w, sizeof(T));
     return v;
 }
+__device__ __forceinline__ int larger(int a, int b) { return a > b ? a : b; }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 __device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
@@ -59,17 +61,17 @@ __device__ __forceinline__ double row_sum(double v) {
     return v;
 }
 // e^a for a <= 0: a = n ln 2 + r, |r| <= ln 2 / 2, and the series of e^r up to r^13 / 13! (what follows is below 2^-57); off by 1.5 units in the last place at most.
-// What is below 2^-995.5 counts as zero: quotients of scores hold all their bits.
-// The coefficients stand in registers: as literals each costs two moves in front of its sum.
+// What is below e^-690 counts as zero: quotients of scores hold all their bits.
+// The coefficients stand in scalar registers: as literals each costs two moves in front of its sum, and in vector registers a wave less fits.
 struct Series {
     double c[13];
     __device__ __forceinline__ Series() : c{1.0 / 6227020800.0, 1.0 / 479001600, 1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 0.5, 1.0} {
 #pragma unroll
-        for (int i = 0; i < 11; i++) asm("" : "+v"(c[i]));
+        for (int i = 0; i < 11; i++) asm("" : "+s"(c[i]));
     }
 };
 __device__ __forceinline__ double exp_of(double a, const Series& S) {
-    a = a > -800.0 ? a : -800.0;
+    a = a < -690.0 ? -3000.0 : a;                           // (0 in the end)
     const double n = rint(a * 1.4426950408889634074);
     double r = fma(n, -0x1.62e42fefa39efp-1, a);            // ln 2 to 53 bits, and what is left of it
     r = fma(n, -0x1.abc9e3b39803fp-56, r);
@@ -77,7 +79,7 @@ __device__ __forceinline__ double exp_of(double a, const Series& S) {
 #pragma unroll
     for (int i = 1; i < 13; i++) s = fma(s, r, S.c[i]);
     s = fma(s, r, 1.0);
-    return ldexp(s, n < -995.0 ? -3000 : (int)n);
+    return ldexp(s, (int)n);
 }
 // 1 / v, 0 < v < 2^1000: an estimate of at least 20 bits and two steps of Newton's
 __device__ __forceinline__ double inverse_of(double v) {
@@ -94,8 +96,9 @@ __device__ __forceinline__ float half_logit(uint16_t v, int dtype) {
 // 16 lanes a row, V neighbouring experts a lane.  BIAS: choice values are sums in 64 bits, else the logits themselves.
 // A row's choice values stand in LDS, 16 lanes' runs of V, and every lane keeps the largest of its run.  A round: the largest of the 16 (four steps between lanes), the first run that
 // holds it; the 16 lanes look through that run together for the first place of it and for what is largest without it.  A row lies within a wave: no barriers.  (Each
-// lane through its own run again in registers: 65536 rows of 256 experts, eight chosen, 84.5 us.)
-template <int V, bool BIAS, bool GROUPS>
+// lane through its own run again in registers: 65536 rows of 256 experts, eight chosen, 84.5 us.)  The rounds compare 32-bit integers: the logits, or the sums rounded to float32, which keeps
+// their order but for sums that it makes equal; a wave that meets equal ones among its largest does its rounds again with the sums themselves (rounds in 64 bits for all: 44.1 us).
+template <int V, bool BIAS, bool GROUPS, bool SIGMOID>
 __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs A) {
     typedef typename std::conditional<BIAS, double, float>::type Key;
     constexpr int T = V == 64 ? 64 : 256, R = T / kRowLanes, P = V + (V > 1 ? 1 : 0);      // P: a run and a word, against bank conflicts
@@ -135,12 +138,14 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
     double common = 1;                          // of all softmax scores
     const Series series;
     auto score = [&](float x) __attribute__((always_inline)) -> double {
-        if (!A.sigmoid) return exp_of((double)x - top, series) * common;
+        if (!SIGMOID) return exp_of((double)x - top, series) * common;
         const double t = exp_of(-fabs((double)x), series);
         return (x >= 0 ? 1.0 : t) * inverse_of(1 + t);
     };
-    const bool sum_wanted = !A.sigmoid && (BIAS || A.pair || !A.renormalise);     // (renormalised and of no other use: any common factor)
-    Key best = kNone;
+    const bool sum_wanted = !SIGMOID && (BIAS || A.pair || !A.renormalise);     // (renormalised and of no other use: any common factor)
+    Key key[V];
+    // an expert that may be chosen (a bias that is no number makes its sum none)
+    auto able = [&](int v) __attribute__((always_inline)) { return l[v] > -INFINITY && (!BIAS || key[v] > kNone); };
     if constexpr (BIAS) {
         double s[V], sum = 0;
         float b[V];
@@ -156,10 +161,8 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
         }
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            const double c = fma(s[v], common, (double)b[v]);
-            const Key k = use && l[v] > -INFINITY && c == c ? c : kNone;
-            s_key[rr][lane * P + v] = k;
-            best = larger(best, k);
+            key[v] = fma(s[v], common, (double)b[v]);
+            if (GROUPS) key[v] = able(v) ? key[v] : kNone;
         }
     } else {
         if (sum_wanted) {
@@ -170,16 +173,15 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
             common = sum > 0 ? inverse_of(sum) : 0.0;
         }
 #pragma unroll
-        for (int v = 0; v < V; v++) s_key[rr][lane * P + v] = use ? l[v] : kNone;
-        best = use ? (Key)l[0] : kNone;
-#pragma unroll
-        for (int v = 1; v < V; v++) best = larger(best, use ? (Key)l[v] : kNone);
+        for (int v = 0; v < V; v++) key[v] = l[v];
     }
-    lds_order();
 
     if constexpr (GROUPS) {
         __shared__ double s_group[R][64];
         __shared__ uint8_t s_kept[R][64];
+#pragma unroll
+        for (int v = 0; v < V; v++) s_key[rr][lane * P + v] = key[v];
+        lds_order();
         const int n = A.E / A.n_groups;
         // a lane per group: its two largest
         for (int g = lane; g < A.n_groups; g += kRowLanes) {
@@ -209,44 +211,97 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
             s_kept[rr][g] = rank < A.top_groups;
         }
         lds_order();
-        best = kNone;
         int g = lane * V / n, in = lane * V - g * n;
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            Key k = kNone;
-            if (g < A.n_groups && s_kept[rr][g]) k = s_key[rr][lane * P + v];
-            else s_key[rr][lane * P + v] = kNone;
-            best = larger(best, k);
+            if (!(g < A.n_groups && s_kept[rr][g])) key[v] = kNone;
             if (++in == n) { in = 0; g++; }
         }
-        lds_order();
     }
 
     // lane j mod 16 keeps number j
     int mine[2] = {-1, -1};
-    for (int j = 0; j < A.top_k; j++) {
-        const Key most = row_max(best);
-        if (!(most > kNone)) break;             // (a row's lanes leave together)
-        const int run = row_min(best == most ? lane : kRowLanes);
-        Key rest = kNone, k[(V + kRowLanes - 1) / kRowLanes];
-        int first = V;
+    constexpr int kPer = (V + kRowLanes - 1) / kRowLanes;       // of a run, per lane
+    bool equal = false;
+    {
+        // integers in the order of the floats (without a second zero); none: the lowest
+        int* const to = (int*)s_key[rr];
+        int best = INT_MIN;
 #pragma unroll
-        for (int i = 0; i < (V + kRowLanes - 1) / kRowLanes; i++) {
-            const int at = i * kRowLanes + lane;
-            k[i] = at < V ? s_key[rr][run * P + at] : kNone;
-            if (k[i] == most && first == V) first = at;
+        for (int v = 0; v < V; v++) {
+            const float c = BIAS ? (float)key[v] : (float)key[v] + 0.0f;        // (a sum that rounds to -0 is below zero)
+            const int bits = __float_as_int(c), k = c > -INFINITY && (!BIAS || GROUPS || l[v] > -INFINITY) ? bits ^ ((bits >> 31) & 0x7fffffff) : INT_MIN;
+            to[lane * P + v] = k;
+            best = k > best ? k : best;
         }
-        first = row_min(first);
-#pragma unroll
-        for (int i = 0; i < (V + kRowLanes - 1) / kRowLanes; i++) {
-            const int at = i * kRowLanes + lane;
-            if (at == first) s_key[rr][run * P + at] = kNone;
-            else rest = larger(rest, k[i]);
-        }
-        rest = row_max(rest);
         lds_order();
-        if (lane == run) best = rest;
-        if (j % kRowLanes == lane) mine[j / kRowLanes] = run * V + first;
+        const int row_at = threadIdx.x & 48;                    // the row's lanes in the wave
+        auto row_bits = [&](bool x) __attribute__((always_inline)) { return (uint32_t)(__ballot(x) >> row_at) & 0xffffu; };
+        for (int j = 0; j < A.top_k; j++) {
+            const int most = row_max(best);
+            if (most == INT_MIN || !use) break;         // (a row's lanes leave together)
+            const uint32_t runs = row_bits(best == most);
+            const int run = __builtin_ctz(runs);
+            int k[kPer], rest = INT_MIN;
+            uint32_t there = 0;
+            int first = 0;
+#pragma unroll
+            for (int i = 0; i < kPer; i++) k[i] = i * kRowLanes + lane < V ? to[run * P + i * kRowLanes + lane] : INT_MIN;
+            bool several = (runs & (runs - 1)) != 0;
+#pragma unroll
+            for (int i = 0; i < kPer; i++) {
+                const uint32_t bits = row_bits(k[i] == most);
+                several |= (bits & (bits - 1)) != 0 || (bits && there);
+                if (bits && !there) first = i * kRowLanes + __builtin_ctz(bits);
+                there |= bits;
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; i++) {
+                if (i * kRowLanes + lane == first) to[run * P + first] = INT_MIN;
+                else rest = k[i] > rest ? k[i] : rest;
+            }
+            rest = row_max(rest);
+            lds_order();
+            if (lane == run) best = rest;
+            if (j % kRowLanes == lane) mine[j / kRowLanes] = run * V + first;
+            equal |= several;
+        }
+    }
+    if (BIAS && __any(equal)) {
+        lds_order();
+        mine[0] = mine[1] = -1;
+        Key best = kNone;
+#pragma unroll
+        for (int v = 0; v < V; v++) {
+            const Key k = GROUPS || able(v) ? key[v] : kNone;
+            s_key[rr][lane * P + v] = k;
+            best = larger(best, k);
+        }
+        lds_order();
+        for (int j = 0; j < A.top_k; j++) {
+            const Key most = row_max(best);
+            if (!(most > kNone) || !use) break;
+            const int run = row_min(best == most ? lane : kRowLanes);
+            Key rest = kNone, k[kPer];
+            int first = V;
+#pragma unroll
+            for (int i = 0; i < kPer; i++) {
+                const int at = i * kRowLanes + lane;
+                k[i] = at < V ? s_key[rr][run * P + at] : kNone;
+                if (k[i] == most && first == V) first = at;
+            }
+            first = row_min(first);
+#pragma unroll
+            for (int i = 0; i < kPer; i++) {
+                const int at = i * kRowLanes + lane;
+                if (at == first) s_key[rr][run * P + at] = kNone;
+                else rest = larger(rest, k[i]);
+            }
+            rest = row_max(rest);
+            lds_order();
+            if (lane == run) best = rest;
+            if (j % kRowLanes == lane) mine[j / kRowLanes] = run * V + first;
+        }
     }
     double s[2];
 #pragma unroll
@@ -297,7 +352,7 @@ int dash_choose(dash_ctx* c, const dash_router* r, const void* logits, int dtype
     memset(&A, 0, sizeof(A));
     A.logits = logits; A.bias = r->bias; A.valid = valid; A.experts = experts; A.gates = gates; A.weights = weights;
     A.row_stride = row_stride; A.n = n; A.E = E; A.top_k = r->top_k; A.n_groups = G; A.top_groups = r->top_groups; A.dtype = dtype;
-    A.sigmoid = r->score == DASH_SIGMOID; A.pair = r->group_score == DASH_GROUP_PAIR && r->top_groups < G; A.renormalise = r->renormalise != 0;
+    A.pair = r->group_score == DASH_GROUP_PAIR && r->top_groups < G; A.renormalise = r->renormalise != 0;
     A.scale = r->scale; A.two = ldexp(1.0, r->gate_bits);
     auto launch = [&](auto v) {
         constexpr int V = decltype(v)::value, T = V == 64 ? 64 : 256, R = T / kRowLanes;
@@ -307,10 +362,12 @@ int dash_choose(dash_ctx* c, const dash_router* r, const void* logits, int dtype
             A.first = first * R;
             const dim3 grid((uint32_t)(blocks - first < most ? blocks - first : most));
             const bool groups = r->top_groups < G;
-            if (r->bias && groups) hipLaunchKernelGGL((k_choose<V, true, true>), grid, dim3(T), 0, (hipStream_t)stream, A);
-            else if (r->bias) hipLaunchKernelGGL((k_choose<V, true, false>), grid, dim3(T), 0, (hipStream_t)stream, A);
-            else if (groups) hipLaunchKernelGGL((k_choose<V, false, true>), grid, dim3(T), 0, (hipStream_t)stream, A);
-            else hipLaunchKernelGGL((k_choose<V, false, false>), grid, dim3(T), 0, (hipStream_t)stream, A);
+            auto kernel = [&](auto sigmoid) {
+                constexpr bool S = decltype(sigmoid)::value;
+                return r->bias ? (groups ? k_choose<V, true, true, S> : k_choose<V, true, false, S>) : groups ? k_choose<V, false, true, S> : k_choose<V, false, false, S>;
+            };
+            const auto k = r->score == DASH_SIGMOID ? kernel(std::true_type{}) : kernel(std::false_type{});
+            hipLaunchKernelGGL(k, grid, dim3(T), 0, (hipStream_t)stream, A);
         }
     };
     using std::integral_constant;

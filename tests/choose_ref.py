@@ -3,9 +3,8 @@ import numpy as np
 
 
 def exp_of(a):
-    """e^a, a <= 0; what is below 2^-995.5 counts as zero (64 bits do not hold all its digits from 2^-1022 on, and 1 / (1 + e^-x) is zero from x = -709.8 on)"""
-    a = np.maximum(a, -800.0)
-    return np.where(np.rint(a * np.log2(np.e)) < -995, 0.0, np.exp(a))
+    """e^a, a <= 0; what is below e^-690 counts as zero (64 bits do not hold all digits of what is below 2^-1022, and 1 / (1 + e^-x) is zero from x = -709.8 on)"""
+    return np.where(a < -690.0, 0.0, np.exp(np.maximum(a, -690.0)))
 
 
 def choose(logits, top_k, sigmoid=False, bias=None, groups=1, top_groups=1, pair=False, renormalise=True, scale=1.0, gate_bits=8, valid=None):
