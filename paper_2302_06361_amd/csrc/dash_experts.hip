@@ -21,36 +21,71 @@ namespace dash {
 constexpr int kWaves = kThreads / 64;
 
 // ---- routing -----------------------------------------------------------------------------------
-// Three launches, once for all layers over the same rows; no atomics, so that the order is the same every time.
+// Three launches, once for all layers over the same rows; no atomics, so that the order is the same every time.  Bound by latency: 11 us for 1 to 16 rows (10 us for
+// three empty launches in a row), 17 us for 1000 rows of 64 experts, 52 for 10000; from there the waves that walk all rows, 500 us for 100000 rows of 8 or 4096 experts.
+// A lane counts the tiles of one (kind, part of the primes) instead of the wave one after the other, 8 of the rows' loads are under way instead of one (16, 23, 77, 880 to 970 us
+// with five kinds of tiles, 27, 36, 91, 970 to 1040 with eight).
+constexpr int kMaxPairs = 128;
+static_assert(2 + 6 * DASH_MAX_PRIMES <= kMaxPairs && kTileKinds <= 8, "pairs of a tile kind and a part of the primes");
 struct RouteArgs {
     const int32_t* experts;
     int64_t n;
-    int E;
-    int parts[3], chunk_first[3][DASH_MAX_PRIMES + 1];      // by TileParts: the parts, and the first chunk of each in the numbering of all
+    int E, pairs;
+    int kind_first[kTileKinds + 1];                 // first pair of every kind
+    struct { uint8_t kind, part; uint16_t first, last; } pair[kMaxPairs];        // a kind's tiles of the chunks first .. last - 1
     RoutingView to;
 };
 __device__ __forceinline__ bool route_match(int32_t id, int e, int E) { return e < E ? id == e : (uint32_t)id >= (uint32_t)E; }
+// Which of the rows r0 + 64 i + lane are of expert e: the loads of a step are under way together, as nothing else hides their latency
+constexpr int kRouteRows = 8;
+__device__ __forceinline__ void route_hits(const RouteArgs& A, int64_t r0, int e, int lane, bool (&hit)[kRouteRows]) {
+    int32_t id[kRouteRows];
+#pragma unroll
+    for (int i = 0; i < kRouteRows; i++) id[i] = A.experts[r0 + 64 * i + lane < A.n ? r0 + 64 * i + lane : 0];
+#pragma unroll
+    for (int i = 0; i < kRouteRows; i++) hit[i] = r0 + 64 * i + lane < A.n && route_match(id[i], e, A.E);
+}
+__device__ __forceinline__ int32_t wave_scan(int32_t v, int lane) {
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) { const int32_t o = __shfl_up(v, d); v += lane >= d ? o : 0; }
+    return v;
+}
+// Tiles that an expert of `rows` rows has before every pair: to[0 .. pairs] (a wave's own; a lane per pair)
+__device__ __forceinline__ void route_pairs(const RouteArgs& A, int32_t rows, int lane, int32_t* to) {
+    int32_t before = 0;
+    for (int q0 = 0; q0 < A.pairs; q0 += 64) {
+        const int q = q0 + lane;
+        int32_t t = 0;
+        if (q < A.pairs) {
+            const auto P = A.pair[q];
+            const int groups = kTileKind[P.kind].groups;
+            t = (int32_t)(((int64_t)rows * (P.last - P.first) + groups - 1) / groups);
+        }
+        const int32_t up_to = before + wave_scan(t, lane);
+        if (q < A.pairs) to[q] = up_to - t;
+        before = __shfl(up_to, 63);
+    }
+    if (lane == 0) to[A.pairs] = before;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 
-// A wave per expert (E + 1 of them: the last is "none") counts its rows.
+// A wave per expert (E + 1 of them: the last is "none") counts its rows and its tiles of every kind.
 __global__ __launch_bounds__(kThreads) void k_route_count(const RouteArgs A) {
+    __shared__ int32_t s_pairs[kWaves][kMaxPairs + 1];
     const int e = (int)(blockIdx.x * kWaves + threadIdx.x / 64), lane = threadIdx.x & 63;
     if (e > A.E) return;
     int32_t count = 0;
-    for (int64_t r0 = 0; r0 < A.n; r0 += 64) {
-        const bool hit = r0 + lane < A.n && route_match(A.experts[r0 + lane], e, A.E);
-        count += __popcll(__ballot(hit));
+    for (int64_t r0 = 0; r0 < A.n; r0 += 64 * kRouteRows) {
+        bool hit[kRouteRows];
+        route_hits(A, r0, e, lane, hit);
+#pragma unroll
+        for (int i = 0; i < kRouteRows; i++) count += __popcll(__ballot(hit[i]));
     }
+    int32_t* const first = s_pairs[threadIdx.x / 64];
+    route_pairs(A, count, lane, first);
     if (lane == 0) A.to.offsets[e + 1] = count;
-}
-// tiles of kind s that `rows` rows make of the chunks first .. last - 1
-__device__ __forceinline__ int32_t route_tiles(int32_t rows, int first, int last, int s) {
-    return (int32_t)(((int64_t)rows * (last - first) + kTileKind[s].groups - 1) / kTileKind[s].groups);
-}
-__device__ __forceinline__ int32_t route_tiles(const RouteArgs& A, int32_t rows, int s) {
-    const int parts = kTileKind[s].parts;
-    int32_t t = 0;
-    for (int i = 0; i < A.parts[parts]; i++) t += route_tiles(rows, A.chunk_first[parts][i], A.chunk_first[parts][i + 1], s);
-    return t;
+    if (lane < kTileKinds) A.to.first_tile[lane][e + 1] = first[A.kind_first[lane + 1]] - first[A.kind_first[lane]];
 }
 // One block: counts to offsets and to first tiles.
 __global__ __launch_bounds__(kThreads) void k_route_scan(const RouteArgs A) {
@@ -58,15 +93,18 @@ __global__ __launch_bounds__(kThreads) void k_route_scan(const RouteArgs A) {
     const int n = A.E + 1, per = (n + kThreads - 1) / kThreads, e0 = threadIdx.x * per, e1 = e0 + per < n ? e0 + per : n;
     int32_t sum[1 + kTileKinds] = {};
     for (int e = e0; e < e1; e++) {
-        const int32_t rows = A.to.offsets[e + 1];
-        sum[0] += rows;
-        for (int s = 0; s < kTileKinds; s++) sum[1 + s] += route_tiles(A, rows, s);
+        sum[0] += A.to.offsets[e + 1];
+        for (int s = 0; s < kTileKinds; s++) sum[1 + s] += A.to.first_tile[s][e + 1];
     }
     for (int s = 0; s < 1 + kTileKinds; s++) part[s][threadIdx.x] = sum[s];
     __syncthreads();
-    if (threadIdx.x < 1 + kTileKinds) {
-        int32_t at = 0;
-        for (int i = 0; i < kThreads; i++) { const int32_t v = part[threadIdx.x][i]; part[threadIdx.x][i] = at; at += v; }
+    // a wave per sum, four threads' parts a lane
+    const int lane = threadIdx.x & 63;
+    for (int s = threadIdx.x / 64; s < 1 + kTileKinds; s += kWaves) {
+        int32_t v[kWaves], all = 0;
+        for (int i = 0; i < kWaves; i++) { v[i] = part[s][lane * kWaves + i]; all += v[i]; }
+        int32_t at = wave_scan(all, lane) - all;
+        for (int i = 0; i < kWaves; i++) { part[s][lane * kWaves + i] = at; at += v[i]; }
     }
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -75,34 +113,56 @@ __global__ __launch_bounds__(kThreads) void k_route_scan(const RouteArgs A) {
     }
     for (int s = 0; s < 1 + kTileKinds; s++) sum[s] = part[s][threadIdx.x];
     for (int e = e0; e < e1; e++) {
-        const int32_t rows = A.to.offsets[e + 1];
-        sum[0] += rows;
+        sum[0] += A.to.offsets[e + 1];
         A.to.offsets[e + 1] = sum[0];
-        for (int s = 0; s < kTileKinds; s++) { sum[1 + s] += route_tiles(A, rows, s); A.to.first_tile[s][e + 1] = sum[1 + s]; }
+        for (int s = 0; s < kTileKinds; s++) { sum[1 + s] += A.to.first_tile[s][e + 1]; A.to.first_tile[s][e + 1] = sum[1 + s]; }
     }
 }
-// The wave of an expert writes its rows in ascending order, and its tiles.
+// The wave of an expert writes its rows in ascending order, and its tiles, a lane each.
 __global__ __launch_bounds__(kThreads) void k_route_fill(const RouteArgs A) {
+    __shared__ int32_t s_pairs[kWaves][kMaxPairs + 1];
     const int e = (int)(blockIdx.x * kWaves + threadIdx.x / 64), lane = threadIdx.x & 63;
     if (e > A.E) return;
     const int32_t start = A.to.offsets[e], count = A.to.offsets[e + 1] - start;
     int32_t at = start;
-    for (int64_t r0 = 0; r0 < A.n; r0 += 64) {
-        const bool hit = r0 + lane < A.n && route_match(A.experts[r0 + lane], e, A.E);
-        const uint64_t m = __ballot(hit);
-        if (hit) A.to.rows[at + __popcll(m & ((1ull << lane) - 1))] = (int32_t)(r0 + lane);
-        at += __popcll(m);
-    }
-    for (int s = 0; s < kTileKinds; s++) {
-        int32_t t0 = A.to.first_tile[s][e];
-        const int parts = kTileKind[s].parts;
-        for (int i = 0; i < A.parts[parts]; i++) {
-            const int c0 = A.chunk_first[parts][i], c1 = A.chunk_first[parts][i + 1];
-            const int32_t tiles = route_tiles(count, c0, c1, s);
-            for (int32_t t = lane; t < tiles; t += 64)
-                A.to.tiles[s][t0 + t] = RouteTile{(uint32_t)e | (uint32_t)i << 24, start, count, c0 * count + t * kTileKind[s].groups};
-            t0 += tiles;
+    for (int64_t r0 = 0; r0 < A.n; r0 += 64 * kRouteRows) {
+        bool hit[kRouteRows];
+        route_hits(A, r0, e, lane, hit);
+#pragma unroll
+        for (int i = 0; i < kRouteRows; i++) {
+            const uint64_t m = __ballot(hit[i]);
+            if (hit[i]) A.to.rows[at + __popcll(m & ((1ull << lane) - 1))] = (int32_t)(r0 + 64 * i + lane);
+            at += __popcll(m);
         }
+    }
+    int32_t* const first = s_pairs[threadIdx.x / 64];
+    route_pairs(A, count, lane, first);
+    if (first[A.pairs] > 16 * A.pairs) {            // many tiles: pair after pair (0.3 us each) instead of a search (1 us for 64 tiles)
+        for (int q = 0; q < A.pairs; q++) {
+            const auto P = A.pair[q];
+            const int s = P.kind, groups = kTileKind[s].groups;
+            RouteTile* const to = A.to.tiles[s] + A.to.first_tile[s][e] + first[q] - first[A.kind_first[s]];
+            for (int32_t t = lane; t < first[q + 1] - first[q]; t += 64)
+                to[t] = RouteTile{(uint32_t)e | (uint32_t)P.part << 24, start, count, P.first * count + t * groups};
+        }
+        return;
+    }
+    struct Pair { RouteTile* to; int32_t block; uint16_t part, groups; };           // where tile i of the expert goes, less i
+    __shared__ Pair s_to[kWaves][kMaxPairs];
+    Pair* const to = s_to[threadIdx.x / 64];
+    for (int q = lane; q < A.pairs; q += 64) {
+        const auto P = A.pair[q];
+        const int s = P.kind;
+        to[q] = Pair{A.to.tiles[s] + A.to.first_tile[s][e] - first[A.kind_first[s]], P.first * count, P.part, (uint16_t)kTileKind[s].groups};
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    for (int32_t i = lane; i < first[A.pairs]; i += 64) {
+        int q = 0;                                  // the last pair that begins at i or before (of those of no tiles, the one behind them)
+#pragma unroll
+        for (int d = kMaxPairs / 2; d; d /= 2) if (q + d < A.pairs && first[q + d] <= i) q += d;
+        const Pair P = to[q];
+        P.to[i] = RouteTile{(uint32_t)e | (uint32_t)P.part << 24, start, count, P.block + (i - first[q]) * P.groups};
     }
 }
 
@@ -446,8 +506,8 @@ static int check_bundle(const dash_ctx* c, const dash_labels* t, int64_t n) {
 constexpr int64_t kMaxLanes = 0x7fffffffll * kThreads;
 // launch(first, n) for blocks first .. first + n - 1: a direction of a grid holds fewer than 2^32 threads.  (A second direction instead, with the
 // grid's size read by the kernel: 84 values, 16 batch elements: 4.3 -> 4.5 us a call; quantisation of 4096 x 4096: 13.65 -> 13.9.)
-template <class Launch> static void in_launches(int64_t blocks, Launch launch) {
-    constexpr int64_t most = 0xffffffffll / kThreads;
+template <int Threads = kThreads, class Launch> static void in_launches(int64_t blocks, Launch launch) {
+    constexpr int64_t most = 0xffffffffll / Threads;
     for (int64_t first = 0; first < blocks; first += most) launch(first, (uint32_t)(blocks - first < most ? blocks - first : most));
 }
 
@@ -573,7 +633,7 @@ int dash_f8_quantise(dash_ctx* c, const void* w, int dtype, int64_t row_stride, 
     if (blocks > 0x7fffffff) return DASH_ESIZE;
     QuantF8Args A{w, row_stride, expert_stride, matrix_bytes(DASH_F8, out_c, K), 0, out_c, K, max_scale, ldexpf(1.0f, base), ldexpf(1.0f, -base), (uint8_t*)prepared, values};
     auto kernel = dtype == DASH_F32 ? k_f8_quantise<QuantF32> : dtype == DASH_BF16 ? k_f8_quantise<QuantBF16> : k_f8_quantise<QuantF16>;
-    in_launches(blocks, [&](int64_t first, uint32_t n) {
+    in_launches<kF8Threads>(blocks, [&](int64_t first, uint32_t n) {
         A.first = (uint32_t)first;
         hipLaunchKernelGGL(kernel, dim3(n), dim3(kF8Threads), 0, (hipStream_t)stream, A);
     });
@@ -614,10 +674,16 @@ int dash_route(dash_ctx* c, const int32_t* experts, int64_t n, int n_experts, vo
     memset(&A, 0, sizeof(A));
     A.experts = experts; A.n = n; A.E = n_experts;
     const PrimeClasses classes = prime_classes(c);
-    A.parts[PARTS_NONE] = 1; A.parts[PARTS_PRIMES] = c->k; A.parts[PARTS_CLASSES] = classes.n;
-    for (int i = 0; i < c->k; i++) A.chunk_first[PARTS_PRIMES][i + 1] = A.chunk_first[PARTS_PRIMES][i] + (int)c->mods[c->prime[i]].nchunk;
-    A.chunk_first[PARTS_NONE][1] = A.chunk_first[PARTS_PRIMES][c->k];
-    for (int i = 0; i < classes.n; i++) A.chunk_first[PARTS_CLASSES][i + 1] = classes.chunk_first[i + 1];
+    for (int s = 0; s < kTileKinds; s++) {
+        const TileParts parts = kTileKind[s].parts;
+        int chunk = 0;
+        for (int i = 0; i < (parts == PARTS_NONE ? 1 : parts == PARTS_PRIMES ? c->k : classes.n); i++) {
+            const int first = chunk;
+            chunk = parts == PARTS_NONE ? (int)total_chunks(c) : parts == PARTS_PRIMES ? chunk + (int)c->mods[c->prime[i]].nchunk : classes.chunk_first[i + 1];
+            A.pair[A.pairs++] = {(uint8_t)s, (uint8_t)i, (uint16_t)first, (uint16_t)chunk};
+        }
+        A.kind_first[s + 1] = A.pairs;
+    }
     A.to = routing_view(c, data, n, n_experts);
     const dim3 grid((uint32_t)((n_experts + 1 + kWaves - 1) / kWaves));
     hipLaunchKernelGGL(k_route_count, grid, dim3(kThreads), 0, (hipStream_t)stream, A);
