@@ -174,7 +174,7 @@ int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void
 /* Layers whose matrix depends on the row (EXPERTS).  Which expert serves a row is public: a garbled circuit is fixed before its
  * inputs are known, so rows are routed by what is known then (the client, the task, a position), never by a label.
  *
- * Sums are held in 31 bits: in_c times 256 (p - 1) for DASH_W8, (p - 1)^2 for DASH_MX4 and DASH_F8, has to stay below 2^31 for the largest prime p,
+ * Sums are held in 31 bits: in_c times 256 (p - 1) for DASH_W8 and DASH_F8, (p - 1)^2 for DASH_MX4, has to stay below 2^31 for the largest prime p,
  * else DASH_ESIZE.
  *
  * Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] one after the other, 16-byte aligned, independent of the
@@ -184,7 +184,7 @@ int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void
  *             the magnitude 0, 1/2, 1, 3/2, 2, 3, 4, 6; the weight that enters the layer is the integer 2 * e2m1 * 2^shift.
  *   DASH_F8   tiles as DASH_W8's with codes in place of the weights; behind a matrix's tiles the scales, int32 [ceil(out_c / 128)][ceil(K / 128)],
  *             padded to a multiple of 16 bytes.  A code is an e4m3 float: bit 7 the sign, bits 3..6 the exponent e, bits 0..2 the mantissa m,
- *             (1 + m/8) 2^(e - 7), or m 2^-9 where e = 0; 0x7f and 0xff, not a number, count as 0.  The weight that enters the layer is the
+ *             (1 + m/8) 2^(e - 7), or m 2^-9 where e = 0; 0x7f and 0xff, not a number, are stored as 0.  The weight that enters the layer is the
  *             integer 512 * e4m3 * scale. */
 size_t dash_expert_weights_bytes(int format, int n_experts, int out_c, int K);
 /* DASH_W8.  w: device int8, element (e, j, i) at w[e * expert_stride + j * row_stride + i] (row_stride >= K, expert_stride
@@ -208,7 +208,7 @@ int dash_mx4_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_strid
 int dash_f8_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_stride, int64_t expert_stride, int n_experts, int out_c,
                      int K, int base, int max_scale, void *prepared, void *values, void *hip_stream);
 /* DASH_F8 from codes and scales that exist already.  codes: device, e4m3 bytes, strides as above; scales: device int32, contiguous
- * [n_experts][ceil(out_c / 128)][ceil(K / 128)], any values. */
+ * [n_experts][ceil(out_c / 128)][ceil(K / 128)], any values.  Codes that are not a number count as 0. */
 int dash_f8_prepare(dash_ctx *ctx, const uint8_t *codes, int64_t row_stride, int64_t expert_stride, const int32_t *scales, int n_experts,
                     int out_c, int K, void *prepared, void *hip_stream);
 /* Experts and gates from a router's logits, public values as everything that a circuit is routed by. */
@@ -232,7 +232,7 @@ typedef struct {
  * scale * s (renormalise: / sum of the chosen s, zero if that is zero), gates = w * 2^gate_bits to the nearest integer, ties to the even.  Scores, sums, choice
  * values and weights are held in 64 bits.
  * A logit that is not a number counts as -infinity, infinity as the largest float32.  Experts whose logit is -infinity, or whose choice value is -infinity or no number, are
- * never chosen; groups without any other are not either.  valid: device, a byte for every row, 0: no expert is chosen (NULL: all rows are valid).  What is missing of
+ * never chosen; groups without any other are not either.  A score below e^-690 (softmax: of the row's largest) is zero.  valid: device, a byte for every row, 0: no expert is chosen (NULL: all rows are valid).  What is missing of
  * top_k: expert -1, weight and gate 0.
  * experts, gates, weights: device [n][top_k]; gates and weights may be NULL.  experts is what dash_route takes (rows n * top_k), gates what COMBINE does.
  * DASH_ESIZE: more than DASH_MAX_ROUTED experts, DASH_MAX_TOP_K of them chosen or 64 groups. */

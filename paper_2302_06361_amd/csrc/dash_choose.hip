@@ -98,6 +98,9 @@ __device__ __forceinline__ float half_logit(uint16_t v, int dtype) {
 // holds it; the 16 lanes look through that run together for the first place of it and for what is largest without it.  A row lies within a wave: no barriers.  (Each
 // lane through its own run again in registers: 65536 rows of 256 experts, eight chosen, 84.5 us.)  The rounds compare 32-bit integers: the logits, or the sums rounded to float32, which keeps
 // their order but for sums that it makes equal; a wave that meets equal ones among its largest does its rounds again with the sums themselves (rounds in 64 bits for all: 44.1 us).
+// Bound by vector instructions, a third of them the exponentials (13 steps in 64 bits an expert; a float32 sum would move a choice or a gate): 65536 rows of 256 experts,
+// eight chosen, 40.5 us, 64 % of the cycles, 39.8 MB read and written in 8.2 us at a copy's rate.  4096 rows of 256 in eight groups, four of them: 9.4 to 11 us; 1000 rows of 160: 7.8;
+// one row of 8: 4.7 to 5.2, a launch and one row's chain of steps.
 template <int V, bool BIAS, bool GROUPS, bool SIGMOID>
 __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs A) {
     typedef typename std::conditional<BIAS, double, float>::type Key;

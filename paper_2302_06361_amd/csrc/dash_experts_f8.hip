@@ -3,13 +3,13 @@
 
 namespace dash {
 
-// A stage's codes take as much LDS as byte weights: three stages.
-typedef ETile<1, 4, 2, 4, 2, 3, 6, false> EBig8;         // 512 digits x 128 features, weights expanded once a block, through LDS
-typedef ETile<1, 1, 4, 8, 1, 3, 2, false> EWide8;        // 256 x 128, expanded in registers as in the others
-typedef ETile<1, 1, 4, 8, 1, 3, 7, false> EWideClass8;   // the same, tiles across a class of primes
-typedef ETile<1, 1, 4, 4, 1, 3, 5, false> ENarrow8;      // 128 x 128, classes
-typedef ETile<2, 1, 4, 4, 1, 3, 5, false> EFew8;         // 128 x 128 by two sets of waves, classes
-typedef ETile<2, 1, 2, 4, 1, 3, 5, false> ESmall8;       // 128 x 64 by two sets of waves, classes
+// Three stages: four and six change nothing for a lone block, whose stages wait for LDS, not for memory.  Each tile's home (us, and the best of the other tiles):
+typedef ETile<1, 4, 2, 4, 2, 3, 6, false> EBig8;         // 512 digits x 128 features, weights expanded once a block, through LDS (128 rows, 4096 -> 4096, 12 primes: 1 127; 1 215)
+typedef ETile<1, 1, 4, 8, 1, 3, 2, false> EWide8;        // 256 x 128, expanded in registers as in the others (256 rows, 32 experts, 1024 -> 2048: 423; 453)
+typedef ETile<1, 1, 4, 8, 1, 3, 7, false> EWideClass8;   // the same, tiles across a class of primes (256 rows, 2048 -> 64: 70.3; 72.0)
+typedef ETile<1, 1, 4, 4, 1, 3, 5, false> ENarrow8;      // 128 x 128, classes (64 rows, 64 experts, 1024 -> 1024: 93.9; 102.9)
+typedef ETile<2, 1, 4, 4, 1, 3, 5, false> EFew8;         // 128 x 128 by two sets of waves, classes (1 row, 4096 -> 4096: 34.8; 37.2)
+typedef ETile<2, 1, 2, 4, 1, 3, 5, false> ESmall8;       // 128 x 64 by two sets of waves, classes (12 rows, 6 experts, 3833 -> 172, 9 primes: 27.2; 32.7)
 
 int experts_mfma_f8(dash_ctx* c, const ExpertsCall& L, const dash_labels* in, dash_labels* out, hipStream_t s) {
     auto launch = [&](auto tl) -> int {

@@ -28,6 +28,18 @@
 // blocks a CU (256 x 256, one block: 412): vector instructions of the expansion in 65 % of the cycles, the matrix pipe in 39 %.  One row,
 // 4096 -> 4096, 4-bit: 26; latency of the stages, about 110 instructions by two to four waves a SIMD.  One row, 784 -> 128, 4-bit: 7.1 to 7.4,
 // 4.8 of them for a single stage: launch, the chain of loads to the first labels, results.
+//
+// 8-bit floats.  512 e4m3 S mod m by a table of 256 bytes in LDS, one for every scale (128 inputs) that a block passes: a byte read a weight (64 lanes in 4.3
+// clocks, bank conflicts among them; 2.8 with the signs apart in 128 entries, whose instructions cost more than that saves), joined by three v_perm for four.  An operand
+// holds 32 features, so what a table read serves is the tile's digits: 512 of them where the weights are expanded once a block, 256 or 128 where a wave's
+// weights are its own.  m is a prime of the tile, or the product (up to 240: signed bytes) of a class of primes whose digits then share a tile and its reads: 2, 3, 5,
+// ... 37 are 6 classes, one row of them 7 tiles of 128 digits instead of 12.  The sums take either sign and start at a multiple of p, as with bytes.
+//   Where many blocks wait, residues of single primes are better, as bytes up to 37 leave more of the power to the clock (128 rows, 4096 -> 4096, largest tile:
+// 1 137 us, classes 1 271).
+//   What bounds it.  128 rows, 4096 -> 4096, 12 primes: 1 127, of the cycles the LDS busy in 49 %, the matrix pipe in 49, vector instructions in 30, at 1.7 to 2.2 GHz.  With
+// 128 x 128 tiles the table reads: LDS 84 %, 1 638.  32 experts, 256 rows, 1024 -> 2048: 455 (256 x 128).  One row, 4096 -> 4096: 34.0, a stage of a lone block 0.45
+// us, of it 0.185 without the expansion: reads wait for codes and products for reads.  One row, 784 -> 128: 10.6.
+//   The compiler must not see accesses that could be LDS or scalar loads near the loop: from then on it waits for all LDS results at once (narrow tiles 1 702 -> 1 638).
 #pragma once
 #include <string.h>
 
@@ -130,6 +142,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr bool kHalfTile = TL::HALF;
     constexpr bool kClass = kTileKind[TL::KIND].parts == PARTS_CLASSES;
     static_assert(!kHalfTile || (kF8 && !kDirect), "loader roles");
+    static_assert(!kF8 || WK <= 2, "a round of the sets' stages is of one block of 128 inputs or half of one");
     static_assert(!kF8 || kDirect || kHalfTile, "steps of the expansion");
     const int M = A.M, K = A.K, nk = (K + 63) / 64;
     const int tid = threadIdx.x, lane = tid & 63, wave_ = __builtin_amdgcn_readfirstlane(tid >> 6), ws = wave_ / NW, wave = wave_ % NW;
@@ -175,8 +188,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     uint8_t* const s_exp = s_raw + S * FT * kRaw;
     __shared__ u32x4 s_lut[kMx4 ? 256 : 1];
     static_assert(!kF8 || kScaleBlock % TL::F == 0, "a block's features have one row of scales");
-    constexpr int kTabs = WK == 4 ? 2 : 1;                          // blocks of 128 inputs that a round of the sets' stages begins
-    __shared__ __attribute__((aligned(256))) uint8_t s_f8[kF8 ? 2 * kTabs * 256 : 16];     // their tables, of this round and the next
+    __shared__ __attribute__((aligned(256))) uint8_t s_f8[kF8 ? 512 : 16];      // tables of two blocks of 128 inputs
 
     // the primes, for lanes that each want another
     struct PrimeLds { uint64_t in, in_cs, out, out_cs, one; uint32_t p, mmagic, pow12, start, chunk_first, pad; };
@@ -294,7 +306,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     const int32_t* f8_scales = nullptr;
     const int f8_blocks = (K + kScaleBlock - 1) / kScaleBlock;
     int32_t f8_loaded = 0;
-    // 64 scales of the tile's row of them, from number `first` (past the end: the last), number i in lane i % 64; a load in flight
+    // A window of the scales: 64 of the tile's row of them, from number `first` (past the end: the last), number i in lane i % 64; a load in flight
     auto load_scales = [&](int first) __attribute__((always_inline)) {
         if constexpr (kF8) {
             const int i = first + ((lane - first) & 63);
@@ -330,7 +342,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         if constexpr (kF8) {
             // (without a branch for the waves past the fourth, which write the same again: a branch amid the products makes the reads around it be waited for)
             const uint32_t v = mul24(f8_residue, lane_of(f8_scale, kb & 63)), r = v - mul24(mulhi(v, f8_magic), f8_mod);
-            s_f8[(kb & (2 * kTabs - 1)) * 256 + (tid & 255)] = (uint8_t)(kClass && 2 * r > f8_mod ? r - f8_mod : r);
+            s_f8[(kb & 1) * 256 + (tid & 255)] = (uint8_t)(kClass && 2 * r > f8_mod ? r - f8_mod : r);
         }
     };
     // four codes' bytes; base: the table's address in LDS (a multiple of 256, below 2^24)
@@ -442,7 +454,7 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
     constexpr integral_constant<int, 0> k0{};
     constexpr integral_constant<int, 1> k1{};
     // loads that may be in flight at the barrier of stage t: those behind the labels of stage t + 1, 4-bit: behind the weights of stage t + 2
-    static_assert(S == 4 || (kF8 && (S == 3 || S == 6)), "the loop's slots; parities of stages follow from slots; the waits of the first stages");
+    static_assert(S == 4 || (kF8 && S == 3), "the loop's slots; parities of stages follow from slots; the waits of the first stages");
     constexpr int kInFlight = kPart ? (S - 3) * kParts + GP : (S - 2) * kParts;
     // the first stages: all weights, then labels (these wait for the rows' numbers), but for the labels of stage S - 1
     auto fill_weights = [&](auto self, auto u) __attribute__((always_inline)) -> void {
@@ -469,7 +481,6 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
         Tile next = tile;
         Begun begun = {0, 0};
         make_table(tile.pi); open_table(tile); make_f8(0);
-        if (kTabs == 2) make_f8(1);
         // (behind the barrier at the end of the last tile's products, before the one in front of this one's)
         more = TL::PERSIST && next_tile(next);
         if (more) begun = begin(next);
@@ -536,13 +547,12 @@ __global__ __launch_bounds__(TL::T, 2) void k_experts_mfma(const ExpArgs A) {
                     static_assert(FB == WT, "a wave expands what it multiplies");
                     if (m == 0) fetch_codes(u1, kHalf);
                     if (m == 0 && !kHalf && (WK > 1 || (U & 1))) make_f8((WK * (t + 1)) >> 1);
-                    if (m == 0 && !kHalf && kTabs == 2) make_f8(2 * t + 3);
                     const uint32_t kb = (uint32_t)(WK * (t + kHalf) + ws) >> 1;            // of the half that is expanded
                     // (in the first slots, the results taken some slots later)
 #pragma unroll
                     for (int i = 0; i < 4 * FB; i++) {
                         const int s = i * kSlots / (8 * FB);
-                        if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + (kb & (2 * kTabs - 1)) * 256);
+                        if (s == m) look4(look[i], code[!kHalf][i / 4][i % 4], f8_base + (kb & 1) * 256);
                         if (s + kSlots / 2 == m) {
                             next.b[i / 4][i % 4] = (int)join4(look[i]);
                             if (kHalf) asm volatile("" : "+v"(next.b[i / 4][i % 4]));

@@ -121,7 +121,7 @@ inline ExpertsRate8 experts_rate8(ExpertsTile tile) {
 //   256 rows, 2048 -> 64, 12 primes: 78.7, 72, 70.3, 73.5, 99.4, 72.9
 //   200 rows, 8 experts, 100 -> 1500, 9 primes: 90.5, 75.8, 73.5, 80.6, 220, 223
 // Over the 120 the choice took over 5 % more than the fastest tile in 5, over 10 % in 2, at most 20 % (141 rows, 2 experts, 3578 -> 162, 7 primes: 102.6 us with the narrow
-// tile, 85.3 with the one across classes), 0.7 % in the mean.
+// tile, 85.3 with the one across classes), 0.7 % in the mean; over 40 drawn layers that were not fitted 0.7 % in the mean, 8 % at most.
 inline double experts_us8(const ExpertsShape8& S, ExpertsTile tile) {
     const ExpertsRate8 R = experts_rate8(tile);
     const double busy = S.rows < S.experts ? (double)S.rows : (double)S.experts, rows = (double)S.rows / busy;

@@ -39,6 +39,8 @@ def test_more_blocks_than_a_launch_numbers(lib):
     big = 2 ** 31 - 1
     assert quantise(lib, E=big, M=200, K=200, row_stride=200) == ESIZE
     assert prepare(lib, E=1, M=big, K=big, row_stride=big) == ESIZE
+    for E in (2 ** 13, 2 ** 14, 2 ** 15, big):                # (products past 63 bits)
+        assert quantise(lib, E=E, M=big, K=big, row_stride=big) == prepare(lib, E=E, M=big, K=big, row_stride=big) == ESIZE
 
 
 def test_bytes(lib):
