@@ -55,7 +55,7 @@ def build_layers(ctx, net, b, batch_base):
             if routing is not None:
                 lay.routing = ctx.route(routing.part(batch_base, b), w.n_experts)
                 lay.c.routing = lay.routing.address()
-                lay.rebase = lambda base, lay=lay, r=routing, e=w.n_experts: ctx.route(r.part(base, b), e, out=lay.routing)
+                lay.rebase = lambda base, to=lay.routing, r=routing, e=w.n_experts: ctx.route(r.part(base, b), e, out=to)      # (not the layer: its memory would wait for a collection of cycles)
         elif kind == "combine":
             gates = _Routed(L["router"], L["rows"] * L["top_k"], ctx, b, "gates") if L.get("router") is not None else _PerBatch(L["gates"], L["rows"] * L["top_k"], ctx, "gates")
             part = gates.part(batch_base, b).clone()

@@ -119,3 +119,22 @@ def test_in_a_graph():
             y = ref.experts(x[j].reshape(T, K, lam), ints, experts.reshape(-1).tolist(), k, p)
             want = ref.combine(y.reshape(T, k, M, lam), gates, p)
             assert (dst.to_numpy(j) == want.reshape(T * M, lam)).all(), (i, p)
+
+
+@pytest.mark.parametrize("net", [dict(), dict(router=dict()), dict(k=12, f8=True, router=dict())])
+def test_memory_goes_back_with_the_network(net):
+    """at once, not with the next collection of cycles"""
+    import gc
+    from paper_2302_06361_amd import Context, GarbledNetwork
+    net = workloads.mixture(**net)
+    ctx = Context(net["primes"], net["seed"], net["digits"])
+    gc.collect()
+    gc.disable()
+    try:
+        before = torch.cuda.memory_allocated()
+        gn = GarbledNetwork(ctx, net)
+        assert torch.cuda.memory_allocated() > before
+        del gn
+        assert torch.cuda.memory_allocated() == before
+    finally:
+        gc.enable()
