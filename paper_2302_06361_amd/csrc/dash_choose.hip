@@ -20,44 +20,49 @@ struct ChooseArgs {
     int32_t* gates;
     float* weights;
     int64_t row_stride, first, n;       // first: the launch's first row
-    int E, top_k, n_groups, top_groups, dtype;
+    int E, top_k, n_groups, group_n, share_log2, top_groups, dtype;     // group_n: experts of a group; 2^share_log2 lanes look through one
     int pair, renormalise;
     double scale, two;                  // two: 2^gate_bits
 };
-constexpr int kRowLanes = 16;           // lanes of a row
 
-// the value of another lane of the row's 16: after the steps 0 to 3 every lane has met all others
-template <class T> __device__ __forceinline__ T from_lane(T v, int step) {
+// Values x and y of neighbouring lanes, blocks of lanes from step 2 on, one of them the lane's own (or its block's): after the steps 0 to 3 every lane of 16 has met all others, after the steps 0 to 5 of 64.
+template <class T> __device__ __forceinline__ void meet(T v, int step, T& x, T& y) {
     constexpr int n = sizeof(T) / 4;
-    int w[n];
+    int w[n], o[n];
     __builtin_memcpy(w, &v, sizeof(T));
 #pragma unroll
-    for (int i = 0; i < n; i++)
-        w[i] = step == 0 ? __builtin_amdgcn_update_dpp(0, w[i], 0xB1, 0xf, 0xf, true)           // quad_perm:[1,0,3,2]
-             : step == 1 ? __builtin_amdgcn_update_dpp(0, w[i], 0x4E, 0xf, 0xf, true)           // quad_perm:[2,3,0,1]
-             : step == 2 ? __builtin_amdgcn_update_dpp(0, w[i], 0x141, 0xf, 0xf, true)          // row_half_mirror
-                         : __builtin_amdgcn_update_dpp(0, w[i], 0x140, 0xf, 0xf, true);         // row_mirror
-    __builtin_memcpy(&v, w, sizeof(T));
-    return v;
+    for (int i = 0; i < n; i++) {
+        if (step == 0) o[i] = __builtin_amdgcn_update_dpp(0, w[i], 0xB1, 0xf, 0xf, true);               // quad_perm:[1,0,3,2]
+        else if (step == 1) o[i] = __builtin_amdgcn_update_dpp(0, w[i], 0x4E, 0xf, 0xf, true);          // quad_perm:[2,3,0,1]
+        else if (step == 2) o[i] = __builtin_amdgcn_update_dpp(0, w[i], 0x141, 0xf, 0xf, true);         // row_half_mirror
+        else if (step == 3) o[i] = __builtin_amdgcn_update_dpp(0, w[i], 0x140, 0xf, 0xf, true);         // row_mirror
+        else {
+            const auto r = step == 4 ? __builtin_amdgcn_permlane16_swap(w[i], w[i], false, false) : __builtin_amdgcn_permlane32_swap(w[i], w[i], false, false);
+            w[i] = (int)r[0]; o[i] = (int)r[1];
+        }
+    }
+    __builtin_memcpy(&x, w, sizeof(T));
+    __builtin_memcpy(&y, o, sizeof(T));
 }
 __device__ __forceinline__ int larger(int a, int b) { return a > b ? a : b; }
 __device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
 __device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 __device__ __forceinline__ float smaller(float a, float b) { return fminf(a, b); }
 __device__ __forceinline__ double smaller(double a, double b) { return fmin(a, b); }
-template <class T> __device__ __forceinline__ T row_max(T v) {
+// of the L lanes of a row
+template <int L, class T> __device__ __forceinline__ T row_max(T v) {
 #pragma unroll
-    for (int s = 0; s < 4; s++) v = larger(v, from_lane(v, s));
+    for (int s = 0; 1 << s < L; s++) { T x, y; meet(v, s, x, y); v = larger(x, y); }
     return v;
 }
-__device__ __forceinline__ int row_min(int v) {
+template <int L> __device__ __forceinline__ int row_min(int v) {
 #pragma unroll
-    for (int s = 0; s < 4; s++) { const int o = from_lane(v, s); v = o < v ? o : v; }
+    for (int s = 0; 1 << s < L; s++) { int x, y; meet(v, s, x, y); v = x < y ? x : y; }
     return v;
 }
-__device__ __forceinline__ double row_sum(double v) {
+template <int L> __device__ __forceinline__ double row_sum(double v) {
 #pragma unroll
-    for (int s = 0; s < 4; s++) v += from_lane(v, s);
+    for (int s = 0; 1 << s < L; s++) { double x, y; meet(v, s, x, y); v = x + y; }
     return v;
 }
 // e^a for a <= 0: a = n ln 2 + r, |r| <= ln 2 / 2, and the series of e^r up to r^13 / 13! (what follows is below 2^-57); off by 1.5 units in the last place at most.
@@ -93,21 +98,22 @@ __device__ __forceinline__ float half_logit(uint16_t v, int dtype) {
     return dtype == DASH_BF16 ? __uint_as_float((uint32_t)v << 16) : (float)__builtin_bit_cast(_Float16, v);
 }
 
-// 16 lanes a row, V neighbouring experts a lane.  BIAS: choice values are sums in 64 bits, else the logits themselves.
-// A row's choice values stand in LDS, 16 lanes' runs of V, and every lane keeps the largest of its run.  A round: the largest of the 16 (four steps between lanes), the first run that
-// holds it; the 16 lanes look through that run together for the first place of it and for what is largest without it.  A row lies within a wave: no barriers.  (Each
+// L lanes a row, V neighbouring experts a lane.  BIAS: choice values are sums in 64 bits, else the logits themselves.
+// A row's choice values stand in LDS, the lanes' runs of V, and every lane keeps the largest of its run.  A round: the largest of these (four to six steps between lanes), the first run that
+// holds it; the lanes look through that run together for the first place of it and for what is largest without it.  A row lies within a wave: no barriers.  (Each
 // lane through its own run again in registers: 65536 rows of 256 experts, eight chosen, 84.5 us.)  The rounds compare 32-bit integers: the logits, or the sums rounded to float32, which keeps
 // their order but for sums that it makes equal; a wave that meets equal ones among its largest does its rounds again with the sums themselves (rounds in 64 bits for all: 44.1 us).
-// Bound by vector instructions, a third of them the exponentials (13 steps in 64 bits an expert; a float32 sum would move a choice or a gate): 65536 rows of 256 experts,
-// eight chosen, 40.5 us, 64 % of the cycles, 39.8 MB read and written in 8.2 us at a copy's rate.  4096 rows of 256 in eight groups, four of them: 9.4 to 11 us; 1000 rows of 160: 7.8;
-// one row of 8: 4.7 to 5.2, a launch and one row's chain of steps.
-template <int V, bool BIAS, bool GROUPS, bool SIGMOID>
-__global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs A) {
+// Bound by vector instructions where rows are many, a third of them the exponentials (13 steps in 64 bits an expert; a float32 sum would move a choice or a gate): 65536 rows of 256 experts,
+// eight chosen, 40.5 us, 64 % of the cycles, 39.8 MB read and written in 8.2 us at a copy's rate.  Few rows: the steps of one row's lanes one after the other, which more lanes make fewer.
+// 4096 rows of 256 in eight groups, four of them: 9.8 us; 1000 rows of 160 in eight groups: 5.8; one row of 8: 4.7 to 5.2.
+constexpr int kChooseThreads = 256;
+template <int L, int V, bool BIAS, bool GROUPS, bool SIGMOID>
+__global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
     typedef typename std::conditional<BIAS, double, float>::type Key;
-    constexpr int T = V == 64 ? 64 : 256, R = T / kRowLanes, P = V + (V > 1 ? 1 : 0);      // P: a run and a word, against bank conflicts
+    constexpr int R = kChooseThreads / L, P = V + (V > 1 ? 1 : 0);      // P: a run and a word, against bank conflicts
     constexpr Key kNone = -(Key)INFINITY;
-    __shared__ Key s_key[R][P * kRowLanes];
-    const int lane = threadIdx.x % kRowLanes, rr = threadIdx.x / kRowLanes;
+    __shared__ Key s_key[R][P * L];
+    const int lane = threadIdx.x % L, rr = threadIdx.x / L;
     const int64_t row_ = A.first + (int64_t)blockIdx.x * R + rr, row = row_ < A.n ? row_ : A.n - 1;
     const bool use = !A.valid || A.valid[row];
     auto lds_order = [&]() __attribute__((always_inline)) { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); __builtin_amdgcn_wave_barrier(); };
@@ -136,7 +142,7 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
     float m = l[0];
 #pragma unroll
     for (int v = 1; v < V; v++) m = fmaxf(m, l[v]);
-    m = row_max(m);
+    m = row_max<L>(m);
     const double top = m > -INFINITY ? (double)m : 0.0;
     double common = 1;                          // of all softmax scores
     const Series series;
@@ -159,7 +165,7 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
 #pragma unroll
         for (int v = 0; v < V; v++) { s[v] = score(l[v]); sum += s[v]; }
         if (sum_wanted) {
-            sum = row_sum(sum);
+            sum = row_sum<L>(sum);
             common = sum > 0 ? inverse_of(sum) : 0.0;
         }
 #pragma unroll
@@ -172,28 +178,53 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
             double sum = 0;
 #pragma unroll
             for (int v = 0; v < V; v++) sum += exp_of((double)l[v] - top, series);
-            sum = row_sum(sum);
+            sum = row_sum<L>(sum);
             common = sum > 0 ? inverse_of(sum) : 0.0;
         }
 #pragma unroll
         for (int v = 0; v < V; v++) key[v] = l[v];
     }
 
+    // a bit of every lane of the row
+    typedef typename std::conditional<L == 64, uint64_t, uint32_t>::type Bits;
+    auto row_bits = [&](bool x) __attribute__((always_inline)) {
+        if constexpr (L == 64) return (Bits)__ballot(x);
+        else return (Bits)(__ballot(x) >> (threadIdx.x & (64 - L))) & (Bits)((1ull << L) - 1);
+    };
+    auto lowest = [](Bits x) __attribute__((always_inline)) { return L == 64 ? __builtin_ctzll(x) : __builtin_ctz((uint32_t)x); };
     if constexpr (GROUPS) {
+        // kBatch of the LDS's values at a time, the last in the place of those past the end (which count for nothing): one wait each
+        constexpr int kBatch = 8;
         __shared__ double s_group[R][64];
-        __shared__ uint8_t s_kept[R][64];
 #pragma unroll
         for (int v = 0; v < V; v++) s_key[rr][lane * P + v] = key[v];
         lds_order();
-        const int n = A.E / A.n_groups;
-        // a lane per group: its two largest
-        for (int g = lane; g < A.n_groups; g += kRowLanes) {
+        const int n = A.group_n;
+        // share_log2: 2^share_log2 neighbouring lanes find a group's two largest, all 16 lanes at work
+        const int share = 1 << A.share_log2;
+        for (int g = lane >> A.share_log2; g < A.n_groups; g += L >> A.share_log2) {
             Key a = kNone, b = kNone;
-            for (int i = 0; i < n; i++) {
-                const int e = g * n + i;
-                const Key k = s_key[rr][e / V * P + e % V];
-                b = larger(b, smaller(a, k));
-                a = larger(a, k);
+            for (int i = lane & (share - 1); i < n; i += share * kBatch) {
+                Key k[kBatch];
+#pragma unroll
+                for (int j = 0; j < kBatch; j++) {
+                    const int e = g * n + (i + j * share < n ? i + j * share : n - 1);
+                    k[j] = s_key[rr][e / V * P + e % V];
+                }
+#pragma unroll
+                for (int j = 0; j < kBatch; j++) {
+                    k[j] = i + j * share < n ? k[j] : kNone;
+                    b = larger(b, smaller(a, k[j]));
+                    a = larger(a, k[j]);
+                }
+            }
+#pragma unroll
+            for (int step = 0; 1 << step < L; step++) {
+                if (step >= A.share_log2) break;
+                Key a0, a1, b0, b1;
+                meet(a, step, a0, a1); meet(b, step, b0, b1);
+                b = larger(smaller(a0, a1), larger(b0, b1));
+                a = larger(a0, a1);
             }
             double value = a;
             if (A.pair && a > kNone) {
@@ -204,27 +235,35 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
             s_group[rr][g] = value;
         }
         lds_order();
-        for (int g = lane; g < A.n_groups; g += kRowLanes) {
-            const double mine = s_group[rr][g];
+        uint64_t kept = 0;
+        for (int g0 = 0; g0 < A.n_groups; g0 += L) {
+            const int g = g0 + lane;
+            const double mine = s_group[rr][g < A.n_groups ? g : 0];
             int rank = 0;
-            for (int i = 0; i < A.n_groups; i++) {
-                const double o = s_group[rr][i];
-                rank += o > mine || (o == mine && i < g) ? 1 : 0;
+            for (int i = 0; i < A.n_groups; i += kBatch) {
+                double o[kBatch];
+#pragma unroll
+                for (int j = 0; j < kBatch; j++) o[j] = s_group[rr][i + j < A.n_groups ? i + j : 0];
+#pragma unroll
+                for (int j = 0; j < kBatch; j++) rank += i + j < A.n_groups && (o[j] > mine || (o[j] == mine && i + j < g)) ? 1 : 0;
             }
-            s_kept[rr][g] = rank < A.top_groups;
+            kept |= (uint64_t)row_bits(g < A.n_groups && rank < A.top_groups) << g0;
         }
         lds_order();
         int g = lane * V / n, in = lane * V - g * n;
 #pragma unroll
         for (int v = 0; v < V; v++) {
-            if (!(g < A.n_groups && s_kept[rr][g])) key[v] = kNone;
+            if (!(g < A.n_groups && (kept >> (g & 63) & 1))) key[v] = kNone;
             if (++in == n) { in = 0; g++; }
         }
     }
 
-    // lane j mod 16 keeps number j
-    int mine[2] = {-1, -1};
-    constexpr int kPer = (V + kRowLanes - 1) / kRowLanes;       // of a run, per lane
+    // lane j mod L keeps number j
+    constexpr int kMine = (DASH_MAX_TOP_K + L - 1) / L;
+    int mine[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; i++) mine[i] = -1;
+    constexpr int kPer = (V + L - 1) / L;       // of a run, per lane
     bool equal = false;
     {
         // integers in the order of the floats (without a second zero); none: the lowest
@@ -238,41 +277,40 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
             best = k > best ? k : best;
         }
         lds_order();
-        const int row_at = threadIdx.x & 48;                    // the row's lanes in the wave
-        auto row_bits = [&](bool x) __attribute__((always_inline)) { return (uint32_t)(__ballot(x) >> row_at) & 0xffffu; };
         for (int j = 0; j < A.top_k; j++) {
-            const int most = row_max(best);
+            const int most = row_max<L>(best);
             if (most == INT_MIN || !use) break;         // (a row's lanes leave together)
-            const uint32_t runs = row_bits(best == most);
-            const int run = __builtin_ctz(runs);
+            const Bits runs = row_bits(best == most);
+            const int run = lowest(runs);
             int k[kPer], rest = INT_MIN;
-            uint32_t there = 0;
+            Bits there = 0;
             int first = 0;
 #pragma unroll
-            for (int i = 0; i < kPer; i++) k[i] = i * kRowLanes + lane < V ? to[run * P + i * kRowLanes + lane] : INT_MIN;
+            for (int i = 0; i < kPer; i++) k[i] = i * L + lane < V ? to[run * P + i * L + lane] : INT_MIN;
             bool several = (runs & (runs - 1)) != 0;
 #pragma unroll
             for (int i = 0; i < kPer; i++) {
-                const uint32_t bits = row_bits(k[i] == most);
+                const Bits bits = row_bits(k[i] == most);
                 several |= (bits & (bits - 1)) != 0 || (bits && there);
-                if (bits && !there) first = i * kRowLanes + __builtin_ctz(bits);
+                if (bits && !there) first = i * L + lowest(bits);
                 there |= bits;
             }
 #pragma unroll
             for (int i = 0; i < kPer; i++) {
-                if (i * kRowLanes + lane == first) to[run * P + first] = INT_MIN;
+                if (i * L + lane == first) to[run * P + first] = INT_MIN;
                 else rest = k[i] > rest ? k[i] : rest;
             }
-            rest = row_max(rest);
+            rest = row_max<L>(rest);
             lds_order();
             if (lane == run) best = rest;
-            if (j % kRowLanes == lane) mine[j / kRowLanes] = run * V + first;
+            if (j % L == lane) mine[j / L] = run * V + first;
             equal |= several;
         }
     }
     if (BIAS && __any(equal)) {
         lds_order();
-        mine[0] = mine[1] = -1;
+#pragma unroll
+        for (int i = 0; i < kMine; i++) mine[i] = -1;
         Key best = kNone;
 #pragma unroll
         for (int v = 0; v < V; v++) {
@@ -282,33 +320,33 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
         }
         lds_order();
         for (int j = 0; j < A.top_k; j++) {
-            const Key most = row_max(best);
+            const Key most = row_max<L>(best);
             if (!(most > kNone) || !use) break;
-            const int run = row_min(best == most ? lane : kRowLanes);
+            const int run = row_min<L>(best == most ? lane : L);
             Key rest = kNone, k[kPer];
             int first = V;
 #pragma unroll
             for (int i = 0; i < kPer; i++) {
-                const int at = i * kRowLanes + lane;
+                const int at = i * L + lane;
                 k[i] = at < V ? s_key[rr][run * P + at] : kNone;
                 if (k[i] == most && first == V) first = at;
             }
-            first = row_min(first);
+            first = row_min<L>(first);
 #pragma unroll
             for (int i = 0; i < kPer; i++) {
-                const int at = i * kRowLanes + lane;
+                const int at = i * L + lane;
                 if (at == first) s_key[rr][run * P + at] = kNone;
                 else rest = larger(rest, k[i]);
             }
-            rest = row_max(rest);
+            rest = row_max<L>(rest);
             lds_order();
             if (lane == run) best = rest;
-            if (j % kRowLanes == lane) mine[j / kRowLanes] = run * V + first;
+            if (j % L == lane) mine[j / L] = run * V + first;
         }
     }
-    double s[2];
+    double s[kMine];
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
+    for (int i = 0; i < kMine; i++) {
         s[i] = 0;
         if (mine[i] >= 0) {
             const int64_t at = row * A.row_stride + mine[i];
@@ -317,13 +355,13 @@ __global__ __launch_bounds__(V == 64 ? 64 : 256) void k_choose(const ChooseArgs 
     }
     double factor = A.scale;
     if (A.renormalise) {
-        const double sum = row_sum(s[0] + s[1]);
+        const double sum = row_sum<L>(kMine == 2 ? s[0] + s[kMine - 1] : s[0]);
         factor = sum > 0 ? A.scale / sum : 0.0;
     }
     if (row_ >= A.n) return;
 #pragma unroll
-    for (int i = 0; i < 2; i++) {
-        const int j = i * kRowLanes + lane;
+    for (int i = 0; i < kMine; i++) {
+        const int j = i * L + lane;
         if (j >= A.top_k) break;
         const int64_t to = row * A.top_k + j;
         const double w = s[i] * factor;
@@ -354,33 +392,45 @@ int dash_choose(dash_ctx* c, const dash_router* r, const void* logits, int dtype
     ChooseArgs A;
     memset(&A, 0, sizeof(A));
     A.logits = logits; A.bias = r->bias; A.valid = valid; A.experts = experts; A.gates = gates; A.weights = weights;
-    A.row_stride = row_stride; A.n = n; A.E = E; A.top_k = r->top_k; A.n_groups = G; A.top_groups = r->top_groups; A.dtype = dtype;
+    A.row_stride = row_stride; A.n = n; A.E = E; A.top_k = r->top_k; A.n_groups = G; A.group_n = E / G; A.top_groups = r->top_groups; A.dtype = dtype;
     A.pair = r->group_score == DASH_GROUP_PAIR && r->top_groups < G; A.renormalise = r->renormalise != 0;
     A.scale = r->scale; A.two = ldexp(1.0, r->gate_bits);
-    auto launch = [&](auto v) {
-        constexpr int V = decltype(v)::value, T = V == 64 ? 64 : 256, R = T / kRowLanes;
-        constexpr int64_t most = 0xffffffffll / 256;
+    auto launch = [&](auto lanes, auto v) {
+        constexpr int L = decltype(lanes)::value, V = decltype(v)::value, R = kChooseThreads / L;
+        constexpr int64_t most = 0xffffffffll / kChooseThreads;
+        const bool groups = r->top_groups < G;
+        while (G << (A.share_log2 + 1) <= L) A.share_log2++;
+        auto kernel = [&](auto sigmoid) -> void (*)(ChooseArgs) {
+            constexpr bool S = decltype(sigmoid)::value;
+            if (r->bias) return groups ? k_choose<L, V, true, true, S> : k_choose<L, V, true, false, S>;
+            if (groups) return k_choose<L, V, false, true, S>;
+            if constexpr (L == 16 || V == 16) return k_choose<L, V, false, false, S>;
+            return nullptr;                     // (by the rule below none)
+        };
+        const auto k = r->score == DASH_SIGMOID ? kernel(std::true_type{}) : kernel(std::false_type{});
         const int64_t blocks = (n + R - 1) / R;
         for (int64_t first = 0; first < blocks; first += most) {
             A.first = first * R;
-            const dim3 grid((uint32_t)(blocks - first < most ? blocks - first : most));
-            const bool groups = r->top_groups < G;
-            auto kernel = [&](auto sigmoid) {
-                constexpr bool S = decltype(sigmoid)::value;
-                return r->bias ? (groups ? k_choose<V, true, true, S> : k_choose<V, true, false, S>) : groups ? k_choose<V, false, true, S> : k_choose<V, false, false, S>;
-            };
-            const auto k = r->score == DASH_SIGMOID ? kernel(std::true_type{}) : kernel(std::false_type{});
-            hipLaunchKernelGGL(k, grid, dim3(T), 0, (hipStream_t)stream, A);
+            hipLaunchKernelGGL(k, dim3((uint32_t)(blocks - first < most ? blocks - first : most)), dim3(kChooseThreads), 0, (hipStream_t)stream, A);
         }
     };
     using std::integral_constant;
-    if (E <= 16) launch(integral_constant<int, 1>{});
-    else if (E <= 32) launch(integral_constant<int, 2>{});
-    else if (E <= 64) launch(integral_constant<int, 4>{});
-    else if (E <= 128) launch(integral_constant<int, 8>{});
-    else if (E <= 256) launch(integral_constant<int, 16>{});
-    else if (E <= 512) launch(integral_constant<int, 32>{});
-    else launch(integral_constant<int, 64>{});
+    constexpr integral_constant<int, 16> l16{};
+    constexpr integral_constant<int, 32> l32{};
+    constexpr integral_constant<int, 64> l64{};
+    // Lanes of a row.  What they do for their own experts one after the other takes the time where rows are few, and with sums in 64 bits and groups of many experts also where they are many; each
+    // round costs instructions by the lane.  us with 16, 32, 64 lanes, eight chosen of 256 experts with a bias and groups (sigmoid): 1 row 9.5, 7.2, 6.2; 1000: 10.2, 7.7, 6.7; 2048: 10.2, 7.9, 7.9;
+    // 4096: 10.3, 9.8, 10.7; 8192: 14.0, 13.5, 16.8; 65536: 66.6, 67.7, 103; with neither: 4.0, 3.9, 4.1 for one row, 18.6, 27.7, 49.1 for 65536.  Of 128: 1000 rows 7.7, 6.4, 6.4;
+    // 8192: 10.2, 10.5, 15.6.  Of 512: 1000 rows 15.9, 10.3, 8.0; 2048: 16.0, 10.3, 9.9; 4096: 16.2, 14.1, 13.8; 16384: 41.6, 33.7, 36.4; with neither 1 row 5.1, 3.9, 4.1, 65536: 30.4, 32.1, 52.8.  Of 1024, 32 and 64: 1000 rows 15.8, 10.4;
+    // 65536: 253, 211.
+    const bool much = r->bias || r->top_groups < G;
+    if (E <= 16) launch(l16, integral_constant<int, 1>{});
+    else if (E <= 32) launch(l16, integral_constant<int, 2>{});
+    else if (E <= 64) launch(l16, integral_constant<int, 4>{});
+    else if (E <= 128) much && n <= 2048 ? launch(l32, integral_constant<int, 4>{}) : launch(l16, integral_constant<int, 8>{});
+    else if (E <= 256) much && n <= 1024 ? launch(l64, integral_constant<int, 4>{}) : much && n <= 8192 ? launch(l32, integral_constant<int, 8>{}) : launch(l16, integral_constant<int, 16>{});
+    else if (E <= 512) much && n <= 2048 ? launch(l64, integral_constant<int, 8>{}) : launch(l32, integral_constant<int, 16>{});
+    else launch(l64, integral_constant<int, 16>{});
     DASH_HIP(hipGetLastError());
     return DASH_OK;
 }

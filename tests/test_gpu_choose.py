@@ -173,6 +173,26 @@ def test_many_rows(ctx):
     check(ctx, 1.5 * g.standard_normal((5000, 64)), 6, "bf16", bias=0.05 * g.standard_normal(64), sigmoid=True, groups=8, top_groups=3, pair=True, scale=2.5, gate_bits=12)
 
 
+@pytest.mark.parametrize("n,E", [(2048, 72), (2049, 72), (1024, 128), (2049, 128), (1024, 136), (1025, 256), (8192, 200), (8193, 256), (2048, 264), (2049, 512), (2049, 400)])
+def test_lanes_of_a_row(ctx, n, E):
+    """the kernels by rows and experts: plain, with a bias, in groups, with both, of rows with ties, masks and nothing at all among others"""
+    g = np.random.default_rng(n + E)
+    rows = 1.5 * g.standard_normal((97, E))
+    rows[5] = -np.inf
+    rows[6, 3:] = -np.inf
+    rows[7] = 0.5
+    rows[8] = np.round(rows[8])
+    rows[9, ::3] = np.nan
+    rows[10, E // 2:] = np.inf
+    l = np.resize(rows, (n, E))
+    b = np.round(0.1 * g.standard_normal(E), 2)
+    check(ctx, l, 6, "bf16")
+    check(ctx, l, 6, "f32", bias=b)
+    check(ctx, l, 6, "f16", bias=b, sigmoid=True, groups=8, top_groups=3, pair=True)
+    check(ctx, l, 6, "f32", groups=8, top_groups=3, pair=True, renormalise=False)
+    check(ctx, l, 6, "bf16", sigmoid=True, groups=4, top_groups=1)
+
+
 def test_another_stream_and_a_graph(ctx):
     from paper_2302_06361_amd import Choice, Router
     g = np.random.default_rng(13)
