@@ -30,15 +30,16 @@
 // 4.8 of them for a single stage: launch, the chain of loads to the first labels, results.
 //
 // 8-bit floats.  512 e4m3 S mod m by a table of 256 bytes in LDS, one for every scale (128 inputs) that a block passes: a byte read a weight (64 lanes in 4.3
-// clocks, bank conflicts among them; 2.8 with the signs apart in 128 entries, whose instructions cost more than that saves), joined by three v_perm for four.  An operand
+// clocks, bank conflicts among them; 2.8 with the signs apart in 128 entries, whose instructions cost more than that saves), joined by two v_perm and a v_or for four.  An operand
 // holds 32 features, so what a table read serves is the tile's digits: 512 of them where the weights are expanded once a block, 256 or 128 where a wave's
 // weights are its own.  m is a prime of the tile, or the product (up to 240: signed bytes) of a class of primes whose digits then share a tile and its reads: 2, 3, 5,
 // ... 37 are 6 classes, one row of them 7 tiles of 128 digits instead of 12.  The sums take either sign and start at a multiple of p, as with bytes.
 //   Where many blocks wait, residues of single primes are better, as bytes up to 37 leave more of the power to the clock (128 rows, 4096 -> 4096, largest tile:
 // 1 137 us, classes 1 271).
 //   What bounds it.  128 rows, 4096 -> 4096, 12 primes: 1 127, of the cycles the LDS busy in 49 %, the matrix pipe in 49, vector instructions in 30, at 1.7 to 2.2 GHz.  With
-// 128 x 128 tiles the table reads: LDS 84 %, 1 638.  32 experts, 256 rows, 1024 -> 2048: 455 (256 x 128).  One row, 4096 -> 4096: 34.0, a stage of a lone block 0.45
-// us, of it 0.185 without the expansion: reads wait for codes and products for reads.  One row, 784 -> 128: 10.6.
+// 128 x 128 tiles the table reads: LDS 84 %, 1 638.  32 experts, 256 rows, 1024 -> 2048: 455 (256 x 128).  One row, 4096 -> 4096: 34.0, a stage 0.43
+// us in each of 224 blocks, the time of its LDS accesses (tables 550 clocks, labels 256, codes and loads 190), 0.185 without the expansion.  One row, 784 -> 128: 10.6, 5.9 for a single
+// stage, then 0.65 for two.
 //   The compiler must not see accesses that could be LDS or scalar loads near the loop: from then on it waits for all LDS results at once (narrow tiles 1 702 -> 1 638).
 #pragma once
 #include <string.h>
