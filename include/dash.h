@@ -229,8 +229,8 @@ typedef struct {
 /* logits: device, n rows of n_experts `dtype` elements (DASH_F32, DASH_BF16, DASH_F16), row_stride (>= n_experts) elements apart.  Of every row: scores s = softmax(l)
  * or sigmoid(l); choice values c = s + bias, without a bias the order of l (groups of DASH_GROUP_PAIR: sums of s); the top_groups groups
  * with the largest value; of their experts the top_k with the largest c, in descending order.  Ties go to the lower number.  Weights w =
- * scale * s (renormalise: / sum of the chosen s, zero if that is zero), gates = w * 2^gate_bits to the nearest integer, ties to the even.  Scores, sums, choice
- * values and weights are held in 64 bits.
+ * scale * s (renormalise: / sum of the chosen s, zero if that is zero), gates = w * 2^gate_bits to the nearest integer, ties to the even
+ * (of the quotient itself, not of its rounding: k equal scores get gates of scale * 2^gate_bits / k).  Scores, sums, choice values and weights are held in 64 bits.
  * A logit that is not a number counts as -infinity, infinity as the largest float32.  Experts whose logit is -infinity, or whose choice value is -infinity or no number, are
  * never chosen; groups without any other are not either.  A score below e^-690 (softmax: of the row's largest) is zero.  valid: device, a byte for every row, 0: no expert is chosen (NULL: all rows are valid).  What is missing of
  * top_k: expert -1, weight and gate 0.

@@ -3,7 +3,7 @@
 //     scores s = softmax(l) or sigmoid(l);  choice values c = s + b, without a bias the order of l;
 //     of n_groups equal groups of experts the top_groups with the largest c (or the largest sum of two);  of their experts the top_k largest c;
 //     w = scale s (renormalise: / sum of the chosen s);  gate = w 2^gate_bits, to the nearest integer, ties to the even.
-// Everything that a comparison or a rounding decides on is held in 64 bits.
+// Everything that a comparison or a rounding decides on is held in 64 bits; where a quotient stands next to the middle of two gates, its remainder decides.
 #include <limits.h>
 #include <math.h>
 #include <string.h>
@@ -86,7 +86,7 @@ __device__ __forceinline__ double exp_of(double a, const Series& S) {
     s = fma(s, r, 1.0);
     return ldexp(s, (int)n);
 }
-// 1 / v, 0 < v < 2^1000: an estimate of at least 20 bits and two steps of Newton's
+// 1 / v, 2^-1000 < v < 2^1000: an estimate of at least 20 bits and two steps of Newton's
 __device__ __forceinline__ double inverse_of(double v) {
     double y = __builtin_amdgcn_rcp(v);
     y = fma(fma(-v, y, 1.0), y, y);
@@ -144,13 +144,16 @@ __global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
     for (int v = 1; v < V; v++) m = fmaxf(m, l[v]);
     m = row_max<L>(m);
     const double top = m > -INFINITY ? (double)m : 0.0;
-    double common = 1;                          // of all softmax scores
+    double whole = 1;                           // softmax: the sum that every score is divided by, and its inverse
+    double common = 1;
     const Series series;
-    auto score = [&](float x) __attribute__((always_inline)) -> double {
-        if (!SIGMOID) return exp_of((double)x - top, series) * common;
+    // score times `whole`
+    auto part = [&](float x) __attribute__((always_inline)) -> double {
+        if (!SIGMOID) return exp_of((double)x - top, series);
         const double t = exp_of(-fabs((double)x), series);
         return (x >= 0 ? 1.0 : t) * inverse_of(1 + t);
     };
+    auto score = [&](float x) __attribute__((always_inline)) -> double { return SIGMOID ? part(x) : part(x) * common; };
     const bool sum_wanted = !SIGMOID && (BIAS || A.pair || !A.renormalise);     // (renormalised and of no other use: any common factor)
     Key key[V];
     // an expert that may be chosen (a bias that is no number makes its sum none)
@@ -165,7 +168,7 @@ __global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
 #pragma unroll
         for (int v = 0; v < V; v++) { s[v] = score(l[v]); sum += s[v]; }
         if (sum_wanted) {
-            sum = row_sum<L>(sum);
+            whole = sum = row_sum<L>(sum);
             common = sum > 0 ? inverse_of(sum) : 0.0;
         }
 #pragma unroll
@@ -178,7 +181,7 @@ __global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
             double sum = 0;
 #pragma unroll
             for (int v = 0; v < V; v++) sum += exp_of((double)l[v] - top, series);
-            sum = row_sum<L>(sum);
+            whole = sum = row_sum<L>(sum);
             common = sum > 0 ? inverse_of(sum) : 0.0;
         }
 #pragma unroll
@@ -344,19 +347,59 @@ __global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
             if (j % L == lane) mine[j / L] = run * V + first;
         }
     }
+    // scores, softmax's times `whole`
     double s[kMine];
 #pragma unroll
     for (int i = 0; i < kMine; i++) {
         s[i] = 0;
         if (mine[i] >= 0) {
             const int64_t at = row * A.row_stride + mine[i];
-            s[i] = score(clean_logit(A.dtype == DASH_F32 ? ((const float*)A.logits)[at] : half_logit(((const uint16_t*)A.logits)[at], A.dtype)));
+            s[i] = part(clean_logit(A.dtype == DASH_F32 ? ((const float*)A.logits)[at] : half_logit(((const uint16_t*)A.logits)[at], A.dtype)));
         }
     }
-    double factor = A.scale;
+    double inverse = common;                    // of what s are divided by
     if (A.renormalise) {
         const double sum = row_sum<L>(kMine == 2 ? s[0] + s[kMine - 1] : s[0]);
-        factor = sum > 0 ? A.scale / sum : 0.0;
+        inverse = sum > 0 ? inverse_of(sum) : 0.0;
+    }
+    double w[kMine], gate[kMine];
+    bool near = false;                          // gates next to the middle of two integers (what was rounded until here is below 2^-19 of a gate)
+#pragma unroll
+    for (int i = 0; i < kMine; i++) {
+        if (i * L >= A.top_k) break;
+        w[i] = s[i] * inverse * A.scale;
+        const double t = w[i] * A.two;
+        gate[i] = rint(t);
+        near |= fabs(fabs(t - gate[i]) - 0.5) < 0x1p-18;
+    }
+    if (A.gates && __any(near)) {
+        // Equal scores share as integers do, and a rounded quotient would take the middle of two gates to either side: the sign of scale 2^gate_bits s - (m + 1/2) sum
+        // decides, without a rounding.  A sum of chosen scores is held in two numbers for that: it is exact where they are equal.
+        double high = s[0], low = 0;
+        auto add = [&](double x, double y) __attribute__((always_inline)) {
+            high = x + y;
+            const double t = high - x;
+            low += (x - (high - t)) + (y - t);
+        };
+        if (A.renormalise) {
+            if (kMine == 2) add(s[0], s[kMine - 1]);
+#pragma unroll
+            for (int step = 0; 1 << step < L; step++) {
+                double x, y, a, b;
+                meet(high, step, x, y); meet(low, step, a, b);
+                low = a + b;
+                add(x, y);
+            }
+        } else high = whole;
+#pragma unroll
+        for (int i = 0; i < kMine; i++) {
+            if (i * L >= A.top_k) break;
+            const double t = w[i] * A.two, m = floor(t), middle = m + 0.5, p = middle * high;
+            if (!(fabs(t - middle) < 0x1p-18)) continue;
+            // (each of these is exact: the products leave less than 40 bits next to p)
+            const double over = fma(A.scale * A.two, s[i], -p) - fma(middle, low, fma(middle, high, -p));
+            gate[i] = over > 0 || (over == 0 && (int)m & 1) ? m + 1 : m;
+        }
     }
     if (row_ >= A.n) return;
 #pragma unroll
@@ -364,10 +407,9 @@ __global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
         const int j = i * L + lane;
         if (j >= A.top_k) break;
         const int64_t to = row * A.top_k + j;
-        const double w = s[i] * factor;
         A.experts[to] = mine[i];
-        if (A.gates) A.gates[to] = (int32_t)rint(w * A.two);
-        if (A.weights) A.weights[to] = (float)w;
+        if (A.gates) A.gates[to] = (int32_t)gate[i];
+        if (A.weights) A.weights[to] = (float)w[i];
     }
 }
 
