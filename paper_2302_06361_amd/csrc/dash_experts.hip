@@ -15,6 +15,7 @@
 #include <string.h>
 
 #include "dash_experts.h"
+#include "dash_experts_rule.h"
 
 namespace dash {
 
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(kF8Threads) void k_f8_quantise(const QuantF8Args A)
     const T* const src = (const T*)A.w + (int64_t)e * A.expert_stride + (int64_t)row0 * A.row_stride;
     __shared__ uint32_t part[kF8Threads / 64];
     typename Q::Vec in[kSteps];
-    if (col0 + kScaleBlock <= A.K) {
+    if (columns_inside(col0, kScaleBlock, A.K)) {
 #pragma unroll
         for (int s = 0; s < kSteps; s++)
             if (s * kRows < rows) in[s] = *(const VecAny*)(src + (int64_t)(r0 + s * kRows < rows ? r0 + s * kRows : rows - 1) * A.row_stride + col);

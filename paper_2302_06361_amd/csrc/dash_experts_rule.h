@@ -1,4 +1,4 @@
-// dash_experts_rule.h -- which tile the products of an expert layer take, as a function of its sizes alone, and the grid of the launch (host code)
+// dash_experts_rule.h -- which tile the products of an expert layer take, as a function of its sizes alone, and the grid of the launch (host code); the columns of a block
 #pragma once
 #include <stdint.h>
 
@@ -148,6 +148,9 @@ inline ExpertsTile experts_tile8(int forced, const ExpertsShape8& S) {
         if (experts_us8(S, (ExpertsTile)t) < experts_us8(S, (ExpertsTile)best)) best = t;
     return (ExpertsTile)best;
 }
+
+// whether the columns first .. first + n - 1 of a row of K all exist (K up to 2^31 - 1: their end may pass 31 bits)
+constexpr bool columns_inside(int first, int n, int K) { return K - first >= n; }
 
 // At least `blocks` blocks of `threads` threads as x times y, x a multiple of the 8 XCDs: a direction of a grid holds fewer than 2^32 threads.
 struct BlockGrid { uint32_t x, y; };

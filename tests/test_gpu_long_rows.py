@@ -1,0 +1,36 @@
+"""GPU: quantisation of the longest rows that 32-bit sizes name.  Blocks do not see each other, so that the last ones are those of a short row with the same end; what lies behind a
+row would make the last scales larger."""
+import pytest
+import torch
+
+from test_gpu_experts_edges import context, memory_goes_back, need      # noqa: F401 (a fixture among them)
+
+pytestmark = pytest.mark.gpu
+SPARE = 256
+
+
+def long_row(ctx, K):
+    """[1][1][K] float16, and large numbers behind it"""
+    whole = torch.empty(K + SPARE, dtype=torch.float16, device=ctx.device)
+    for at in range(0, K, 2 ** 28):
+        whole[at:min(at + 2 ** 28, K)].normal_()
+    whole[K:] = 60000.0
+    return whole, whole[:K].view(1, 1, K)
+
+
+@pytest.mark.parametrize("K", [2 ** 31 - 1, 2 ** 31 - 128])
+def test_8_bit_floats(K):
+    ctx = context([5])
+    tiles = -(-K // 64)
+    need(2 * K + 2048 * tiles + 4 * -(-K // 128))
+    whole, w = long_row(ctx, K)
+    got = ctx.f8_quantise(w, -9).data
+    first = (K - 1) // 128 * 128 - 128
+    short = ctx.f8_quantise(w[:, :, first:].contiguous(), -9).data
+    n = -(-(K - first) // 64)
+    torch.cuda.synchronize()
+    assert torch.equal(got[(tiles - n) * 2048:tiles * 2048], short[:n * 2048])
+    scales = got[tiles * 2048:][:4 * -(-K // 128)].view(torch.int32)
+    want = short[n * 2048:][:4 * -(-(K - first) // 128)].view(torch.int32)
+    assert torch.equal(scales[-want.numel():], want)
+    assert (whole[K:] == 60000.0).all()
