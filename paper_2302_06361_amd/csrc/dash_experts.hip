@@ -264,7 +264,7 @@ __global__ __launch_bounds__(kThreads) void k_mx4_quantise(const QuantArgs A) {
     const int have = A.K - col;                      // columns from the lane's first to the end
     // all loads go out before the first is waited for: no branch but the one on the tile; rows and columns past the end read the last
     typename Q::Vec in[kSteps];
-    if ((int)(tile - rt * kt) * kTileCols + kTileCols <= A.K) {
+    if (columns_inside((int)(tile - rt * kt) * kTileCols, kTileCols, A.K)) {
 #pragma unroll
         for (int s = 0; s < kSteps; s++) {
             const int row = row0 + kRows * s < A.M ? row0 + kRows * s : A.M - 1;

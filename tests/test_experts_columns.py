@@ -31,7 +31,7 @@ def test_the_last_blocks_of_a_row(inside, n, K):
         assert bool(inside(first, n, K)) == (first + n <= K), first
 
 
-@pytest.mark.parametrize("kernel", ["k_f8_quantise"])
+@pytest.mark.parametrize("kernel", ["k_f8_quantise", "k_mx4_quantise"])
 def test_kernels_ask_it(kernel):
     """no sum of a block's first column and its width, which may pass 31 bits, in front of the loads"""
     text = open(os.path.join(CSRC, "dash_experts.hip")).read()

@@ -1,5 +1,5 @@
 """GPU: quantisation of the longest rows that 32-bit sizes name.  Blocks do not see each other, so that the last ones are those of a short row with the same end; what lies behind a
-row would make the last scales larger."""
+row would make the last scales and shifts larger."""
 import pytest
 import torch
 
@@ -33,4 +33,18 @@ def test_8_bit_floats(K):
     scales = got[tiles * 2048:][:4 * -(-K // 128)].view(torch.int32)
     want = short[n * 2048:][:4 * -(-(K - first) // 128)].view(torch.int32)
     assert torch.equal(scales[-want.numel():], want)
+    assert (whole[K:] == 60000.0).all()
+
+
+@pytest.mark.parametrize("K", [2 ** 31 - 1, 2 ** 31 - 64])
+def test_4_bit_floats(K):
+    ctx = context([5])
+    tiles = -(-K // 64)
+    need(2 * K + 1088 * tiles)
+    whole, w = long_row(ctx, K)
+    got = ctx.mx4_quantise(w, -9).data
+    first = (K - 1) // 64 * 64 - 64
+    short = ctx.mx4_quantise(w[:, :, first:].contiguous(), -9).data
+    torch.cuda.synchronize()
+    assert torch.equal(got[(tiles - 2) * 1088:], short) and short.any()
     assert (whole[K:] == 60000.0).all()
