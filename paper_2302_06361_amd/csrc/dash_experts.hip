@@ -522,7 +522,8 @@ int experts_layer(dash_ctx* c, const dash_layer* L, bool garble, const dash_labe
     if (!L->weights || ((uintptr_t)L->weights & 15) || !weight_format(L->weight_format)) return DASH_EINVAL;
     const int64_t n = L->n_elem, T = n / L->top_k;
     const int M = L->out_c, K = L->in_c, E = L->n_experts;
-    if (T > 0x7fffffff / K || n > 0x7fffffff / M || K > 1 << 26) return DASH_ESIZE;        // (offsets inside a row of weights or a row's labels: 32 bits)
+    // (offsets inside a row of weights or a row's labels, and the ends of blocks of 256 outputs: 32 bits)
+    if (T > 0x7fffffff / K || n > 0x7fffffff / M || K > 1 << 26 || M > 0x7fffffff - 255) return DASH_ESIZE;
     if (L->routing) {
         if (!L->routing->data || L->routing->ctx != c || L->routing->n != n || L->routing->n_experts != E) return DASH_EINVAL;
     } else if (E != 1) return DASH_EINVAL;

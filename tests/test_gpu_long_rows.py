@@ -48,3 +48,17 @@ def test_4_bit_floats(K):
     torch.cuda.synchronize()
     assert torch.equal(got[(tiles - 2) * 1088:], short) and short.any()
     assert (whole[K:] == 60000.0).all()
+
+
+@pytest.mark.parametrize("format", ["w8", "mx4", "f8"])
+@pytest.mark.parametrize("M", [2 ** 31 - 1, 2 ** 31 - 255])
+def test_more_outputs_than_blocks_of_them_end_in_31_bits(format, M):
+    """the blocks of 256 outputs that a layer is cut into are counted in 32 bits"""
+    from paper_2302_06361_amd import EXPERTS, F8, MX4, W8, Labels, Layer, binding
+    ctx = context([5], lam=[1])
+    some = torch.zeros(4096, dtype=torch.uint8, device=ctx.device)
+    lay = Layer(EXPERTS, 1, 1, in_c=1, out_c=M, top_k=1, n_experts=1, weights=some)
+    lay.c.weight_format = dict(w8=W8, mx4=MX4, f8=F8)[format]
+    src, dst = Labels(ctx, 1, zero=True), Labels(ctx, 1, zero=True)     # (a bundle of one label: nothing is launched for it in any case)
+    with pytest.raises(binding.DashError, match=r"\(-2\)"):
+        ctx.garble_layer(lay, src, dst)
