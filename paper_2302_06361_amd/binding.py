@@ -224,13 +224,25 @@ class Router:
 
 
 class Choice:
-    """What Context.choose fills for n rows: experts (int32 [n][top_k], -1: none), gates (int32, what COMBINE layers take), weights (float32)."""
+    """What Context.choose fills for n rows: experts (int32 [n][top_k], -1: none), gates (int32, what COMBINE layers take), weights (float32).  They may be
+    replaced by tensors of the same type and size (parts of larger ones)."""
 
     def __init__(self, ctx, n, top_k):
         import torch
-        self.n, self.top_k = int(n), int(top_k)
+        self.n, self.top_k, self.device = int(n), int(top_k), ctx.device
         self.experts, self.gates = (torch.empty((self.n, self.top_k), dtype=torch.int32, device=ctx.device) for _ in range(2))
         self.weights = torch.empty((self.n, self.top_k), dtype=torch.float32, device=ctx.device)
+
+    def __setattr__(self, name, value):
+        # (read by address in every call: looked at here, once)
+        if name in ("experts", "gates", "weights"):
+            import torch
+            dtype = torch.float32 if name == "weights" else torch.int32
+            if not torch.is_tensor(value) or value.dtype != dtype or value.numel() != self.n * self.top_k or not value.is_contiguous() or value.device != self.device:
+                raise DashError("Choice: %s has to be a contiguous tensor [%d][%d] of %s on %s" % (name, self.n, self.top_k, dtype, self.device))
+        elif name in ("n", "top_k", "device") and hasattr(self, name):
+            raise DashError("Choice: made for %d rows of %d" % (self.n, self.top_k))
+        object.__setattr__(self, name, value)
 
 
 class Layer:
