@@ -211,16 +211,23 @@ class Routing:
 
 class Router:
     """A dash_router: how Context.choose takes top_k of n_experts from a row's logits.  bias: float32 tensor [n_experts] on the device, added to
-    the scores for the choice; groups: equal groups of experts, of which the top_groups best ones (group_score) are chosen from."""
+    the scores for the choice (it may be replaced); groups: equal groups of experts, of which the top_groups best ones (group_score) are chosen from."""
 
     def __init__(self, n_experts, top_k, score=SOFTMAX, bias=None, groups=1, top_groups=1, group_score=GROUP_MAX, renormalise=True, scale=1.0, gate_bits=8):
         self.c = CRouter(int(n_experts), int(top_k), int(score), int(groups), int(top_groups), int(group_score), int(bool(renormalise)), int(gate_bits), float(scale))
         self.n_experts, self.top_k, self.bias = int(n_experts), int(top_k), bias
-        if bias is not None:
-            import torch
-            if bias.dtype != torch.float32 or not bias.is_contiguous() or bias.numel() != self.n_experts:
-                raise DashError("Router: bias has to be a contiguous float32 tensor [n_experts]")
-            self.c.bias = bias.data_ptr()
+
+    def __setattr__(self, name, value):
+        # (the library reads the descriptor: it follows another bias and keeps its sizes)
+        if name == "bias":
+            if value is not None:
+                import torch
+                if value.dtype != torch.float32 or not value.is_contiguous() or value.numel() != self.n_experts:
+                    raise DashError("Router: bias has to be a contiguous float32 tensor [n_experts]")
+            self.c.bias = None if value is None else value.data_ptr()
+        elif name in ("c", "n_experts", "top_k") and hasattr(self, name):
+            raise DashError("Router: made for %d of %d experts" % (self.top_k, self.n_experts))
+        object.__setattr__(self, name, value)
 
 
 class Choice:
