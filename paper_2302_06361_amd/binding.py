@@ -214,6 +214,10 @@ class Router:
     the scores for the choice (it may be replaced); groups: equal groups of experts, of which the top_groups best ones (group_score) are chosen from."""
 
     def __init__(self, n_experts, top_k, score=SOFTMAX, bias=None, groups=1, top_groups=1, group_score=GROUP_MAX, renormalise=True, scale=1.0, gate_bits=8):
+        given = dict(n_experts=n_experts, top_k=top_k, score=score, groups=groups, top_groups=top_groups, group_score=group_score, gate_bits=gate_bits)
+        for name, v in given.items():
+            if v != int(v) or not -2 ** 31 <= v < 2 ** 31:          # (the descriptor would hold another number)
+                raise DashError("Router: %s has to be an integer of 32 bits, got %r" % (name, v))
         self.c = CRouter(int(n_experts), int(top_k), int(score), int(groups), int(top_groups), int(group_score), int(bool(renormalise)), int(gate_bits), float(scale))
         self.n_experts, self.top_k, self.bias = int(n_experts), int(top_k), bias
 

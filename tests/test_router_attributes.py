@@ -1,4 +1,5 @@
 """A router's attributes and the descriptor that the library reads stay the same thing.  No GPU involved."""
+import numpy as np
 import pytest
 import torch
 
@@ -26,3 +27,15 @@ def test_sizes_stay(name):
     with pytest.raises(DashError):
         setattr(r, name, 1)
     assert (r.n_experts, r.top_k) == (r.c.n_experts, r.c.top_k) == (8, 2)
+
+
+@pytest.mark.parametrize("name", ["n_experts", "top_k", "score", "groups", "top_groups", "group_score", "gate_bits"])
+def test_integers_that_the_descriptor_does_not_hold(name):
+    """refused, not cut off"""
+    good = dict(n_experts=8, top_k=2, score=0, groups=1, top_groups=1, group_score=0, gate_bits=8)
+    for bad in (2 ** 32 + good[name], -2 ** 32 + good[name], 2 ** 31, good[name] + 0.5):
+        with pytest.raises(DashError, match=name):
+            Router(**dict(good, **{name: bad}))
+    for same in (np.int64(good[name]), np.uint8(good[name]), float(good[name])):
+        r = Router(**dict(good, **{name: same}))
+        assert (r.c.n_experts, r.c.top_k, r.c.score, r.c.n_groups, r.c.top_groups, r.c.group_score, r.c.gate_bits) == tuple(good.values())
