@@ -110,7 +110,7 @@ class _Routed:
         logits, bias, valid = given.pop("logits"), given.pop("bias", None), given.pop("valid", None)
         self.ctx, self.what, self.b = ctx, what, b
         self.logits = torch.as_tensor(np.ascontiguousarray(logits, dtype=np.float32)).to(ctx.device)
-        self.valid = None if valid is None else torch.as_tensor(np.ascontiguousarray(valid, dtype=np.uint8)).to(ctx.device)
+        self.valid = None if valid is None else torch.as_tensor(np.ascontiguousarray(np.asarray(valid) != 0)).to(ctx.device)          # (truth values: a byte of 256 would be 0)
         if bias is not None:
             bias = torch.as_tensor(np.ascontiguousarray(bias, dtype=np.float32)).to(ctx.device)
         self.router = B.Router(self.logits.shape[1], bias=bias, **given)
