@@ -101,18 +101,30 @@ class _PerBatch:
         return self.all[base * self.per:(base + b) * self.per]
 
 
+def _floats(values, ctx, dtypes):
+    """an array, or a tensor of any device, as a tensor of its own on the context's, in float32 or its own type among `dtypes`"""
+    import torch
+    if not torch.is_tensor(values):
+        values = torch.as_tensor(np.ascontiguousarray(values, dtype=np.float32))
+    values = values.detach()
+    return values.to(ctx.device, values.dtype if values.dtype in dtypes else torch.float32, copy=True).contiguous()
+
+
 class _Routed:
-    """experts or gates that a router chooses from the logits of the whole batch, top_k for every batch element"""
+    """experts or gates that a router chooses from the logits (an array or a tensor) of the whole batch, top_k for every batch element"""
 
     def __init__(self, router, per, ctx, b, what):
         import torch
         given = dict(router)
         logits, bias, valid = given.pop("logits"), given.pop("bias", None), given.pop("valid", None)
         self.ctx, self.what, self.b = ctx, what, b
-        self.logits = torch.as_tensor(np.ascontiguousarray(logits, dtype=np.float32)).to(ctx.device)
-        self.valid = None if valid is None else torch.as_tensor(np.ascontiguousarray(np.asarray(valid) != 0)).to(ctx.device)          # (truth values: a byte of 256 would be 0)
+        self.logits = _floats(logits, ctx, (torch.float32, torch.bfloat16, torch.float16))
+        # (truth values: a byte of 256 would be 0)
+        if valid is not None:
+            valid = valid.to(ctx.device) != 0 if torch.is_tensor(valid) else torch.as_tensor(np.ascontiguousarray(np.asarray(valid) != 0)).to(ctx.device)
+        self.valid = valid
         if bias is not None:
-            bias = torch.as_tensor(np.ascontiguousarray(bias, dtype=np.float32)).to(ctx.device)
+            bias = _floats(bias, ctx, (torch.float32,))
         self.router = B.Router(self.logits.shape[1], bias=bias, **given)
         if self.router.top_k != per:
             raise ValueError("router: top_k is %d, the layer takes %d rows of a batch element" % (self.router.top_k, per))
