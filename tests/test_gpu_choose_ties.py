@@ -110,3 +110,23 @@ def test_small_scores_under_large_scales(ctx, x):
     for top_k in (1, 2, 4):
         got = ctx.choose(Router(8, top_k, score=SIGMOID, scale=2.0 ** 30, gate_bits=0), l)
         assert (got.gates == 2 ** 30 // top_k).all() and (got.weights == 2.0 ** 30 / top_k).all()
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("renormalise", [False, True])
+def test_gates_next_to_a_middle(ctx, sigmoid, renormalise):
+    """millions of gates of 30 bits, some so near to a middle that the remainder decides (2^-18), but farther than 64 bits leave open: the sum, quotient and products of the
+    reference and the scores are off by less than 2^-49 of a gate of up to 2^30, 2^-19"""
+    from paper_2302_06361_amd import SIGMOID, SOFTMAX, Router
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    l = 1.5 * torch.randn((500000, 16), device="cuda", generator=g)
+    got = ctx.choose(Router(16, 8, score=SIGMOID if sigmoid else SOFTMAX, renormalise=renormalise, gate_bits=30), l)
+    d = l.double()
+    s = 1 / (1 + torch.exp(-d)) if sigmoid else torch.exp(d - d.amax(1, keepdim=True))
+    chosen = s.gather(1, got.experts.long())
+    t = chosen / (chosen.sum(1, keepdim=True) if renormalise else 1 if sigmoid else s.sum(1, keepdim=True)) * 2.0 ** 30
+    off = (t - t.floor() - 0.5).abs()
+    assert int(((off > 2.0 ** -19) & (off < 2.0 ** -18)).sum()) >= 5
+    wrong = (got.gates.double() != torch.round(t)) & (off > 2.0 ** -19)
+    assert not wrong.any(), (int(wrong.sum()), t[wrong][:3].tolist())
