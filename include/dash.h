@@ -175,7 +175,7 @@ int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void
  * inputs are known, so rows are routed by what is known then (the client, the task, a position), never by a label.
  *
  * Sums are held in 31 bits: in_c times 256 (p - 1) for DASH_W8 and DASH_F8, (p - 1)^2 for DASH_MX4, has to stay below 2^31 for the largest prime p,
- * else DASH_ESIZE.
+ * else DASH_ESIZE; so for more than 2^31 - 256 outputs.
  *
  * Prepared weights of an EXPERTS layer: n_experts matrices [out_c][K] one after the other, 16-byte aligned, independent of the
  * primes.  A matrix is cut into tiles of 32 rows x 64 columns, row tiles outermost, zeros past out_c and K.
@@ -185,7 +185,8 @@ int dash_weights_prepare(dash_ctx *ctx, const int32_t *w, int out_c, int K, void
  *   DASH_F8   tiles as DASH_W8's with codes in place of the weights; behind a matrix's tiles the scales, int32 [ceil(out_c / 128)][ceil(K / 128)],
  *             padded to a multiple of 16 bytes.  A code is an e4m3 float: bit 7 the sign, bits 3..6 the exponent e, bits 0..2 the mantissa m,
  *             (1 + m/8) 2^(e - 7), or m 2^-9 where e = 0; 0x7f and 0xff, not a number, are stored as 0.  The weight that enters the layer is the
- *             integer 512 * e4m3 * scale. */
+ *             integer 512 * e4m3 * scale.  The product of the primes has to hold the sums of these: 458752 * scale at least for one of the largest code
+ *             (8 primes from 2 on, 9699690, up to a scale of 21; 12 primes, 7.4e12). */
 size_t dash_expert_weights_bytes(int format, int n_experts, int out_c, int K);
 /* DASH_W8.  w: device int8, element (e, j, i) at w[e * expert_stride + j * row_stride + i] (row_stride >= K, expert_stride
  * >= 0). */
@@ -203,7 +204,8 @@ int dash_mx4_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_strid
 /* DASH_F8, quantised on the device.  w, dtype, strides, values as for dash_mx4_quantise.  The weights of a block of 128 rows by 128 columns
  * (fewer at the ends) with largest magnitude a get the scale S = ceil(a / (448 * 2^base)), brought into [1, max_scale] (-64 <= base <= 64, 1 <=
  * max_scale <= 32767); each weight becomes the e4m3 value nearest to w / (S 2^base), ties to the even code, magnitudes past 448 the 448.  The
- * layer multiplies by integers in units of 2^(base - 9), at most 229376 * max_scale of them.  A NaN counts as 0, an infinity as the
+ * layer multiplies by integers in units of 2^(base - 9), at most 229376 * max_scale of them.  (From base = ceil(log2(largest magnitude /
+ * (448 * max_scale))) on no weight is clipped; a larger base makes the integers smaller, and weights below 2^(base - 6) are then steps of 2^(base - 9).)  A NaN counts as 0, an infinity as the
  * largest float32; no sign on a zero.  values: e4m3 * S * 2^base, rounded once to `dtype`. */
 int dash_f8_quantise(dash_ctx *ctx, const void *w, int dtype, int64_t row_stride, int64_t expert_stride, int n_experts, int out_c,
                      int K, int base, int max_scale, void *prepared, void *values, void *hip_stream);

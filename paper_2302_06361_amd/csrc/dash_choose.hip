@@ -105,7 +105,8 @@ __device__ __forceinline__ float half_logit(uint16_t v, int dtype) {
 // their order but for sums that it makes equal; a wave that meets equal ones among its largest does its rounds again with the sums themselves (rounds in 64 bits for all: 44.1 us).
 // Bound by vector instructions where rows are many, a third of them the exponentials (13 steps in 64 bits an expert; a float32 sum would move a choice or a gate): 65536 rows of 256 experts,
 // eight chosen, 40.5 us, 64 % of the cycles, 39.8 MB read and written in 8.2 us at a copy's rate.  Few rows: the steps of one row's lanes one after the other, which more lanes make fewer.
-// 4096 rows of 256 in eight groups, four of them: 9.8 us; 1000 rows of 160 in eight groups: 5.8; one row of 8: 4.7 to 5.2.
+// 4096 rows of 256 in eight groups, four of them: 9.5 us; 1000 rows of 160 in eight groups: 5.9; one row of 8: 4.7.
+// What looks for gates next to a middle costs 0.05 to 0.1 us, 0.35 where 65536 rows of 16 are chosen from without renormalisation (7.6 -> 7.95); a quotient by division 0.15 more there.
 constexpr int kChooseThreads = 256;
 template <int L, int V, bool BIAS, bool GROUPS, bool SIGMOID>
 __global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
@@ -203,7 +204,7 @@ __global__ __launch_bounds__(kChooseThreads) void k_choose(const ChooseArgs A) {
         for (int v = 0; v < V; v++) s_key[rr][lane * P + v] = key[v];
         lds_order();
         const int n = A.group_n;
-        // share_log2: 2^share_log2 neighbouring lanes find a group's two largest, all 16 lanes at work
+        // share_log2: 2^share_log2 neighbouring lanes find a group's two largest, all L lanes at work
         const int share = 1 << A.share_log2;
         for (int g = lane >> A.share_log2; g < A.n_groups; g += L >> A.share_log2) {
             Key a = kNone, b = kNone;
@@ -460,7 +461,7 @@ int dash_choose(dash_ctx* c, const dash_router* r, const void* logits, int dtype
     constexpr integral_constant<int, 16> l16{};
     constexpr integral_constant<int, 32> l32{};
     constexpr integral_constant<int, 64> l64{};
-    // Lanes of a row.  What they do for their own experts one after the other takes the time where rows are few, and with sums in 64 bits and groups of many experts also where they are many; each
+    // Lanes of a row (times without the search for gates next to a middle, which adds 0.05 to 0.1 us to each).  What they do for their own experts one after the other takes the time where rows are few, and with sums in 64 bits and groups of many experts also where they are many; each
     // round costs instructions by the lane.  us with 16, 32, 64 lanes, eight chosen of 256 experts with a bias and groups (sigmoid): 1 row 9.5, 7.2, 6.2; 1000: 10.2, 7.7, 6.7; 2048: 10.2, 7.9, 7.9;
     // 4096: 10.3, 9.8, 10.7; 8192: 14.0, 13.5, 16.8; 65536: 66.6, 67.7, 103; with neither: 4.0, 3.9, 4.1 for one row, 18.6, 27.7, 49.1 for 65536.  Of 128: 1000 rows 7.7, 6.4, 6.4;
     // 8192: 10.2, 10.5, 15.6.  Of 512: 1000 rows 15.9, 10.3, 8.0; 2048: 16.0, 10.3, 9.9; 4096: 16.2, 14.1, 13.8; 16384: 41.6, 33.7, 36.4; with neither 1 row 5.1, 3.9, 4.1, 65536: 30.4, 32.1, 52.8.  Of 1024, 32 and 64: 1000 rows 15.8, 10.4;
